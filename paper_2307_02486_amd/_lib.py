@@ -35,6 +35,12 @@ class PlanInfo(ctypes.Structure):
                 ("bytes_combine", ctypes.c_double)]
 
 
+class PagedCacheArgs(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("seq_lens", ctypes.c_void_p), ("q_start", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int64), ("max_pages", ctypes.c_int64)]
+
+
 class DilatedAttnError(RuntimeError):
     def __init__(self, code: int, lib):
         self.code = code
@@ -83,6 +89,21 @@ def load():
     lib.dilated_attn_layernorm_bwd_workspace.restype = ctypes.c_int
     lib.dilated_attn_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, ctypes.c_uint64, vp]
     lib.dilated_attn_layernorm_bwd.restype = ctypes.c_int
+    u64 = ctypes.c_uint64
+    lib.dilated_attn_qk_norm_xpos.argtypes = [vp] * 6 + [i64] * 7 + [f32, i64, f32, f32, f32, i64, vp]
+    lib.dilated_attn_qk_norm_xpos.restype = ctypes.c_int
+    lib.dilated_attn_qk_norm_xpos_bwd_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(u64)]
+    lib.dilated_attn_qk_norm_xpos_bwd_workspace.restype = ctypes.c_int
+    lib.dilated_attn_qk_norm_xpos_bwd.argtypes = [vp] * 10 + [i64] * 7 + [f32, i64, f32, f32, f32, i64, vp, u64, vp]
+    lib.dilated_attn_qk_norm_xpos_bwd.restype = ctypes.c_int
+    cache = ctypes.POINTER(PagedCacheArgs)
+    lib.dilated_attn_cache_append.argtypes = [vp] * 6 + [cache] + [i64] * 8 + [f32, i64, i64, f32, f32, f32, i64, vp]
+    lib.dilated_attn_cache_append.restype = ctypes.c_int
+    lib.dilated_attn_paged_workspace.argtypes = [i64] * 9 + [ctypes.POINTER(Pattern), i64, i64, ctypes.POINTER(u64)]
+    lib.dilated_attn_paged_workspace.restype = ctypes.c_int
+    lib.dilated_attn_paged_fwd.argtypes = [vp, cache, vp, vp] + [i64] * 7 + [ctypes.POINTER(Pattern), i64, i64, f32,
+                                                                            vp, u64, vp]
+    lib.dilated_attn_paged_fwd.restype = ctypes.c_int
     lib.dilated_attn_strerror.argtypes = [ctypes.c_int]
     lib.dilated_attn_strerror.restype = ctypes.c_char_p
     lib.dilated_attn_profile_begin.argtypes = [i64]

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <vector>
@@ -34,6 +35,55 @@ void destroy_events(ProfileWindow& w) {
   w.ev.clear();
   w.active = false;
   w.capacity = w.used = 0;
+}
+
+// Whether the parameters of an xPos rotation of positions 0 .. last are valid
+// (see dilated_attn_xpos: the scale exponents stay within 2^+-64).
+bool xpos_ok(int64_t center, int64_t last, float base, float gamma, float scale_base) {
+  if (center < 0 || center > last) return false;
+  if (!std::isfinite(base) || !(base > 1.0f) || !std::isfinite(gamma) || !(gamma > 0.0f) ||
+      !std::isfinite(scale_base) || !(scale_base > 0.0f))
+    return false;
+  // zeta_i ranges over [gamma / (1 + gamma), 1): the smallest gives the
+  // largest |log2 zeta| (every zeta_i < 1 for gamma > 0 and i < D/2).
+  const double l2z = std::fabs(std::log2(static_cast<double>(gamma) / (1.0 + gamma)));
+  return static_cast<double>(std::max(center, last - center)) / scale_base * l2z <= 64.0;
+}
+
+// Bytes of n tokens of `row` elements each, `stride` elements apart.
+uint64_t strided_bytes(int64_t n, int64_t row, int64_t stride, int64_t esize) {
+  return n > 0 ? static_cast<uint64_t>((n - 1) * stride + row) * esize : 0;
+}
+
+// Head counts, head size, type and token strides that the head operators take.
+int head_shapes(int64_t tokens, int64_t H, int64_t Hkv, int64_t D, int64_t dtype, const int64_t* strides,
+                const int64_t* heads, int n) {
+  if (tokens < 0 || tokens >= (int64_t{1} << 31) || H < 1 || H >= (int64_t{1} << 16) || Hkv < 1 ||
+      Hkv >= (int64_t{1} << 16))
+    return DA_EINVAL;
+  if (dtype != DA_BF16 && dtype != DA_F32) return DA_EUNSUPPORTED;
+  if (D != 32 && D != 64 && D != 128) return DA_EUNSUPPORTED;
+  for (int i = 0; i < n; ++i) {
+    if (strides[i] < heads[i] * D || strides[i] >= (int64_t{1} << 32)) return DA_EINVAL;
+    if (strides[i] % (dtype == DA_BF16 ? 8 : 4)) return DA_EALIGN;
+  }
+  return DA_OK;
+}
+
+struct Span {
+  const void* p;
+  uint64_t bytes;
+};
+
+// Whether an output overlaps another output or an input.
+bool any_overlap(const Span* outs, int no, const Span* ins, int ni) {
+  for (int i = 0; i < no; ++i) {
+    for (int j = i + 1; j < no; ++j)
+      if (overlaps(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return true;
+    for (int j = 0; j < ni; ++j)
+      if (overlaps(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes)) return true;
+  }
+  return false;
 }
 
 }  // namespace
@@ -162,19 +212,11 @@ int dilated_attn_xpos(const void* x, void* y, int64_t B, int64_t N, int64_t H, i
   if (B <= 0 || N <= 0 || H <= 0 || D < 8 || D > 256 || D % 8 != 0) return DA_EINVAL;
   if (dtype != DA_BF16 && dtype != DA_F32) return DA_EUNSUPPORTED;
   if ((sign != 1 && sign != -1) || (transpose != 0 && transpose != 1)) return DA_EINVAL;
-  if (center < 0 || center >= N) return DA_EINVAL;
-  if (!std::isfinite(base) || !(base > 1.0f) || !std::isfinite(gamma) || !(gamma > 0.0f) ||
-      !std::isfinite(scale_base) || !(scale_base > 0.0f))
-    return DA_EINVAL;
   // At most 2^34 elements: one thread per 8 keeps the grid within 2^32 work-items.
   if (B > (int64_t{1} << 34) / N || B * N > (int64_t{1} << 34) / H ||
       B * N * H > (int64_t{1} << 34) / D)
     return DA_EINVAL;
-  // zeta_i ranges over [gamma / (1 + gamma), 1): the smallest gives the
-  // largest |log2 zeta| (every zeta_i < 1 for gamma > 0 and i < D/2).
-  const double l2z = std::fabs(std::log2(static_cast<double>(gamma) / (1.0 + gamma)));
-  const double far = static_cast<double>(std::max(center, N - 1 - center));
-  if (far / scale_base * l2z > 64.0) return DA_EINVAL;
+  if (!xpos_ok(center, N - 1, base, gamma, scale_base)) return DA_EINVAL;
   if (!aligned16(x) || !aligned16(y)) return DA_EALIGN;
   const uint64_t bytes = static_cast<uint64_t>(B * N * H * D) * (dtype == DA_BF16 ? 2 : 4);
   if (x != y && overlaps(x, bytes, y, bytes)) return DA_EINVAL;
@@ -273,6 +315,163 @@ int dilated_attn_layernorm_bwd(const void* dy, const void* x, const void* g, con
                                static_cast<hipStream_t>(stream)) != hipSuccess)
     return DA_EHIP;
   return DA_OK;
+}
+
+int dilated_attn_qk_norm_xpos(const void* q, const void* k, const void* qw, const void* kw, void* qo, void* ko,
+                              int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride,
+                              int64_t k_stride, float eps, int64_t center, float base, float gamma,
+                              float scale_base, int64_t dtype, void* stream) {
+  if (!q || !k || !qw || !kw || !qo || !ko) return DA_EINVAL;
+  if (B < 1 || N < 1 || B >= (int64_t{1} << 31) / N || !std::isfinite(eps) || !(eps >= FLT_MIN)) return DA_EINVAL;
+  const int64_t strides[2] = {q_stride, k_stride}, heads[2] = {H, Hkv};
+  if (const int rc = head_shapes(B * N, H, Hkv, D, dtype, strides, heads, 2); rc != DA_OK) return rc;
+  if (!xpos_ok(center, N - 1, base, gamma, scale_base)) return DA_EINVAL;
+  for (const void* p : {q, k, qw, kw, static_cast<const void*>(qo), static_cast<const void*>(ko)})
+    if (!aligned16(p)) return DA_EALIGN;
+  const int64_t T = B * N, es = dtype == DA_BF16 ? 2 : 4;
+  const uint64_t wb = static_cast<uint64_t>(D * es);
+  const Span ins[4] = {{q, strided_bytes(T, H * D, q_stride, es)}, {k, strided_bytes(T, Hkv * D, k_stride, es)},
+                       {qw, wb}, {kw, wb}};
+  const Span outs[2] = {{qo, static_cast<uint64_t>(T * H * D * es)}, {ko, static_cast<uint64_t>(T * Hkv * D * es)}};
+  if (any_overlap(outs, 2, ins, 4)) return DA_EINVAL;
+  const da::QkNormCall c{q, k, qw, kw, qo, ko, B, N, H, Hkv, D, q_stride, k_stride, eps,
+                         {true, center, base, gamma, scale_base}, static_cast<int>(dtype)};
+  return da::launch_qk_norm(c, static_cast<hipStream_t>(stream)) == hipSuccess ? DA_OK : DA_EHIP;
+}
+
+int dilated_attn_qk_norm_xpos_bwd_workspace(int64_t B, int64_t N, int64_t D, uint64_t* bytes) {
+  if (!bytes || B < 1 || N < 1 || B >= (int64_t{1} << 31) / N) return DA_EINVAL;
+  if (D != 32 && D != 64 && D != 128) return DA_EUNSUPPORTED;
+  *bytes = da::qk_norm_bwd_workspace(B * N, D);
+  return DA_OK;
+}
+
+int dilated_attn_qk_norm_xpos_bwd(const void* dqo, const void* dko, const void* q, const void* k, const void* qw,
+                                  const void* kw, void* dq, void* dk, void* dqw, void* dkw, int64_t B, int64_t N,
+                                  int64_t H, int64_t Hkv, int64_t D, int64_t q_stride, int64_t k_stride, float eps,
+                                  int64_t center, float base, float gamma, float scale_base, int64_t dtype,
+                                  void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!dqo || !dko || !q || !k || !qw || !kw || !dq || !dk || !dqw || !dkw || !workspace) return DA_EINVAL;
+  if (!std::isfinite(eps) || !(eps >= FLT_MIN)) return DA_EINVAL;
+  uint64_t need = 0;
+  if (const int rc = dilated_attn_qk_norm_xpos_bwd_workspace(B, N, D, &need); rc != DA_OK) return rc;
+  const int64_t strides[2] = {q_stride, k_stride}, heads[2] = {H, Hkv};
+  if (const int rc = head_shapes(B * N, H, Hkv, D, dtype, strides, heads, 2); rc != DA_OK) return rc;
+  if (!xpos_ok(center, N - 1, base, gamma, scale_base)) return DA_EINVAL;
+  for (const void* p : {dqo, dko, q, k, qw, kw, static_cast<const void*>(dq), static_cast<const void*>(dk),
+                        static_cast<const void*>(dqw), static_cast<const void*>(dkw),
+                        static_cast<const void*>(workspace)})
+    if (!aligned16(p)) return DA_EALIGN;
+  if (workspace_bytes < need) return DA_EWORKSPACE;
+  const int64_t T = B * N, es = dtype == DA_BF16 ? 2 : 4;
+  const uint64_t wb = static_cast<uint64_t>(D * es), qb = static_cast<uint64_t>(T * H * D * es),
+                 kb = static_cast<uint64_t>(T * Hkv * D * es);
+  const Span ins[6] = {{dqo, qb}, {dko, kb}, {q, strided_bytes(T, H * D, q_stride, es)},
+                       {k, strided_bytes(T, Hkv * D, k_stride, es)}, {qw, wb}, {kw, wb}};
+  const Span outs[5] = {{dq, qb}, {dk, kb}, {dqw, wb}, {dkw, wb}, {workspace, need}};
+  if (any_overlap(outs, 5, ins, 6)) return DA_EINVAL;
+  const da::QkNormCall c{q, k, qw, kw, nullptr, nullptr, B, N, H, Hkv, D, q_stride, k_stride, eps,
+                         {true, center, base, gamma, scale_base}, static_cast<int>(dtype)};
+  return da::launch_qk_norm_bwd(c, dqo, dko, dq, dk, dqw, dkw, workspace, static_cast<hipStream_t>(stream)) ==
+                 hipSuccess
+             ? DA_OK
+             : DA_EHIP;
+}
+
+namespace {
+
+// Cache sizes that both paged calls take; the rows fit 32-bit indices.
+bool cache_ok(int64_t B, int64_t Hkv, const da_paged_cache_t* c) {
+  if (!c || !c->k || !c->v || !c->block_table || !c->seq_lens || !c->q_start) return false;
+  constexpr int64_t kMost = int64_t{1} << 31;
+  return B >= 1 && B < kMost && c->page_size >= 1 && c->page_size <= (int64_t{1} << 16) &&
+         (c->page_size & (c->page_size - 1)) == 0 && c->max_pages >= 1 && c->max_pages < kMost / c->page_size &&
+         c->num_pages >= 1 && c->num_pages < kMost && c->num_pages <= (int64_t{1} << 32) / c->page_size / Hkv;
+}
+
+da::PagedCache paged_cache(const da_paged_cache_t* c) {
+  int page_log2 = 0;
+  while ((int64_t{1} << page_log2) < c->page_size) ++page_log2;
+  return da::PagedCache{c->k, c->v, c->block_table, c->seq_lens, c->q_start, c->num_pages, c->max_pages, page_log2};
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace
+
+int dilated_attn_cache_append(const void* q, const void* k, const void* v, const void* qw, const void* kw, void* qo,
+                              const da_paged_cache_t* cache, int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D,
+                              int64_t q_stride, int64_t k_stride, int64_t v_stride, float eps, int64_t rotate,
+                              int64_t center, float base, float gamma, float scale_base, int64_t dtype,
+                              void* stream) {
+  const int64_t strides[3] = {k_stride, v_stride, q_stride}, heads[3] = {Hkv, Hkv, H};
+  if (const int rc = head_shapes(T, H, Hkv, D, dtype, strides, heads, q ? 3 : 2); rc != DA_OK) return rc;
+  if (!cache_ok(B, Hkv, cache) || (T > 0 && (!k || !v)) || (q != nullptr) != (qo != nullptr)) return DA_EINVAL;
+  if (((qw || kw) && (!std::isfinite(eps) || !(eps >= FLT_MIN))) || (rotate != 0 && rotate != 1)) return DA_EINVAL;
+  if (rotate && !xpos_ok(center, cache->max_pages * cache->page_size - 1, base, gamma, scale_base)) return DA_EINVAL;
+  for (const void* p : {q, k, v, qw, kw, static_cast<const void*>(qo), static_cast<const void*>(cache->k),
+                        static_cast<const void*>(cache->v)})
+    if (!aligned16(p)) return DA_EALIGN;
+  if (!aligned4(cache->block_table) || !aligned4(cache->seq_lens) || !aligned4(cache->q_start)) return DA_EALIGN;
+  const int64_t es = dtype == DA_BF16 ? 2 : 4;
+  const uint64_t wb = static_cast<uint64_t>(D * es),
+                 cb = static_cast<uint64_t>(cache->num_pages * cache->page_size * Hkv) * static_cast<uint64_t>(D * es);
+  const Span ins[8] = {{q, q ? strided_bytes(T, H * D, q_stride, es) : 0}, {k, strided_bytes(T, Hkv * D, k_stride, es)},
+                       {v, strided_bytes(T, Hkv * D, v_stride, es)}, {qw, qw ? wb : 0}, {kw, kw ? wb : 0},
+                       {cache->block_table, static_cast<uint64_t>(B) * cache->max_pages * 4},
+                       {cache->seq_lens, static_cast<uint64_t>(B) * 4}, {cache->q_start, static_cast<uint64_t>(B + 1) * 4}};
+  const Span outs[3] = {{qo, qo ? static_cast<uint64_t>(T * H * D * es) : 0}, {cache->k, cb}, {cache->v, cb}};
+  if (any_overlap(outs, 3, ins, 8)) return DA_EINVAL;
+  if (T == 0) return DA_OK;
+  const da::QkNormCall c{q, k, qw, kw, qo, nullptr, B, 0, H, Hkv, D, q_stride, k_stride, eps,
+                         {rotate != 0, rotate ? center : 0, base, gamma, scale_base}, static_cast<int>(dtype)};
+  return da::launch_cache_append(c, v, v_stride, paged_cache(cache), T, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? DA_OK
+             : DA_EHIP;
+}
+
+int dilated_attn_paged_workspace(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages,
+                                 int64_t page_size, int64_t max_pages, int64_t max_new, const da_pattern_t* patterns,
+                                 int64_t num_patterns, int64_t dtype, uint64_t* bytes) {
+  if (!bytes) return DA_EINVAL;
+  da::PagedPlan p;
+  const int rc = da::make_paged_plan(T, B, H, Hkv, D, num_pages, page_size, max_pages, max_new, patterns,
+                                     num_patterns, dtype, 0.0f, &p);
+  if (rc == DA_OK) *bytes = p.workspace_bytes;
+  return rc;
+}
+
+int dilated_attn_paged_fwd(const void* q, const da_paged_cache_t* cache, void* out, float* lse, int64_t T, int64_t B,
+                           int64_t H, int64_t Hkv, int64_t D, int64_t q_stride, int64_t max_new,
+                           const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype, float softmax_scale,
+                           void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (const int rc = head_shapes(T, H, Hkv, D, dtype, &q_stride, &H, 1); rc != DA_OK) return rc;
+  if (!cache_ok(B, Hkv, cache)) return DA_EINVAL;
+  da::PagedPlan p;
+  if (const int rc = da::make_paged_plan(T, B, H, Hkv, D, cache->num_pages, cache->page_size, cache->max_pages,
+                                         max_new, patterns, num_patterns, dtype, softmax_scale, &p);
+      rc != DA_OK)
+    return rc;
+  if (T == 0) return DA_OK;
+  if (!q || !out || !lse || !workspace) return DA_EINVAL;
+  for (const void* x : {q, static_cast<const void*>(out), static_cast<const void*>(workspace),
+                        static_cast<const void*>(cache->k), static_cast<const void*>(cache->v)})
+    if (!aligned16(x)) return DA_EALIGN;
+  if (!aligned4(cache->block_table) || !aligned4(cache->seq_lens) || !aligned4(cache->q_start) || !aligned4(lse))
+    return DA_EALIGN;
+  if (workspace_bytes < p.workspace_bytes) return DA_EWORKSPACE;
+  const int64_t es = dtype == DA_BF16 ? 2 : 4;
+  const uint64_t cb = static_cast<uint64_t>(cache->num_pages * cache->page_size * Hkv) * static_cast<uint64_t>(D * es);
+  const Span ins[6] = {{q, strided_bytes(T, H * D, q_stride, es)}, {cache->k, cb}, {cache->v, cb},
+                       {cache->block_table, static_cast<uint64_t>(B) * cache->max_pages * 4},
+                       {cache->seq_lens, static_cast<uint64_t>(B) * 4}, {cache->q_start, static_cast<uint64_t>(B + 1) * 4}};
+  const Span outs[3] = {{out, static_cast<uint64_t>(T * H * D * es)}, {lse, static_cast<uint64_t>(T * H) * 4},
+                        {workspace, p.workspace_bytes}};
+  if (any_overlap(outs, 3, ins, 6)) return DA_EINVAL;
+  return da::launch_paged(p, q, q_stride, paged_cache(cache), out, lse, workspace, static_cast<hipStream_t>(stream)) ==
+                 hipSuccess
+             ? DA_OK
+             : DA_EHIP;
 }
 
 int dilated_attn_profile_begin(int64_t capacity) {

@@ -1,6 +1,7 @@
 // Host-side plan of a dilated-attention forward call (see plan.h).
 #include "plan.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -177,6 +178,93 @@ int make_bwd_layout(const Plan& p, BwdLayout* out) {
   l.bytes_combine = static_cast<double>(rows_all) * 3.0 * D * es + cov * 3.0 * grad_row;
   if (l.delta_pass) l.bytes_combine += static_cast<double>(rows_all) * (2.0 * D * es + 4.0 + 8.0);
   *out = l;
+  return DA_OK;
+}
+
+int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages, int64_t page,
+                    int64_t max_pages, int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns,
+                    int64_t dtype, float softmax_scale, PagedPlan* out) {
+  constexpr int64_t kMost = int64_t{1} << 31;
+  if (!patterns || !out) return DA_EINVAL;
+  if (T < 0 || T >= kMost || B < 1 || B >= kMost || H < 1 || H >= (int64_t{1} << 16) || Hkv < 1 || H % Hkv)
+    return DA_EINVAL;
+  if (page < 1 || page > (int64_t{1} << 16) || (page & (page - 1)) || max_pages < 1 || max_pages >= kMost / page ||
+      num_pages < 1 || num_pages > (int64_t{1} << 32) / page / Hkv || num_pages >= kMost || max_new < 0)
+    return DA_EINVAL;
+  if (num_patterns < 1 || num_patterns > DA_MAX_PATTERNS) return DA_EINVAL;
+  if (!(softmax_scale >= 0.0f) || std::isinf(softmax_scale)) return DA_EINVAL;
+  for (int64_t i = 0; i < num_patterns; ++i)
+    if (patterns[i].w < 1 || patterns[i].r < 1 || patterns[i].r > patterns[i].w) return DA_EINVAL;
+  if (dtype != DA_F32 && dtype != DA_BF16) return DA_EUNSUPPORTED;
+  if (D != 32 && D != 64 && D != 128) return DA_EUNSUPPORTED;
+
+  PagedPlan p;
+  std::memset(&p, 0, sizeof(p));
+  p.T = T; p.B = B; p.H = H; p.Hkv = Hkv; p.D = D;
+  p.num_pages = num_pages; p.page = page; p.max_pages = max_pages;
+  p.dtype = static_cast<int>(dtype);
+  while ((int64_t{1} << p.page_log2) < page) ++p.page_log2;
+  p.npat = static_cast<int>(num_patterns);
+  p.scale = softmax_scale > 0.0f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(double(D)));
+  const int64_t reach = max_pages * page;  // positions that the table holds
+  p.all_few = dtype == DA_F32 || std::min(max_new, T) <= kPagedFew;
+  p.by_token = p.all_few || T <= B * kPagedFew;
+  p.singles = p.by_token ? T : B * kPagedFew;
+  const int64_t G = H / Hkv;
+  const int64_t units = dtype == DA_F32 ? p.singles * H : p.singles * Hkv * ((G + kPagedGroupRows - 1) / kPagedGroupRows);
+  // Workgroups with work if every listed token were there (a pattern's rows
+  // belong to one head in r), and of the tiles.
+  double one_busy = 0.0, tile_busy = 0.0;
+  for (int i = 0; i < p.npat; ++i) {
+    const double r = static_cast<double>(patterns[i].r);
+    one_busy += units * std::min(1.0, (dtype == DA_F32 ? 1.0 : double(G)) / r);
+    tile_busy += H * std::ceil(double(T) / r / kPagedRows);
+  }
+  int64_t items = 0;
+  for (int i = 0; i < p.npat; ++i) {
+    PagedPattern& t = p.pat[i];
+    t.w = static_cast<int32_t>(std::min(patterns[i].w, reach));
+    // a dilation beyond the table's reach keeps one row of a segment, whatever it is
+    t.r = static_cast<int32_t>(std::min(patterns[i].r, kMost - 1));
+    t.fw = make_fastdiv(static_cast<uint32_t>(t.w));
+    t.fr = make_fastdiv(static_cast<uint32_t>(t.r));
+    const int64_t keys = (t.w + int64_t{t.r} - 1) / t.r;  // of a row, at most
+    const int64_t one = std::max<int64_t>(
+        1, std::min({static_cast<int64_t>(4096.0 / std::max(1.0, one_busy)), (keys + 127) / 128, int64_t{64}}));
+    t.one_split = make_fastdiv(static_cast<uint32_t>(one));
+    t.one_slot = static_cast<int32_t>(p.one_slots);
+    p.one_slots += one;
+    if (p.all_few) continue;
+    const int64_t ts = std::max<int64_t>(
+        1, std::min({static_cast<int64_t>(512.0 / std::max(1.0, tile_busy)), (keys + 511) / 512, int64_t{16}}));
+    t.tile_splits = static_cast<int32_t>(ts);
+    t.tile_slot = static_cast<int32_t>(p.tile_slots);
+    p.tile_slots += ts;
+    // A sequence of n tokens touches at most n / w + 2 segments, each with one
+    // tile more than its rows fill.
+    const int64_t tiles = std::min(T, T / (int64_t{t.r} * kPagedRows) + T / t.w + 2 * B + 2);
+    if (items + tiles * H * ts >= kMost) return DA_EINVAL;
+    t.tiles = static_cast<int32_t>(tiles);
+    t.item_begin = static_cast<int32_t>(items);
+    items += tiles * H * ts;
+  }
+  p.tile_items = items;
+  p.one_items = (units + 7) / 8 * 8 * p.one_slots;
+  if (p.one_items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
+  uint64_t off = 0;
+  auto take = [&off](uint64_t bytes) {
+    const uint64_t at = off;
+    off = align_up(off + bytes);
+    return at;
+  };
+  const uint64_t one_rows = static_cast<uint64_t>(p.singles * H * p.one_slots);
+  const uint64_t tile_rows = static_cast<uint64_t>(p.T * H * p.tile_slots);
+  p.one_rec_off = take(one_rows * 4);
+  p.one_row_off = take(one_rows * D * 4);
+  p.tile_rec_off = take(tile_rows * 8);
+  p.tile_row_off = take(tile_rows * D * 2);
+  p.workspace_bytes = off;
+  *out = p;
   return DA_OK;
 }
 

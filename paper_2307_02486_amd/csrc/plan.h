@@ -109,4 +109,42 @@ int make_plan(int64_t B, int64_t N, int64_t H, int64_t D, const da_pattern_t* pa
               int64_t num_patterns, int64_t causal, int64_t dtype, float softmax_scale,
               Plan* out);
 
+// Attention over a paged cache.  A sequence's new tokens are computed in one of
+// two ways: each token by itself (all its keys' splits in parallel), or in
+// tiles of kept query rows.  A sequence of at most kPagedFew new tokens takes
+// the first.  Both write one partial row per (token, head) and slot, a slot
+// being one split of one pattern's keys, and the join reads them.
+constexpr int64_t kPagedFew = 8;
+constexpr int64_t kPagedRows = 128;      // query rows of a tile
+constexpr int64_t kPagedKeyTile = 64;    // its keys at a time
+constexpr int64_t kPagedGroupRows = 16;  // query heads of one key head that a token's workgroup holds
+
+struct PagedPattern {
+  int32_t w, r;              // segment length (clamped to the table's reach), dilation
+  FastDiv fw, fr;            // divisions by them
+  FastDiv one_split;         // division by the splits of a single token's keys
+  int32_t one_slot;          // its first slot there
+  int32_t tile_splits;       // splits of a tile's keys
+  int32_t tile_slot;         // its first slot there
+  int32_t tiles;             // bound on the pattern's query tiles per head
+  int32_t item_begin;        // its first workgroup of the tile launch
+};
+
+struct PagedPlan {
+  int64_t T, B, H, Hkv, D, num_pages, page, max_pages;
+  int dtype, page_log2, npat;
+  float scale;
+  bool all_few;              // every token by itself
+  bool by_token;             // single tokens are listed by token, else as (sequence, token < kPagedFew)
+  int64_t singles;           // tokens listed for the first way
+  int64_t one_slots, tile_slots;
+  int64_t one_items, tile_items;  // workgroups
+  uint64_t one_rec_off, one_row_off, tile_rec_off, tile_row_off, workspace_bytes;
+  PagedPattern pat[DA_MAX_PATTERNS];
+};
+
+int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages, int64_t page,
+                    int64_t max_pages, int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns,
+                    int64_t dtype, float softmax_scale, PagedPlan* out);
+
 }  // namespace da

@@ -2,8 +2,9 @@
 
 `plan`/`dilated_attn`, `plan_bwd`/`dilated_attn_bwd` and `xpos` mirror the
 C ABI (dilated_attn_plan / dilated_attn_fwd, dilated_attn_bwd_plan /
-dilated_attn_bwd, dilated_attn_xpos): torch supplies device memory and the
-stream, every step of the computation runs in the HIP kernels of
+dilated_attn_bwd, dilated_attn_xpos), and so do `qk_norm_xpos` and its
+gradients, `cache_append` and `paged_attn`: torch supplies device memory and
+the stream, every step of the computation runs in the HIP kernels of
 libdilated_attn.so.
 """
 from __future__ import annotations
@@ -390,3 +391,230 @@ def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, [ws, dx, dw, db])
     return dx, dw, db
+
+
+def _token_stride(name: str, t: torch.Tensor, lead: int, dtype, device) -> int:
+    """Elements between the tokens of a [..., heads, D] tensor with `lead`
+    leading dimensions whose heads are contiguous and whose tokens are evenly
+    spaced (a contiguous tensor, or a slice of a joint projection's output)."""
+    if t.dim() != lead + 2 or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a {lead + 2}-dimensional {dtype} tensor on {device}")
+    H, D = t.shape[-2:]
+    if (D > 1 and t.stride(-1) != 1) or (H > 1 and t.stride(-2) != D):
+        raise ValueError(f"{name} must have the heads of a token contiguous")
+    sizes, strides = t.shape[:lead], t.stride()[:lead]
+    step, span = None, 1
+    for n, s in zip(reversed(sizes), reversed(strides)):
+        if n > 1:
+            if step is None:
+                step = s
+                if span != 1:
+                    raise ValueError(f"{name} must have its tokens evenly spaced")
+            elif s != step * span:
+                raise ValueError(f"{name} must have its tokens evenly spaced")
+        span *= n
+    return H * D if step is None else step
+
+
+def _qk_shapes(q: torch.Tensor, k: torch.Tensor, q_weight, k_weight):
+    if q.device.type != "cuda":
+        raise RuntimeError("the head norms run on the GPU only; q must be a device tensor")
+    if q.dim() != 4 or k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
+        raise ValueError("q and k must be [B, N, H, D] and [B, N, Hkv, D]")
+    B, N, H, D = q.shape
+    _check_like("q_weight", q_weight, (D,), q.dtype, q.device)
+    _check_like("k_weight", k_weight, (D,), q.dtype, q.device)
+    qs, ks = _token_stride("q", q, 2, q.dtype, q.device), _token_stride("k", k, 2, q.dtype, q.device)
+    return B, N, H, k.shape[2], D, qs, ks
+
+
+def qk_norm_xpos(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor,
+                 eps: float = 1e-6, center: int | None = None, base: float = 10000.0, gamma: float = 0.4,
+                 scale_base: float = 512.0, stream: torch.cuda.Stream | None = None):
+    """RMS norm of every head of q [B, N, H, D] and k [B, N, Hkv, D] with the
+    weights [D], then xPos (sign +1 for q, -1 for k; center defaults to
+    N // 2), in one pass.  The heads of a token are contiguous and the tokens
+    evenly spaced.  Returns new contiguous (q_out, k_out).  Enqueued on `stream`."""
+    lib = _lib.load()
+    B, N, H, Hkv, D, qs, ks = _qk_shapes(q, k, q_weight, k_weight)
+    qo = torch.empty((B, N, H, D), dtype=q.dtype, device=q.device)
+    ko = torch.empty((B, N, Hkv, D), dtype=q.dtype, device=q.device)
+    raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
+    rc = lib.dilated_attn_qk_norm_xpos(q.data_ptr(), k.data_ptr(), q_weight.data_ptr(), k_weight.data_ptr(),
+                                       qo.data_ptr(), ko.data_ptr(), B, N, H, Hkv, D, qs, ks, float(eps),
+                                       N // 2 if center is None else int(center), float(base), float(gamma),
+                                       float(scale_base), _dtype_code(q.dtype), raw)
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    _stream_use(stream, [qo, ko])
+    return qo, ko
+
+
+def qk_norm_xpos_bwd(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                     q_weight: torch.Tensor, k_weight: torch.Tensor, eps: float = 1e-6, center: int | None = None,
+                     base: float = 10000.0, gamma: float = 0.4, scale_base: float = 512.0,
+                     stream: torch.cuda.Stream | None = None):
+    """Gradients (dq, dk, dq_weight, dk_weight) of qk_norm_xpos given its inputs
+    and the contiguous gradients of its outputs; the float32 workspace comes
+    from torch's caching allocator."""
+    lib = _lib.load()
+    B, N, H, Hkv, D, qs, ks = _qk_shapes(q, k, q_weight, k_weight)
+    _check_like("dq_out", dq_out, (B, N, H, D), q.dtype, q.device)
+    _check_like("dk_out", dk_out, (B, N, Hkv, D), q.dtype, q.device)
+    need = _workspace_bytes("dilated_attn_qk_norm_xpos_bwd_workspace", B, N, D)
+    dq, dk = torch.empty_like(dq_out), torch.empty_like(dk_out)
+    dqw, dkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
+    rc = lib.dilated_attn_qk_norm_xpos_bwd(
+        dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), q_weight.data_ptr(), k_weight.data_ptr(),
+        dq.data_ptr(), dk.data_ptr(), dqw.data_ptr(), dkw.data_ptr(), B, N, H, Hkv, D, qs, ks, float(eps),
+        N // 2 if center is None else int(center), float(base), float(gamma), float(scale_base),
+        _dtype_code(q.dtype), ws.data_ptr(), need, raw)
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    _stream_use(stream, [dq, dk, dqw, dkw, ws])
+    return dq, dk, dqw, dkw
+
+
+def _paged_cache(q_dtype, device, D: int, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                 seq_lens: torch.Tensor, q_start: torch.Tensor):
+    """The da_paged_cache_t of a call, its sequence count and key heads."""
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache and v_cache must be [num_pages, Hkv, page_size, D]")
+    pages, Hkv, page, Dc = k_cache.shape
+    if Dc != D:
+        raise ValueError(f"k_cache holds heads of {Dc}, the call has heads of {D}")
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _check_like(name, t, k_cache.shape, q_dtype, device)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
+    B, max_pages = block_table.shape
+    _check_like("block_table", block_table, (B, max_pages), torch.int32, device)
+    _check_like("seq_lens", seq_lens, (B,), torch.int32, device)
+    _check_like("q_start", q_start, (B + 1,), torch.int32, device)
+    args = _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                               q_start.data_ptr(), pages, page, max_pages)
+    return args, B, Hkv
+
+
+def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
+                 v_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, q_start: torch.Tensor,
+                 q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+                 rotate: bool = True, center: int = 0, base: float = 10000.0, gamma: float = 0.4,
+                 scale_base: float = 512.0, stream: torch.cuda.Stream | None = None):
+    """New keys and values into a paged cache, the keys normed (with k_weight)
+    and rotated by xPos on the way; returns the queries normed (with q_weight)
+    and rotated, [T, H, D], or None without q.
+
+    q [T, H, D], k and v [T, Hkv, D]: the new tokens of all sequences side by
+    side, those of sequence b in rows q_start[b]:q_start[b + 1] (int32 [B + 1]).
+    They are the last of its seq_lens[b] tokens (int32 [B]).  Token p lies in
+    page block_table[b, p // page_size] (int32 [B, max_pages]) of k_cache and
+    v_cache [num_pages, Hkv, page_size, D], page_size a power of two.  `center`
+    is the xPos centre, the same for the life of a cache.  Enqueued on `stream`."""
+    lib = _lib.load()
+    if k.device.type != "cuda":
+        raise RuntimeError("cache_append runs on the GPU only; k must be a device tensor")
+    if k.dim() != 3 or v.shape != k.shape:
+        raise ValueError("k and v must be [T, Hkv, D]")
+    T, Hkv, D = k.shape
+    ks, vs = _token_stride("k", k, 1, k.dtype, k.device), _token_stride("v", v, 1, k.dtype, k.device)
+    cache, B, cached_heads = _paged_cache(k.dtype, k.device, D, k_cache, v_cache, block_table, seq_lens, q_start)
+    if cached_heads != Hkv:
+        raise ValueError(f"the cache has {cached_heads} key heads, k has {Hkv}")
+    H, qs, qo = Hkv, Hkv * D, None
+    if q is not None:
+        qs = _token_stride("q", q, 1, k.dtype, k.device)
+        H = q.shape[1]
+        if q.shape != (T, H, D):
+            raise ValueError("q must be [T, H, D] for the tokens of k")
+        qo = torch.empty((T, H, D), dtype=k.dtype, device=k.device)
+    elif q_weight is not None:
+        raise ValueError("q_weight without q")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _check_like(name, w, (D,), k.dtype, k.device)
+    raw = _raw_stream(k.device) if stream is None else stream.cuda_stream
+    rc = lib.dilated_attn_cache_append(
+        None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        None if qo is None else qo.data_ptr(), ctypes.byref(cache), T, B, H, Hkv, D, qs, ks, vs, float(eps),
+        int(bool(rotate)), int(center), float(base), float(gamma), float(scale_base), _dtype_code(k.dtype), raw)
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    if qo is not None:
+        _stream_use(stream, [qo])
+    return qo
+
+
+@functools.lru_cache(maxsize=256)
+def _paged_workspace(shape: tuple, pats: tuple, dtype_code: int) -> int:
+    lib = _lib.load()
+    arr, n = _pattern_array_cached(pats)
+    need = ctypes.c_uint64(0)
+    rc = lib.dilated_attn_paged_workspace(*shape, arr, n, dtype_code, ctypes.byref(need))
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    return need.value
+
+
+def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+               seq_lens: torch.Tensor, q_start: torch.Tensor, patterns: Sequence[Tuple[int, int]],
+               max_new: int | None = None, scale: float | None = None, out: torch.Tensor | None = None,
+               lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+               stream: torch.cuda.Stream | None = None):
+    """Causal dilated attention of new tokens q [T, H, D] over a paged cache that
+    holds their keys and values already (see cache_append for the cache and
+    the sequences' arrays): a token at position p gets what row p of
+    dilated_attn gives on its sequence.  H is a multiple of the cache's heads.
+
+    max_new, the most new tokens of any sequence if the caller knows it,
+    spares the launches for long ones where it is at most 8.  Returns (out
+    [T, H, D], lse [H, T] float32); a token of no sequence has zeros and -inf.
+    Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor of
+    at least paged_workspace_bytes."""
+    lib = _lib.load()
+    if q.device.type != "cuda":
+        raise RuntimeError("paged_attn runs on the GPU only; q must be a device tensor")
+    qs = _token_stride("q", q, 1, q.dtype, q.device)
+    T, H, D = q.shape
+    cache, B, Hkv = _paged_cache(q.dtype, q.device, D, k_cache, v_cache, block_table, seq_lens, q_start)
+    dcode = _dtype_code(q.dtype)
+    pats = _pattern_key(patterns)
+    new = T if max_new is None else int(max_new)
+    need = _paged_workspace((T, B, H, Hkv, D, cache.num_pages, cache.page_size, cache.max_pages, new), pats, dcode)
+    owned = []
+    if out is None:
+        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        owned.append(out)
+    else:
+        _check_like("out", out, (T, H, D), q.dtype, q.device)
+    if lse is None:
+        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        owned.append(lse)
+    else:
+        _check_like("lse", lse, (H, T), torch.float32, q.device)
+    if workspace is None:
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        owned.append(workspace)
+    elif workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
+    arr, n = _pattern_array_cached(pats)
+    raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
+    rc = lib.dilated_attn_paged_fwd(q.data_ptr(), ctypes.byref(cache), out.data_ptr(), lse.data_ptr(), T, B, H, Hkv,
+                                    D, qs, new, arr, n, dcode, float(scale or 0.0), workspace.data_ptr(),
+                                    workspace.numel(), raw)
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    _stream_use(stream, owned)
+    return out, lse
+
+
+def paged_workspace_bytes(T: int, B: int, H: int, Hkv: int, D: int, num_pages: int, page_size: int, max_pages: int,
+                          patterns: Sequence[Tuple[int, int]], max_new: int | None = None,
+                          dtype=torch.bfloat16) -> int:
+    """Validate a paged_attn problem and return the workspace it needs (host only)."""
+    shape = (int(T), int(B), int(H), int(Hkv), int(D), int(num_pages), int(page_size), int(max_pages),
+             int(T if max_new is None else max_new))
+    return _paged_workspace(shape, _pattern_key(patterns), _dtype_code(dtype))
