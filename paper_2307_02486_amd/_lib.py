@@ -1,4 +1,5 @@
-"""ctypes view of libdilated_attn.so (the C ABI of include/dilated_attn.h).
+"""ctypes view of libdilated_attn.so (the C ABI of include/dilated_attn.h
+and include/dilated_attn_paged.h).
 
 Argument marshalling only.  torch is imported first so that the library binds
 to the HIP runtime torch already loaded (one runtime per process).

@@ -7,6 +7,7 @@
 #include <cstdint>
 #include <vector>
 
+#include "../../include/dilated_attn_paged.h"
 #include "kernels.h"
 #include "plan.h"
 

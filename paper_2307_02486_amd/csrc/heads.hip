@@ -249,9 +249,9 @@ struct HeadBwdArgs {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kHeadThreads) void heads_bwd(HeadBwdArgs a) {
+__global__ __launch_bounds__(kHeadThreads, 4) void heads_bwd(HeadBwdArgs a) {
   typedef typename Raw8<T>::type Raw;
-  constexpr int kLanes = D / 8, kRows = 64 / kLanes, kUnroll = 3;
+  constexpr int kLanes = D / 8, kRows = 64 / kLanes;
   __shared__ float red[kHeadWaves][2 * D];
   const int tid = __builtin_amdgcn_workitem_id_x();
   const int lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -263,71 +263,69 @@ __global__ __launch_bounds__(kHeadThreads) void heads_bwd(HeadBwdArgs a) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 0.0f;
 
-  const int64_t step = static_cast<int64_t>(__builtin_amdgcn_grid_size_x() / kHeadThreads) * kHeadWaves;
-  for (int64_t tok = static_cast<int64_t>(__builtin_amdgcn_workgroup_id_x()) * kHeadWaves + wv; tok < a.T;
-       tok += step) {
+  // A step is kRows heads of a token; the next step's rows, of this token or
+  // the wave's next one, are loaded while a step is computed.
+  const int64_t stride = static_cast<int64_t>(__builtin_amdgcn_grid_size_x() / kHeadThreads) * kHeadWaves;
+  int64_t tok = static_cast<int64_t>(__builtin_amdgcn_workgroup_id_x()) * kHeadWaves + wv;
+  Raw nx{}, ndy{};
+  auto load = [&](int64_t t, int r0) {
+    const int row = r0 + sub;
+    nx = ndy = Raw{};  // lanes past the last row hold zeros
+    if (t < a.T && row < rows) {
+      const bool is_q = row < nq;
+      const T* x = is_q ? static_cast<const T*>(a.q) + (t * a.qs + row * D)
+                        : static_cast<const T*>(a.k) + (t * a.ks + (row - nq) * D);
+      const T* dy = is_q ? static_cast<const T*>(a.dqo) + (t * a.H + row) * D
+                         : static_cast<const T*>(a.dko) + (t * a.Hkv + row - nq) * D;
+      nx = *reinterpret_cast<const Raw*>(x + ch * 8);
+      ndy = *reinterpret_cast<const Raw*>(dy + ch * 8);
+    }
+  };
+  load(tok, 0);
+  for (; tok < a.T; tok += stride) {
     const int pos = static_cast<int>(tok) - static_cast<int>(a.fn.div(static_cast<uint32_t>(tok)) * a.fn.d);
-    const T* q = static_cast<const T*>(a.q) + tok * a.qs + ch * 8;
-    const T* k = static_cast<const T*>(a.k) + tok * a.ks + ch * 8;
-    const T* dqo = static_cast<const T*>(a.dqo) + tok * a.H * D + ch * 8;
-    const T* dko = static_cast<const T*>(a.dko) + tok * a.Hkv * D + ch * 8;
-    Raw x[kUnroll], dy[kUnroll];
-    auto load = [&](int r0) {
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int row = r0 + u * kRows + sub;
-        x[u] = dy[u] = Raw{};
-        if (row < rows) {
-          x[u] = *reinterpret_cast<const Raw*>(row < nq ? q + row * D : k + (row - nq) * D);
-          dy[u] = *reinterpret_cast<const Raw*>(row < nq ? dqo + row * D : dko + (row - nq) * D);
-        }
-      }
-    };
-    load(0);
     const Rotation rt = rotation(a.tab, ch * 4, pos, pos - a.center);
-    for (int r0 = 0; r0 < rows; r0 += kUnroll * kRows) {
-      if (r0 > 0) load(r0);
+    for (int r0 = 0; r0 < rows; r0 += kRows) {
+      const Raw x = nx, dy = ndy;
+      const bool last = r0 + kRows >= rows;
+      load(last ? tok + stride : tok, last ? 0 : r0 + kRows);
+      const int row = r0 + sub;
+      const bool is_q = row < nq;
+      float f[8], g[8], h[8];  // x, dy, then dn and dn w
+      unpack(x, f);
+      unpack(dy, g);
+      float ss = 0.0f, dot = 0.0f;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (r0 + u * kRows >= rows) break;
-        const int row = r0 + u * kRows + sub;  // lanes past the last row hold zeros
-        const bool is_q = row < nq;
-        float f[8], g[8], h[8];  // x, dy, then dn and dn w
-        unpack(x[u], f);
-        unpack(dy[u], g);
-        float ss = 0.0f, dot = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float s = is_q ? rt.up[e] : rt.down[e];
-          const float g0 = g[2 * e], g1 = g[2 * e + 1];
-          g[2 * e] = s * (g0 * rt.cs[e] + g1 * rt.sn[e]);
-          g[2 * e + 1] = s * (g1 * rt.cs[e] - g0 * rt.sn[e]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          h[e] = g[e] * (is_q ? wq[e] : wk[e]);
-          ss += f[e] * f[e];
-          dot += h[e] * f[e];
-        }
-        ss = row_sum<kLanes>(ss);
-        dot = row_sum<kLanes>(dot);
-        const float rstd = __builtin_amdgcn_rsqf(ss * (1.0f / D) + a.eps);
-        const float m = dot * rstd * (1.0f / D) * rstd;  // mean(dn w xhat) rstd
-        float dx[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          dx[e] = rstd * (h[e] - f[e] * m);
-          const float t = g[e] * f[e] * rstd;
-          gq[e] += is_q ? t : 0.0f;
-          gk[e] += is_q ? 0.0f : t;
-        }
-        Raw o;
-        pack(dx, o);
-        if (row >= rows) continue;
-        T* dst = is_q ? static_cast<T*>(a.dq) + (tok * a.H + row) * D
-                      : static_cast<T*>(a.dk) + (tok * a.Hkv + row - nq) * D;
-        *reinterpret_cast<Raw*>(dst + ch * 8) = o;
+      for (int e = 0; e < 4; ++e) {
+        const float s = is_q ? rt.up[e] : rt.down[e];
+        const float g0 = g[2 * e], g1 = g[2 * e + 1];
+        g[2 * e] = s * (g0 * rt.cs[e] + g1 * rt.sn[e]);
+        g[2 * e + 1] = s * (g1 * rt.cs[e] - g0 * rt.sn[e]);
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        h[e] = g[e] * (is_q ? wq[e] : wk[e]);
+        ss += f[e] * f[e];
+        dot += h[e] * f[e];
+      }
+      ss = row_sum<kLanes>(ss);
+      dot = row_sum<kLanes>(dot);
+      const float rstd = __builtin_amdgcn_rsqf(ss * (1.0f / D) + a.eps);
+      const float m = dot * rstd * (1.0f / D) * rstd;  // mean(dn w xhat) rstd
+      float dx[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dx[e] = rstd * (h[e] - f[e] * m);
+        const float t = g[e] * f[e] * rstd;
+        gq[e] += is_q ? t : 0.0f;
+        gk[e] += is_q ? 0.0f : t;
+      }
+      Raw o;
+      pack(dx, o);
+      if (row >= rows) continue;
+      T* dst = is_q ? static_cast<T*>(a.dq) + (tok * a.H + row) * D
+                    : static_cast<T*>(a.dk) + (tok * a.Hkv + row - nq) * D;
+      *reinterpret_cast<Raw*>(dst + ch * 8) = o;
     }
   }
   // Lanes of one ch hold the same eight columns: over the wave's row groups by

@@ -11,13 +11,13 @@
 // device from the lengths, so that a launch needs no plan of the lengths on the
 // host and can be captured in a graph.
 //
-// paged_one: a workgroup is one (token, key head, pattern, split of its keys),
+// single_tokens: a workgroup is one (token, key head, pattern, split of its keys),
 // for sequences with few new tokens.  Bound by HBM and, for few sequences, by
 // latency: the keys are split over workgroups, and in one over its four waves,
 // which take 32-key tiles in turn without a barrier.  K goes from the cache to
 // registers in the operand layout of v_mfma_f32_16x16x32_bf16 (16 keys by up to
 // 16 query heads), V to the wave's own LDS buffer, read transposed.
-// paged_tile: a workgroup is 128 kept query rows of one (sequence, head,
+// query_tiles: a workgroup is 128 kept query rows of one (sequence, head,
 // segment) of a pattern against 64-key tiles in LDS.  Bound by the matrix cores
 // and the softmax's vector work.
 // Both write normalised partial rows with their log-sum-exps; paged_join mixes
@@ -46,45 +46,79 @@ struct PagedArgs {
   int64_t qs;  // elements between tokens of q
   int64_t one_rec, one_row, tile_rec, tile_row;  // byte offsets in the workspace
   int32_t T, B, H, Hkv, G, npat, num_pages, max_pages, page_log2;
-  int32_t all_few, by_token, units, one_slots, tile_slots;
+  int32_t by_token, few, units, one_slots, tile_items;
   uint32_t reach;  // positions the table holds
   FastDiv fslots, funits;  // division by one_slots and by a token's units
   float scale_log2;
   PagedPattern pat[DA_MAX_PATTERNS];
 };
 
-// The sequence of token tok (see heads.hip): -1 if it has none.
-__device__ inline int sequence_at(const int32_t* start, int B, int tok, int lane) {
-  int n = 0;
-  for (int b0 = 0; b0 <= B; b0 += 64) {
+// A sequence's new tokens: rows begin .. end - 1 of the call, the last of its
+// length len.
+struct Sequence {
+  int b;  // -1: the token has none
+  int begin, end, len;
+};
+// The sequences of kTokens tokens (the same in all lanes), by all lanes of a
+// wave: start [B + 1] ascends and the last entry that is not above a token is
+// its sequence's (empty ones before it share that value).  Whatever start
+// holds, the result is below B.  Up to 63 sequences all entries arrive in one
+// round of loads.
+template <int kTokens>
+__device__ inline void find_sequences(const PagedArgs& a, const int (&tok)[kTokens], int lane, Sequence (&sq)[kTokens]) {
+  int n[kTokens];
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) n[i] = 0;
+  int start = 0, len = 0;
+  for (int b0 = 0; b0 <= a.B; b0 += 64) {
     const int b = b0 + lane;
-    n += __popcll(__ballot(b <= B && start[min(b, B)] <= tok));
+    start = a.start[min(b, a.B)];
+    len = a.lens[min(b, a.B - 1)];
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) n[i] += __popcll(__ballot(b <= a.B && start <= tok[i]));
   }
-  return n > B ? -1 : n - 1;
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) {
+    const int b = n[i] > a.B ? -1 : n[i] - 1;
+    sq[i] = Sequence{b, 0, 0, 0};
+    if (b < 0) continue;
+    if (a.B < 64) {
+      sq[i].begin = __builtin_amdgcn_readlane(start, b);
+      sq[i].end = __builtin_amdgcn_readlane(start, b + 1);
+      sq[i].len = __builtin_amdgcn_readlane(len, b);
+    } else {
+      sq[i].begin = a.start[b];
+      sq[i].end = a.start[b + 1];
+      sq[i].len = a.lens[b];
+    }
+  }
+}
+
+// Position of row tok of its sequence; -1 where it has none in the table.
+__device__ inline int position_of(const PagedArgs& a, const Sequence& sq, int tok) {
+  const int64_t p = static_cast<int64_t>(sq.len) - sq.end + tok;
+  return sq.b >= 0 && tok < sq.end && p >= 0 && p < a.reach ? static_cast<int>(p) : -1;
 }
 
 // A listed token: its row of q, its sequence and position.  False: not there,
 // not in the cache, or computed in tiles.
 struct Token {
-  int tok, b;
-  int pos;
+  int tok, b, pos;
 };
 __device__ inline bool single_token(const PagedArgs& a, int e, int lane, Token& t) {
+  Sequence sq[1];
   if (a.by_token) {
+    const int tok[1] = {e};
     t.tok = e;
-    t.b = __builtin_amdgcn_readfirstlane(sequence_at(a.start, a.B, e, lane));
-    if (t.b < 0) return false;
+    find_sequences(a, tok, lane, sq);
   } else {
-    t.b = e / static_cast<int>(kPagedFew);
-    t.tok = a.start[t.b] + e % static_cast<int>(kPagedFew);
+    const int b = e / a.few;
+    sq[0] = Sequence{b, a.start[b], a.start[b + 1], a.lens[b]};
+    t.tok = sq[0].begin + (e - b * a.few);
   }
-  const int64_t end = a.start[t.b + 1], n = end - a.start[t.b];
-  if (t.tok < 0 || t.tok >= a.T || t.tok >= end) return false;
-  if (!a.all_few && n > kPagedFew) return false;
-  const int64_t p = a.lens[t.b] - end + t.tok;
-  if (p < 0 || p >= a.reach) return false;
-  t.pos = static_cast<int>(p);
-  return true;
+  t.b = sq[0].b;
+  t.pos = position_of(a, sq[0], t.tok);
+  return t.pos >= 0 && t.tok >= 0 && t.tok < a.T && static_cast<int64_t>(sq[0].end) - sq[0].begin <= a.few;
 }
 
 // The heads of key head hk's group that pattern P keeps at segment-local
@@ -131,9 +165,7 @@ __device__ inline void wait_loads() {
 struct OneItem {
   int e, slot, hk, block;
 };
-template <typename A>
-__device__ inline bool one_item(const A& a, OneItem& it, int per_token_heads) {
-  const int idx = launch_index();
+__device__ inline bool one_item(const PagedArgs& a, int idx, OneItem& it, int heads) {
   const int k = idx >> 3;
   const int j = a.fslots.div(k);
   const int unit = j * 8 + (idx & 7);
@@ -141,8 +173,8 @@ __device__ inline bool one_item(const A& a, OneItem& it, int per_token_heads) {
   it.slot = k - j * a.one_slots;
   it.e = a.funits.div(unit);
   const int rest = unit - it.e * a.funits.d;
-  it.block = rest / per_token_heads;
-  it.hk = rest - it.block * per_token_heads;
+  it.block = rest / heads;
+  it.hk = rest - it.block * heads;
   return true;
 }
 
@@ -152,21 +184,28 @@ struct KeyFrag {
   u32x4 v[2][KC];
 };
 
+constexpr int kOneTile = 32;  // keys of a wave's tile
 template <int D>
-__global__ __launch_bounds__(kPgThreads) void paged_one(PagedArgs a) {
-  constexpr int KC = D / 32, DB = D / 16, kTile = 32;
+struct SmemOne {
+  __attribute__((aligned(16))) char v[kPgWaves][2 * kOneTile * D * 2];  // each wave's two V tiles
+  float ml[kPgWaves][2][16];
+};
+
+template <int D>
+__device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm) {
+  constexpr int KC = D / 32, DB = D / 16, kTile = kOneTile;
   using TL = TileLayout<D>;
   constexpr int kVLoads = kTile * TL::kSlots / 64;
   constexpr int kBuf = kTile * D * 2;  // bytes of a V tile
   constexpr int kJoin = D + 4;         // floats between joined rows
   static_assert(16 * kJoin * 4 <= 2 * kBuf, "the join fits a wave's V buffers");
-  __shared__ __attribute__((aligned(16))) char sv[kPgWaves][2 * kBuf];
-  __shared__ float sml[kPgWaves][2][16];
+  auto& sv = sm.v;
+  auto& sml = sm.ml;
 
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   OneItem it;
-  if (!one_item(a, it, a.Hkv)) return;
+  if (!one_item(a, idx, it, a.Hkv)) return;
   int pi = 0;
   for (int i = 1; i < a.npat; ++i)
     if (it.slot >= a.pat[i].one_slot) pi = i;
@@ -367,7 +406,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
   __shared__ float sml[2][kGroups];
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   OneItem it;
-  if (!one_item(a, it, a.H)) return;
+  if (!one_item(a, launch_index(), it, a.H)) return;
   int pi = 0;
   for (int i = 1; i < a.npat; ++i)
     if (it.slot >= a.pat[i].one_slot) pi = i;
@@ -463,7 +502,7 @@ __device__ inline bool query_tile(const PagedArgs& a, const PagedPattern& P, int
       const int64_t len = a.lens[b];
       c1 = static_cast<int>(max(int64_t{0}, min(len, static_cast<int64_t>(a.reach))));
       c0 = static_cast<int>(max(int64_t{0}, min(len - n, static_cast<int64_t>(c1))));
-      if (n > kPagedFew && c1 > c0) {
+      if (n > a.few && c1 > c0) {
         const int g0 = P.fw.div(c0), g1 = P.fw.div(c1 - 1);
         cnt = g0 == g1 ? tiles_of(c1 - c0)
                        : tiles_of((g0 + 1) * P.w - c0) + (g1 - g0 - 1) * tiles_of(P.w) + tiles_of(c1 - g1 * P.w);
@@ -507,15 +546,13 @@ struct SmemTile {
 };
 
 template <int D>
-__global__ __launch_bounds__(kPgThreads) void paged_tile(PagedArgs a) {
+__device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm) {
   constexpr int BM = kPagedRows, BN = kPagedKeyTile;
   constexpr int KC = D / 16, DB = D / 32;
   using TL = TileLayout<D>;
   constexpr int kLoads = BN * TL::kSlots / 64 / kPgWaves;
-  __shared__ SmemTile<D> sm;
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int idx = launch_index();
   int pi = 0;
   for (int i = 1; i < a.npat; ++i)
     if (idx >= a.pat[i].item_begin) pi = i;
@@ -745,8 +782,28 @@ __global__ __launch_bounds__(kPgThreads) void paged_tile(PagedArgs a) {
   }
 }
 
+// One launch for both: the tiles first, as they take longer.
+template <int D, bool kTiles>
+__global__ __launch_bounds__(kPgThreads) void paged_attn(PagedArgs a) {
+  const int idx = launch_index();
+  if constexpr (kTiles) {
+    union Smem {
+      SmemTile<D> tile;
+      SmemOne<D> one;
+    };
+    __shared__ Smem sm;
+    if (idx < a.tile_items) query_tiles<D>(a, idx, sm.tile);
+    else single_tokens<D>(a, idx - a.tile_items, sm.one);
+  } else {
+    __shared__ SmemOne<D> sm;
+    single_tokens<D>(a, idx, sm);
+  }
+}
+
 // ---------------------------------------------------------------------------
-// Joins
+// The join: a row's partials, of every pattern that keeps it and every split,
+// mixed by their denominators.  D/8 lanes read a partial row; kSubs partials
+// of a row at a time, so that their loads are under way together.
 // ---------------------------------------------------------------------------
 __device__ inline void put8(u16* p, const f32x8& v) {
   bf16x8 b;
@@ -756,46 +813,77 @@ __device__ inline void put8(u16* p, const f32x8& v) {
 }
 __device__ inline void put8(float* p, const f32x8& v) { *reinterpret_cast<f32x8*>(p) = v; }
 
-// Single tokens: a wave per (token, head), D/8 lanes across a partial row and
-// 64 / (D/8) of the row's splits at a time.
-template <typename T, int D>
-__global__ __launch_bounds__(kPgThreads) void paged_join_one(PagedArgs a) {
-  constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes;
+template <typename T, int D, bool kTiles>
+__global__ __launch_bounds__(kPgThreads) void paged_join(PagedArgs a) {
+  constexpr int kLanes = D / 8;
+  constexpr int kSubs = kTiles ? 4 : 64 / kLanes;
+  constexpr int kRows = 64 / kLanes / kSubs;  // rows of a wave
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
-  const int64_t row = static_cast<int64_t>(launch_index()) * kPgWaves + __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int e = static_cast<int>(row / a.H), head = static_cast<int>(row - static_cast<int64_t>(e) * a.H);
-  const int listed = a.units / static_cast<int>(a.funits.d);
-  if (e >= listed) return;
-  const int ch = lane % kLanes, sub = lane / kLanes;
-  Token tk;
-  const bool there = single_token(a, e, lane, tk);
-  if (!there && !a.all_few) return;
+  const int ch = lane % kLanes, sub = lane / kLanes % kSubs, mine = lane / (kLanes * kSubs);
+  const int row0 = (launch_index() * kPgWaves + __builtin_amdgcn_readfirstlane(tid >> 6)) * kRows;
+  const int total = a.T * a.H;
+  if (row0 >= total) return;
+  int toks[kRows];
+  Sequence sq[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) toks[i] = min(row0 + i, total - 1) / a.H;
+  find_sequences(a, toks, lane, sq);
+  int tok = toks[0], pos = position_of(a, sq[0], toks[0]), begin = sq[0].begin, n = sq[0].end - begin, b = sq[0].b;
+#pragma unroll
+  for (int i = 1; i < kRows; ++i)
+    if (mine == i) {
+      tok = toks[i];
+      pos = position_of(a, sq[i], tok);
+      begin = sq[i].begin;
+      n = sq[i].end - begin;
+      b = sq[i].b;
+    }
+  const int row = row0 + mine;
+  const int head = row - tok * a.H;
+  const bool single = !kTiles || n <= a.few;
+  const int64_t e = a.by_token ? tok : static_cast<int64_t>(b) * a.few + (tok - begin);
+  const float* one_rec = reinterpret_cast<const float*>(a.ws + a.one_rec) + (e * a.H + head) * a.one_slots;
+  const float* one_row = reinterpret_cast<const float*>(a.ws + a.one_row) + (e * a.H + head) * a.one_slots * D;
+
   float m = -INFINITY, l = 0.0f;
   f32x8 acc = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-  if (there) {
-    const float* rec = reinterpret_cast<const float*>(a.ws + a.one_rec) + row * a.one_slots;
-    const float* part = reinterpret_cast<const float*>(a.ws + a.one_row) + row * a.one_slots * D + ch * 8;
-    for (int i = 0; i < a.npat; ++i) {
-      const PagedPattern& P = a.pat[i];
-      const int g = P.fw.div(tk.pos), loc = tk.pos - g * P.w;
-      const int t = P.fr.div(loc), rho = loc - t * P.r;
-      if (head - static_cast<int>(P.fr.div(head)) * P.r != rho) continue;
-      const int per = split_keys_of(P, t + 1);
-      const int used = t / per + 1;
-      for (int s = sub; s < used; s += kAtOnce) {
-        const float x = rec[P.one_slot + s];
-        const f32x8 o = *reinterpret_cast<const f32x8*>(part + static_cast<int64_t>(P.one_slot + s) * D);
-        if (x == -INFINITY) continue;
-        const float mn = fmaxf(m, x);
-        const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(x - mn);
-        m = mn;
-        l = l * f0 + f1;
-        acc = acc * f0 + o * f1;
+  if (pos >= 0 && row < total) {
+    for (int want = sub;; want += kSubs) {  // the want-th partial of the row
+      int slot = -1, before = 0;
+      for (int i = 0; i < a.npat; ++i) {
+        const PagedPattern& P = a.pat[i];
+        const int g = P.fw.div(pos), loc = pos - g * P.w;
+        const int t = P.fr.div(loc), rho = loc - t * P.r;
+        if (head - static_cast<int>(P.fr.div(head)) * P.r != rho) continue;
+        const int used = single ? t / split_keys_of(P, t + 1) + 1 : P.tile_splits;
+        if (want >= before && want < before + used) slot = (single ? P.one_slot : P.tile_slot) + want - before;
+        before += used;
       }
+      if (slot < 0) break;
+      float x, scale = 1.0f;
+      f32x8 o;
+      if (single) {
+        x = one_rec[slot];
+        o = *reinterpret_cast<const f32x8*>(one_row + static_cast<int64_t>(slot) * D + ch * 8);
+      } else {
+        const int64_t at = static_cast<int64_t>(slot) * total + row;
+        const f32x2 r = reinterpret_cast<const f32x2*>(a.ws + a.tile_rec)[at];
+        const f16x8 h = *reinterpret_cast<const f16x8*>(a.ws + a.tile_row + (at * D + ch * 8) * 2);
+        x = r[0];
+        scale = r[1];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) o[c] = static_cast<float>(h[c]);
+      }
+      if (x == -INFINITY) continue;  // a split without a visible key: its row is not read
+      const float mn = fmaxf(m, x);
+      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(x - mn);
+      m = mn;
+      l = l * f0 + f1;
+      acc = acc * f0 + o * (f1 * scale);
     }
   }
 #pragma unroll
-  for (int x = kLanes; x < 64; x <<= 1) {
+  for (int x = kLanes; x < kLanes * kSubs; x <<= 1) {
     const float mo = __shfl_xor(m, x, 64), lo = __shfl_xor(l, x, 64);
     const float mn = fmaxf(m, mo);
     const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
@@ -805,71 +893,23 @@ __global__ __launch_bounds__(kPgThreads) void paged_join_one(PagedArgs a) {
 #pragma unroll
     for (int c = 0; c < 8; ++c) acc[c] = acc[c] * f0 + __shfl_xor(acc[c], x, 64) * f1;
   }
-  if (sub != 0) return;
-  const int64_t tok = a.by_token ? e : tk.tok;
+  if (sub != 0 || row >= total) return;
   acc *= l > 0.0f ? 1.0f / l : 0.0f;
-  put8(static_cast<T*>(a.out) + (tok * a.H + head) * D + ch * 8, acc);
+  put8(static_cast<T*>(a.out) + static_cast<int64_t>(row) * D + ch * 8, acc);
   if (ch == 0) a.lse[static_cast<int64_t>(head) * a.T + tok] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-}
-
-// Tokens of tiles (and of no sequence): a workgroup per token, D/8 lanes per head.
-template <int D>
-__global__ __launch_bounds__(kPgThreads) void paged_join_tile(PagedArgs a) {
-  constexpr int kLanes = D / 8;
-  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
-  const int tok = launch_index();
-  if (tok >= a.T) return;
-  const int b = sequence_at(a.start, a.B, tok, lane);
-  int64_t p = -1;
-  if (b >= 0) {
-    const int64_t end = a.start[b + 1], n = end - a.start[b];
-    if (tok < end) p = a.lens[b] - end + tok;
-    if (n <= kPagedFew && p >= 0 && p < a.reach) return;  // computed by itself
-  }
-  const int ch = tid % kLanes;
-  for (int head = tid / kLanes; head < a.H; head += kPgThreads / kLanes) {
-    float m = -INFINITY, l = 0.0f;
-    f32x8 acc = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-    if (p >= 0 && p < a.reach) {
-      const int pos = static_cast<int>(p);
-      for (int i = 0; i < a.npat; ++i) {
-        const PagedPattern& P = a.pat[i];
-        const int g = P.fw.div(pos), loc = pos - g * P.w;
-        const int t = P.fr.div(loc), rho = loc - t * P.r;
-        if (head - static_cast<int>(P.fr.div(head)) * P.r != rho) continue;
-        for (int s = 0; s < P.tile_splits; ++s) {
-          const int64_t at = (static_cast<int64_t>(P.tile_slot + s) * a.T + tok) * a.H + head;
-          const f32x2 r = reinterpret_cast<const f32x2*>(a.ws + a.tile_rec)[at];
-          if (r[0] == -INFINITY) continue;
-          const f16x8 o = *reinterpret_cast<const f16x8*>(a.ws + a.tile_row + (at * D + ch * 8) * 2);
-          const float mn = fmaxf(m, r[0]);
-          const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(r[0] - mn);
-          m = mn;
-          l = l * f0 + f1;
-          const float w = f1 * r[1];
-#pragma unroll
-          for (int c = 0; c < 8; ++c) acc[c] = acc[c] * f0 + static_cast<float>(o[c]) * w;
-        }
-      }
-    }
-    acc *= l > 0.0f ? 1.0f / l : 0.0f;
-    put8(static_cast<u16*>(a.out) + (static_cast<int64_t>(tok) * a.H + head) * D + ch * 8, acc);
-    if (ch == 0)
-      a.lse[static_cast<int64_t>(head) * a.T + tok] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-  }
 }
 
 template <int D>
 void launch_all(const PagedPlan& p, const PagedArgs& a, hipStream_t stream) {
-  const dim3 threads(kPgThreads);
-  const bool f32 = p.dtype == DA_F32;
-  if (!p.all_few) hipLaunchKernelGGL(paged_tile<D>, grid_of(p.tile_items), threads, 0, stream, a);
-  if (f32) hipLaunchKernelGGL(paged_one_f32<D>, grid_of(p.one_items), threads, 0, stream, a);
-  else hipLaunchKernelGGL(paged_one<D>, grid_of(p.one_items), threads, 0, stream, a);
-  const dim3 one = grid_of((p.singles * p.H + kPgWaves - 1) / kPgWaves);
-  if (f32) hipLaunchKernelGGL((paged_join_one<float, D>), one, threads, 0, stream, a);
-  else hipLaunchKernelGGL((paged_join_one<u16, D>), one, threads, 0, stream, a);
-  if (!p.all_few) hipLaunchKernelGGL(paged_join_tile<D>, grid_of(p.T), threads, 0, stream, a);
+  const dim3 threads(kPgThreads), grid = grid_of(p.tile_items + p.one_items);
+  if (p.dtype == DA_F32) hipLaunchKernelGGL(paged_one_f32<D>, grid, threads, 0, stream, a);
+  else if (p.all_few) hipLaunchKernelGGL((paged_attn<D, false>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((paged_attn<D, true>), grid, threads, 0, stream, a);
+  const int64_t rows = p.T * p.H, few = (rows + kPgWaves - 1) / kPgWaves;
+  constexpr int kPerGroup = kPgWaves * (64 / (D / 8) / 4);  // rows of a workgroup beside tiles
+  if (p.dtype == DA_F32) hipLaunchKernelGGL((paged_join<float, D, false>), grid_of(few), threads, 0, stream, a);
+  else if (p.all_few) hipLaunchKernelGGL((paged_join<u16, D, false>), grid_of(few), threads, 0, stream, a);
+  else hipLaunchKernelGGL((paged_join<u16, D, true>), grid_of((rows + kPerGroup - 1) / kPerGroup), threads, 0, stream, a);
 }
 
 }  // namespace
@@ -900,12 +940,12 @@ hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, con
   a.num_pages = static_cast<int32_t>(p.num_pages);
   a.max_pages = static_cast<int32_t>(p.max_pages);
   a.page_log2 = p.page_log2;
-  a.all_few = p.all_few;
   a.by_token = p.by_token;
+  a.few = static_cast<int32_t>(p.few);
+  a.tile_items = static_cast<int32_t>(p.tile_items);
   const int64_t per_token = p.dtype == DA_F32 ? p.H : p.Hkv * ((a.G + kPagedGroupRows - 1) / kPagedGroupRows);
   a.units = static_cast<int32_t>(p.singles * per_token);
   a.one_slots = static_cast<int32_t>(p.one_slots);
-  a.tile_slots = static_cast<int32_t>(p.tile_slots);
   a.reach = static_cast<uint32_t>(p.max_pages * p.page);
   a.fslots = make_fastdiv(static_cast<uint32_t>(p.one_slots));
   a.funits = make_fastdiv(static_cast<uint32_t>(per_token));

@@ -208,8 +208,9 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   p.scale = softmax_scale > 0.0f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(double(D)));
   const int64_t reach = max_pages * page;  // positions that the table holds
   p.all_few = dtype == DA_F32 || std::min(max_new, T) <= kPagedFew;
-  p.by_token = p.all_few || T <= B * kPagedFew;
-  p.singles = p.by_token ? T : B * kPagedFew;
+  p.few = p.all_few ? T : B == 1 ? 0 : kPagedFew;
+  p.by_token = p.all_few || T <= B * p.few;
+  p.singles = p.by_token ? T : B * p.few;
   const int64_t G = H / Hkv;
   const int64_t units = dtype == DA_F32 ? p.singles * H : p.singles * Hkv * ((G + kPagedGroupRows - 1) / kPagedGroupRows);
   // Workgroups with work if every listed token were there (a pattern's rows
@@ -248,9 +249,9 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     t.item_begin = static_cast<int32_t>(items);
     items += tiles * H * ts;
   }
-  p.tile_items = items;
+  p.tile_items = (items + 7) / 8 * 8;  // the single tokens' workgroups after them keep their XCDs
   p.one_items = (units + 7) / 8 * 8 * p.one_slots;
-  if (p.one_items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
+  if (p.one_items + p.tile_items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
   uint64_t off = 0;
   auto take = [&off](uint64_t bytes) {
     const uint64_t at = off;

@@ -112,8 +112,9 @@ int make_plan(int64_t B, int64_t N, int64_t H, int64_t D, const da_pattern_t* pa
 // Attention over a paged cache.  A sequence's new tokens are computed in one of
 // two ways: each token by itself (all its keys' splits in parallel), or in
 // tiles of kept query rows.  A sequence of at most kPagedFew new tokens takes
-// the first.  Both write one partial row per (token, head) and slot, a slot
-// being one split of one pattern's keys, and the join reads them.
+// the first, unless it is the call's only one.  Both write one partial row per
+// (token, head) and slot, a slot being one split of one pattern's keys, and the
+// join reads them.
 constexpr int64_t kPagedFew = 8;
 constexpr int64_t kPagedRows = 128;      // query rows of a tile
 constexpr int64_t kPagedKeyTile = 64;    // its keys at a time
@@ -127,7 +128,7 @@ struct PagedPattern {
   int32_t tile_splits;       // splits of a tile's keys
   int32_t tile_slot;         // its first slot there
   int32_t tiles;             // bound on the pattern's query tiles per head
-  int32_t item_begin;        // its first workgroup of the tile launch
+  int32_t item_begin;        // its first workgroup among the tiles'
 };
 
 struct PagedPlan {
@@ -135,7 +136,8 @@ struct PagedPlan {
   int dtype, page_log2, npat;
   float scale;
   bool all_few;              // every token by itself
-  bool by_token;             // single tokens are listed by token, else as (sequence, token < kPagedFew)
+  bool by_token;             // single tokens are listed by token, else as (sequence, token < few)
+  int64_t few;               // new tokens up to which a sequence's are computed by themselves
   int64_t singles;           // tokens listed for the first way
   int64_t one_slots, tile_slots;
   int64_t one_items, tile_items;  // workgroups
