@@ -25,15 +25,29 @@ namespace {
 
 constexpr int kHeadThreads = 256;
 constexpr int kHeadWaves = kHeadThreads / 64;
-constexpr int kMaxHeadPairs = 64;  // D <= 128
 
-// Per pair i: quarter turns per position and log2 zeta_i / scale_base, in
-// float64 (they multiply positions of up to millions).  Without a rotation
-// both are zero.
+// Per pair i of kPairs: quarter turns per position and log2 zeta_i /
+// scale_base, in float64 (they multiply positions of up to millions).  Without
+// a rotation both are zero.
+template <int kPairs>
 struct HeadTab {
-  double turn[kMaxHeadPairs];
-  double l2z[kMaxHeadPairs];
+  double turn[kPairs];
+  double l2z[kPairs];
 };
+// A lane's four pairs of it.
+struct LaneTab {
+  double turn[4], l2z[4];
+};
+template <int kPairs>
+__device__ inline LaneTab lane_tab(const HeadTab<kPairs>& tab, int pair0) {
+  LaneTab t;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    t.turn[e] = tab.turn[pair0 + e];
+    t.l2z[e] = tab.l2z[pair0 + e];
+  }
+  return t;
+}
 
 template <typename T> struct Raw8;
 template <> struct Raw8<u16> { typedef u32x4 type; };
@@ -80,14 +94,14 @@ __device__ inline float row_sum(float v) {
 struct Rotation {
   float cs[4], sn[4], up[4], down[4];
 };
-__device__ inline Rotation rotation(const HeadTab& tab, int pair0, int pos, int rel) {
+__device__ inline Rotation rotation(const LaneTab& tab, int pos, int rel) {
   Rotation r;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     // The angle in quarter turns, reduced in float64 to [-1/2, 1/2]: the
     // float32 series below then have arguments of at most pi/4 and are exact
     // to a rounding (first terms left out: x^11/11! < 2e-9, x^10/10! < 3e-8).
-    const double a = static_cast<double>(pos) * tab.turn[pair0 + e];
+    const double a = static_cast<double>(pos) * tab.turn[e];
     const double n = rint(a);
     const int quad = static_cast<int>(n);
     const float x = static_cast<float>(a - n) * 1.57079632679489662f, x2 = x * x;
@@ -97,7 +111,7 @@ __device__ inline Rotation rotation(const HeadTab& tab, int pair0, int pos, int 
     const float sq = quad & 1 ? c : s, cq = quad & 1 ? s : c;
     r.sn[e] = quad & 2 ? -sq : sq;
     r.cs[e] = (quad + 1) & 2 ? -cq : cq;
-    const double z = static_cast<double>(rel) * tab.l2z[pair0 + e];
+    const double z = static_cast<double>(rel) * tab.l2z[e];
     const double k = rint(z);
     const float f = static_cast<float>(z - k);
     r.up[e] = ldexpf(__builtin_amdgcn_exp2f(f), static_cast<int>(k));
@@ -117,7 +131,6 @@ struct HeadFwdArgs {
   int32_t B, H, Hkv, num_pages, page_log2, max_pages, center;
   float eps;
   FastDiv fn;               // division by N: a token's position without a cache
-  HeadTab tab;
 };
 
 // The sequence that token tok belongs to, by all lanes of a wave: start [B + 1]
@@ -135,7 +148,7 @@ __device__ inline int sequence_of(const int32_t* start, int B, int tok, int lane
 }
 
 template <typename T, int D, bool kCache>
-__global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a) {
+__global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a, HeadTab<D / 2> tab) {
   typedef typename Raw8<T>::type Raw;
   constexpr int kLanes = D / 8;        // lanes per row
   constexpr int kRows = 64 / kLanes;   // rows a wave holds at once
@@ -154,6 +167,7 @@ __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a) {
     const T* p = row < nq ? q + row * D : row < nk ? k + (row - nq) * D : v + (row - nk) * D;
     return *reinterpret_cast<const Raw*>(p);
   };
+  const LaneTab lt = lane_tab(tab, ch * 4);
   const int first = a.q ? 0 : nq;  // without queries their rows are passed over
   Raw x[kUnroll];
 #pragma unroll
@@ -183,7 +197,7 @@ __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a) {
   } else {
     pos = static_cast<int>(tok) - static_cast<int>(a.fn.div(static_cast<uint32_t>(tok)) * a.fn.d);
   }
-  const Rotation rt = rotation(a.tab, ch * 4, live ? pos : 0, live ? pos - a.center : 0);
+  const Rotation rt = rotation(lt, live ? pos : 0, live ? pos - a.center : 0);
   const bool norm_q = a.qw != nullptr, norm_k = a.kw != nullptr;
   float wq[8], wk[8];
 #pragma unroll
@@ -245,11 +259,10 @@ struct HeadBwdArgs {
   int32_t H, Hkv, center;
   float eps;
   FastDiv fn;
-  HeadTab tab;
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kHeadThreads, 4) void heads_bwd(HeadBwdArgs a) {
+__global__ __launch_bounds__(kHeadThreads, sizeof(T) == 2 ? 4 : 3) void heads_bwd(HeadBwdArgs a, HeadTab<D / 2> tab) {
   typedef typename Raw8<T>::type Raw;
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;
   __shared__ float red[kHeadWaves][2 * D];
@@ -282,9 +295,10 @@ __global__ __launch_bounds__(kHeadThreads, 4) void heads_bwd(HeadBwdArgs a) {
     }
   };
   load(tok, 0);
+  const LaneTab lt = lane_tab(tab, ch * 4);
   for (; tok < a.T; tok += stride) {
     const int pos = static_cast<int>(tok) - static_cast<int>(a.fn.div(static_cast<uint32_t>(tok)) * a.fn.d);
-    const Rotation rt = rotation(a.tab, ch * 4, pos, pos - a.center);
+    const Rotation rt = rotation(lt, pos, pos - a.center);
     for (int r0 = 0; r0 < rows; r0 += kRows) {
       const Raw x = nx, dy = ndy;
       const bool last = r0 + kRows >= rows;
@@ -375,32 +389,45 @@ __global__ __launch_bounds__(kHeadThreads) void heads_sum(const float* part, T* 
   else *dst = t;
 }
 
-HeadTab make_tab(const HeadRotation& r, int D) {
-  HeadTab t{};
-  if (!r.rotate) return t;
-  const double l2b = std::log2(static_cast<double>(r.base)), gamma = r.gamma;
-  for (int i = 0; i < D / 2; ++i) {
-    t.turn[i] = std::exp2(-2.0 * i / D * l2b) * 0.63661977236758134308;  // 2 / pi
-    t.l2z[i] = std::log2((2.0 * i / D + gamma) / (1.0 + gamma)) / r.scale_base;
+// The constants of a rotation.  They depend on the parameters alone and are
+// kept for the next call with the same ones (64 logarithms and powers take as
+// long as a third of a launch).
+template <int kPairs>
+const HeadTab<kPairs>& make_tab(const HeadRotation& r) {
+  static thread_local HeadRotation known{};
+  static thread_local HeadTab<kPairs> t{};
+  if (r.rotate != known.rotate || r.base != known.base || r.gamma != known.gamma || r.scale_base != known.scale_base) {
+    known = r;
+    const double l2b = r.rotate ? std::log2(static_cast<double>(r.base)) : 0.0, gamma = r.gamma;
+    for (int i = 0; i < kPairs; ++i) {
+      const double x = static_cast<double>(i) / kPairs;  // 2 i / D
+      t.turn[i] = r.rotate ? std::exp2(-x * l2b) * 0.63661977236758134308 : 0.0;  // 2 / pi
+      t.l2z[i] = r.rotate ? std::log2((x + gamma) / (1.0 + gamma)) / r.scale_base : 0.0;
+    }
   }
   return t;
 }
 
+template <typename T, int D, bool kCache>
+void launch_fwd_d(const HeadFwdArgs& a, const HeadRotation& r, hipStream_t stream) {
+  hipLaunchKernelGGL((heads_fwd<T, D, kCache>), grid_of((a.T + kHeadWaves - 1) / kHeadWaves), dim3(kHeadThreads), 0,
+                     stream, a, make_tab<D / 2>(r));
+}
+
 template <typename T, bool kCache>
-void launch_fwd(const HeadFwdArgs& a, int D, hipStream_t stream) {
-  const dim3 grid = grid_of((a.T + kHeadWaves - 1) / kHeadWaves);
-  if (D == 32) hipLaunchKernelGGL((heads_fwd<T, 32, kCache>), grid, dim3(kHeadThreads), 0, stream, a);
-  else if (D == 64) hipLaunchKernelGGL((heads_fwd<T, 64, kCache>), grid, dim3(kHeadThreads), 0, stream, a);
-  else hipLaunchKernelGGL((heads_fwd<T, 128, kCache>), grid, dim3(kHeadThreads), 0, stream, a);
+void launch_fwd(const HeadFwdArgs& a, const HeadRotation& r, int D, hipStream_t stream) {
+  if (D == 32) launch_fwd_d<T, 32, kCache>(a, r, stream);
+  else if (D == 64) launch_fwd_d<T, 64, kCache>(a, r, stream);
+  else launch_fwd_d<T, 128, kCache>(a, r, stream);
 }
 
 template <typename T>
-void launch_bwd(const HeadBwdArgs& a, void* dqw, void* dkw, int D, int nwg, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(nwg));
-  if (D == 32) hipLaunchKernelGGL((heads_bwd<T, 32>), grid, dim3(kHeadThreads), 0, stream, a);
-  else if (D == 64) hipLaunchKernelGGL((heads_bwd<T, 64>), grid, dim3(kHeadThreads), 0, stream, a);
-  else hipLaunchKernelGGL((heads_bwd<T, 128>), grid, dim3(kHeadThreads), 0, stream, a);
-  hipLaunchKernelGGL(heads_sum<T>, dim3(static_cast<unsigned>(D / 8)), dim3(kHeadThreads), 0, stream,
+void launch_bwd(const HeadBwdArgs& a, const HeadRotation& r, void* dqw, void* dkw, int D, int nwg, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(nwg)), threads(kHeadThreads);
+  if (D == 32) hipLaunchKernelGGL((heads_bwd<T, 32>), grid, threads, 0, stream, a, make_tab<16>(r));
+  else if (D == 64) hipLaunchKernelGGL((heads_bwd<T, 64>), grid, threads, 0, stream, a, make_tab<32>(r));
+  else hipLaunchKernelGGL((heads_bwd<T, 128>), grid, threads, 0, stream, a, make_tab<64>(r));
+  hipLaunchKernelGGL(heads_sum<T>, dim3(static_cast<unsigned>(D / 8)), threads, 0, stream,
                      static_cast<const float*>(a.part), static_cast<T*>(dqw), static_cast<T*>(dkw), nwg, D);
 }
 
@@ -416,9 +443,8 @@ hipError_t launch_qk_norm(const QkNormCall& c, hipStream_t stream) {
   a.center = static_cast<int32_t>(c.rot.center);
   a.eps = c.eps;
   a.fn = make_fastdiv(static_cast<uint32_t>(c.N));
-  a.tab = make_tab(c.rot, static_cast<int>(c.D));
-  if (c.dtype == DA_BF16) launch_fwd<u16, false>(a, static_cast<int>(c.D), stream);
-  else launch_fwd<float, false>(a, static_cast<int>(c.D), stream);
+  if (c.dtype == DA_BF16) launch_fwd<u16, false>(a, c.rot, static_cast<int>(c.D), stream);
+  else launch_fwd<float, false>(a, c.rot, static_cast<int>(c.D), stream);
   return hipGetLastError();
 }
 
@@ -440,10 +466,9 @@ hipError_t launch_qk_norm_bwd(const QkNormCall& c, const void* dqo, const void* 
   a.center = static_cast<int32_t>(c.rot.center);
   a.eps = c.eps;
   a.fn = make_fastdiv(static_cast<uint32_t>(c.N));
-  a.tab = make_tab(c.rot, static_cast<int>(c.D));
   const int nwg = static_cast<int>(qk_norm_groups(a.T));
-  if (c.dtype == DA_BF16) launch_bwd<u16>(a, dqw, dkw, static_cast<int>(c.D), nwg, stream);
-  else launch_bwd<float>(a, dqw, dkw, static_cast<int>(c.D), nwg, stream);
+  if (c.dtype == DA_BF16) launch_bwd<u16>(a, c.rot, dqw, dkw, static_cast<int>(c.D), nwg, stream);
+  else launch_bwd<float>(a, c.rot, dqw, dkw, static_cast<int>(c.D), nwg, stream);
   return hipGetLastError();
 }
 
@@ -463,9 +488,8 @@ hipError_t launch_cache_append(const QkNormCall& c, const void* v, int64_t v_str
   a.max_pages = static_cast<int32_t>(cache.max_pages);
   a.center = static_cast<int32_t>(c.rot.center);
   a.eps = c.eps;
-  a.tab = make_tab(c.rot, static_cast<int>(c.D));
-  if (c.dtype == DA_BF16) launch_fwd<u16, true>(a, static_cast<int>(c.D), stream);
-  else launch_fwd<float, true>(a, static_cast<int>(c.D), stream);
+  if (c.dtype == DA_BF16) launch_fwd<u16, true>(a, c.rot, static_cast<int>(c.D), stream);
+  else launch_fwd<float, true>(a, c.rot, static_cast<int>(c.D), stream);
   return hipGetLastError();
 }
 

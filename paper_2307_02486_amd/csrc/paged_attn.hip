@@ -46,12 +46,62 @@ struct PagedArgs {
   int64_t qs;  // elements between tokens of q
   int64_t one_rec, one_row, tile_rec, tile_row;  // byte offsets in the workspace
   int32_t T, B, H, Hkv, G, npat, num_pages, max_pages, page_log2;
-  int32_t by_token, few, units, one_slots, tile_items;
-  uint32_t reach;  // positions the table holds
-  FastDiv fslots, funits;  // division by one_slots and by a token's units
+  int32_t by_token, few, singles, one_slots, tile_items, one_items, join_groups;
+  uint32_t reach;     // positions the table holds
+  FastDiv fheads;     // division by H
   float scale_log2;
+  // Single tokens: the pattern that holds every key of its segment (r = 1, the
+  // longest such segment), or -1, and its segment length.
+  int32_t full, full_w;
+  FastDiv full_fw;
+  // Where each pattern's workgroups begin, beyond all others' for
+  // patterns that are not there: found without a loop over the records.
+  int32_t one_begin[DA_MAX_PATTERNS], item_begin[DA_MAX_PATTERNS];
   PagedPattern pat[DA_MAX_PATTERNS];
 };
+
+// One word of every 64 bytes of the arguments, requested together: what a
+// kernel reads of them later is then near.  (Read where they are used, a launch
+// of few workgroups waits for them a dozen times in turn.)
+__device__ inline void touch(const PagedArgs& a) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&a);
+  uint32_t x = 0;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(PagedArgs) / 4; i += 16) x |= w[i];
+  asm volatile("" ::"s"(x));
+}
+
+// The last pattern that begins at or before x.
+__device__ inline int pattern_at(const int32_t (&begin)[DA_MAX_PATTERNS], int x) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < DA_MAX_PATTERNS; ++i) n += begin[i] <= x;
+  return n - 1;
+}
+
+// The keys of pattern P that a query at position pos sees, if its head is kept:
+// positions first + t r, t < n; rho is the head offset that is kept.
+struct Lattice {
+  int rho, first, n;
+};
+__device__ inline Lattice lattice_of(const PagedPattern& P, int pos) {
+  const int seg = static_cast<int>(P.fw.div(pos)) * P.w, loc = pos - seg;
+  const int t = P.fr.div(loc), rho = loc - t * P.r;
+  return {rho, seg + rho, t + 1};
+}
+// How many of them a single token reads for P: where the list has a pattern
+// that holds every key of its segment, the others leave the keys of that
+// segment to it, which weights a key by the number of patterns that hold it.
+// (A token's patterns overlap near its position: the paper's five at 1K to 32K
+// tokens, 64 sequences, read 277 MB instead of 367.)
+__device__ inline int own_keys(const PagedArgs& a, const PagedPattern& P, bool is_full, int pos, const Lattice& x) {
+  if (a.full < 0 || is_full) return x.n;
+  const int begin = static_cast<int>(a.full_fw.div(pos)) * a.full_w;
+  return begin > x.first ? min(x.n, static_cast<int>(P.fr.div(begin - x.first - 1)) + 1) : 0;
+}
+__device__ inline int head_offset(const PagedPattern& P, int head) {
+  return head - static_cast<int>(P.fr.div(head)) * P.r;
+}
 
 // A sequence's new tokens: rows begin .. end - 1 of the call, the last of its
 // length len.
@@ -134,10 +184,14 @@ __device__ inline KeptHeads kept_heads(const PagedPattern& P, int hk, int G, int
   return {h0 + x, static_cast<int>(P.fr.div(G - 1 - x)) + 1};
 }
 
-// Row of key head hk in the cache for position pos of sequence b.  A page
-// outside the pool reads the pool's last page: in bounds, whatever the table holds.
-__device__ inline uint32_t cache_row(const PagedArgs& a, const int32_t* table, int hk, int pos) {
-  const uint32_t page = min(static_cast<uint32_t>(table[pos >> a.page_log2]), static_cast<uint32_t>(a.num_pages - 1));
+// The table's entry for position pos of a sequence, and key head hk's row of the
+// cache there.  They are two steps so that the entry can be on its way while
+// earlier tiles are: taken together, the wait for the entry would be one for
+// the tile requested before it.  A page outside the pool reads the pool's last
+// page: in bounds, whatever the table holds.
+__device__ inline int table_entry(const PagedArgs& a, const int32_t* table, int pos) { return table[pos >> a.page_log2]; }
+__device__ inline uint32_t cache_row(const PagedArgs& a, int entry, int hk, int pos) {
+  const uint32_t page = min(static_cast<uint32_t>(entry), static_cast<uint32_t>(a.num_pages - 1));
   return ((page * a.Hkv + hk) << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
 }
 
@@ -160,35 +214,42 @@ __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
 
-// A workgroup's place among the single tokens' items: unit u = (token, key
-// head, block of 16 of its query heads) on XCD u mod 8 with all its slots.
+// A workgroup's place among the single tokens' items, pattern by pattern: unit
+// u = (token e, number of its block of heads) runs with all its splits on XCD u
+// mod 8 (dealt out split by split over the XCDs, the 472 MB of 8 sequences with
+// heads of 128 took 105 us instead of 90).
 struct OneItem {
-  int e, slot, hk, block;
+  int pi, split, e, head;
 };
-__device__ inline bool one_item(const PagedArgs& a, int idx, OneItem& it, int heads) {
-  const int k = idx >> 3;
-  const int j = a.fslots.div(k);
-  const int unit = j * 8 + (idx & 7);
-  if (unit >= a.units) return false;
-  it.slot = k - j * a.one_slots;
-  it.e = a.funits.div(unit);
-  const int rest = unit - it.e * a.funits.d;
-  it.block = rest / heads;
-  it.hk = rest - it.block * heads;
-  return true;
+__device__ inline bool one_item(const PagedArgs& a, int idx, OneItem& it) {
+  if (idx >= a.one_items) return false;
+  it.pi = pattern_at(a.one_begin, idx);
+  const PagedPattern& P = a.pat[it.pi];
+  const int local = idx - P.one_begin;
+  const int j = local >> 3, block8 = P.one_split.div(j);
+  const int unit = block8 * 8 + (local & 7);
+  it.split = j - block8 * P.one_split.d;
+  it.e = P.one_heads.div(unit);
+  it.head = unit - it.e * P.one_heads.d;
+  return it.e < a.singles;
 }
 
-// A wave's K operand of a 32-key tile: two blocks of 16 keys.
-template <int KC>
-struct KeyFrag {
-  u32x4 v[2][KC];
+// A wave's 32-key tile on its way: two blocks of 16 keys as operands, and V's
+// rows as they come.
+template <int D>
+struct KeyTile {
+  u32x4 k[2][D / 32];
+  u32x4 v[D / 16];
 };
 
-constexpr int kOneTile = 32;  // keys of a wave's tile
+constexpr int kOneTile = 32;    // keys of a wave's tile
+constexpr int kOneRows = 1024;  // keys whose rows are looked up at once
 template <int D>
 struct SmemOne {
-  __attribute__((aligned(16))) char v[kPgWaves][2 * kOneTile * D * 2];  // each wave's two V tiles
+  __attribute__((aligned(16))) char v[kPgWaves][kOneTile * D * 2];  // each wave's V tile
   float ml[kPgWaves][2][16];
+  u32x4 q[D / 32][64];     // Q^T operand, lane by lane
+  uint32_t row[kOneRows];  // cache rows of the split's keys, a chunk at a time
 };
 
 template <int D>
@@ -196,82 +257,85 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
   constexpr int KC = D / 32, DB = D / 16, kTile = kOneTile;
   using TL = TileLayout<D>;
   constexpr int kVLoads = kTile * TL::kSlots / 64;
-  constexpr int kBuf = kTile * D * 2;  // bytes of a V tile
-  constexpr int kJoin = D + 4;         // floats between joined rows
-  static_assert(16 * kJoin * 4 <= 2 * kBuf, "the join fits a wave's V buffers");
+  // Joined rows are D floats apart, 16-byte chunk c of row r at c ^ (r mod D/4).
+  auto join_at = [](int r, int chunk) { return r * D + 4 * (chunk ^ (r & (D / 4 - 1))); };
+  static_assert(16 * D * 4 <= kTile * D * 2, "the join fits a wave's V tile");
   auto& sv = sm.v;
   auto& sml = sm.ml;
 
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   OneItem it;
-  if (!one_item(a, idx, it, a.Hkv)) return;
-  int pi = 0;
-  for (int i = 1; i < a.npat; ++i)
-    if (it.slot >= a.pat[i].one_slot) pi = i;
+  if (!one_item(a, idx, it)) return;
+  const int pi = it.pi;
   const PagedPattern& P = a.pat[pi];
   Token tk;
   if (!single_token(a, it.e, lane, tk)) return;
-  const int g = P.fw.div(tk.pos), loc = tk.pos - g * P.w;
-  const int tq = P.fr.div(loc), rho = loc - tq * P.r;
-  KeptHeads kh = kept_heads(P, it.hk, a.G, rho);
-  const int m0 = it.block * static_cast<int>(kPagedGroupRows);
+  const Lattice lat = lattice_of(P, tk.pos);
+  // Dilations of a group's size and above keep one head of a group at most: the
+  // head-th kept one; below, every group has some, in blocks.
+  int hk = it.head, block = 0;
+  if (P.r >= a.G) {
+    const int64_t h = lat.rho + static_cast<int64_t>(it.head) * P.r;
+    if (h >= a.H) return;
+    hk = static_cast<int>(h) / a.G;
+  } else if (a.G > static_cast<int>(kPagedGroupRows)) {
+    block = it.head / a.Hkv;
+    hk = it.head - block * a.Hkv;
+  }
+  const KeptHeads kh = kept_heads(P, hk, a.G, lat.rho);
+  const int m0 = block * static_cast<int>(kPagedGroupRows);
   if (m0 >= kh.count) return;
   const int rows = min(static_cast<int>(kPagedGroupRows), kh.count - m0);
-  const int n = tq + 1, per = split_keys_of(P, n), sp = it.slot - P.one_slot;
-  const int k0 = sp * per;
+  const int n = own_keys(a, P, pi == a.full, tk.pos, lat), per = split_keys_of(P, n);
+  const int k0 = it.split * per;
   if (k0 >= n) return;
-  const int ke = min(k0 + per, n), ntile = (ke - k0 + kTile - 1) / kTile;
+  const int ke = min(k0 + per, n);
 
   const int m = lane & 15, grp = lane >> 4;
   const int head = kh.first + (m0 + min(m, rows - 1)) * P.r;
-  bf16x8 qf[KC];
-#pragma unroll
-  for (int c = 0; c < KC; ++c) {
+  // Q^T operand (kept in LDS: in registers it would spill at D = 128).
+  for (int c = wv; c < KC; c += kPgWaves) {
     const u32x4 x = load16(static_cast<const u16*>(a.q) + tk.tok * a.qs + head * D + 32 * c + 8 * grp);
-    qf[c] = __builtin_bit_cast(bf16x8, m < rows ? x : u32x4{0u, 0u, 0u, 0u});
+    sm.q[c][lane] = m < rows ? x : u32x4{0u, 0u, 0u, 0u};
   }
 
   const int32_t* table = a.table + static_cast<int64_t>(tk.b) * a.max_pages;
-  const int base = g * P.w + rho;
-  // Lanes l and l + 32 look up key l of a tile; keys past the split's end are its last.
-  auto look_up = [&](int tile) {
-    const int t = min(k0 + tile * kTile + (lane & 31), ke - 1);
-    return cache_row(a, table, it.hk, base + t * P.r);
-  };
-  int vrow[kVLoads], vslot[kVLoads];
-#pragma unroll
-  for (int i = 0; i < kVLoads; ++i) {
-    const int s = 64 * i + lane;
-    vrow[i] = s / TL::kSlots;
-    vslot[i] = (s % TL::kSlots) ^ TL::swz(vrow[i]);
-  }
-  char* my = sv[wv];
-  auto load_v = [&](uint32_t row, int buf) {
-#pragma unroll
-    for (int i = 0; i < kVLoads; ++i) {
-      const uint32_t rv = __shfl(row, vrow[i], 64);
-      const int64_t at = static_cast<int64_t>(rv) * TL::kRowBytes + vslot[i] * 16;
-      __builtin_amdgcn_global_load_lds(a.vc + at, (lds_void*)(my + buf * kBuf + 1024 * i), 16, 0, 0);
+  const int base = lat.first;
+  // Patterns whose keys this one reads too, for any head here and for the lane's.
+  unsigned with = 0, mine = 0;
+  if (pi == a.full && a.npat > 1) {
+    const PagedPattern Q = a.pat[lane & 15];  // a pattern per lane
+    const bool there = lane < a.npat && lane != pi;
+    const int rho = there ? lattice_of(Q, tk.pos).rho : 0;
+    for (int r = 0; r < rows; ++r) {
+      const bool kept = there && head_offset(Q, kh.first + (m0 + r) * P.r) == rho;
+      const unsigned mask = static_cast<unsigned>(__ballot(kept));
+      with |= mask;
+      if (m == r) mine = mask;
     }
-  };
-  auto load_k = [&](uint32_t row, KeyFrag<KC>& kf) {
+  }
+  constexpr int kVStep = 64 / TL::kSlots;  // V rows of a load
+  const int vrow = lane / TL::kSlots;
+  char* my = sv[wv];
+  // Requests the 32 keys from `key` on (counted within the chunk whose rows are in LDS).
+  auto request = [&](int key, KeyTile<D>& kt) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const uint32_t rk = __shfl(row, 16 * u + m, 64);
-      const char* p = a.kc + (static_cast<int64_t>(rk) * TL::kRowBytes + 16 * grp);
+      const char* p = a.kc + (static_cast<int64_t>(sm.row[key + 16 * u + m]) * TL::kRowBytes + 16 * grp);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) kf.v[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+      for (int c = 0; c < KC; ++c) kt.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
     }
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i)
+      kt.v[i] = *reinterpret_cast<const u32x4*>(
+          a.vc + (static_cast<int64_t>(sm.row[key + kVStep * i + vrow]) * TL::kRowBytes + (lane % TL::kSlots) * 16));
   };
   // V^T operand: lane's d = 16 db + (lane & 15), keys 4 grp + 0..3 and 16 more.
-  const int tr_r = (lane & 15) >> 2;
-  int voff[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    const int d = 16 * db + (lane & 3) * 4;
-    voff[db] = TL::offset(4 * grp + tr_r, d >> 3) + (d & 7) * 2;
-  }
+  // Block db's 16-byte slots are 2 db and 2 db + 1 before the swizzle, an
+  // exclusive or: its address is block 0's with bits of db flipped.
+  const int tr_r = 4 * grp + ((lane & 15) >> 2), tr_d = (lane & 3) * 4;
+  const uint32_t voff = TL::offset(tr_r, tr_d >> 3) + (tr_d & 7) * 2;
 
   f32x4 acc[DB];
 #pragma unroll
@@ -279,16 +343,17 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
 
-  auto compute = [&](int tile, int buf, const KeyFrag<KC>& kf) {
-    f32x4 s[2];
+  // first: the tile's first key (t)
+  auto compute = [&](int first, const KeyTile<D>& kt) {
+    f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = f32x4{0, 0, 0, 0};
+    for (int c = 0; c < KC; ++c) {
+      const bf16x8 qf = __builtin_bit_cast(bf16x8, sm.q[c][lane]);
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
-        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf.v[u][c]), qf[c], s[u], 0, 0, 0);
+      for (int u = 0; u < 2; ++u)
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt.k[u][c]), qf, s[u], 0, 0, 0);
     }
-    const int left = ke - k0 - tile * kTile - 4 * grp;  // keys from this lane's first on
+    const int left = ke - first - 4 * grp;  // keys from this lane's first on
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -308,68 +373,95 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] *= alpha;
     }
+    f32x4 count[2] = {f32x4{1, 1, 1, 1}, f32x4{1, 1, 1, 1}};
+    for (unsigned rest = with; rest; rest &= rest - 1) {
+      const int i = __builtin_ctz(rest);
+      const PagedPattern& Q = a.pat[i];
+      const int d = base + first + 4 * grp - lattice_of(Q, tk.pos).first;
+      const float one = mine >> i & 1 ? 1.0f : 0.0f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int x = d + 16 * u + e;
+          const int q = Q.fr.div(max(x, 0));
+          count[u][e] += x >= 0 && q * Q.r == x ? one : 0.0f;
+        }
+    }
     bf16x8 pb;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], c2, -m_run));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], c2, -m_run)) * count[u][e];
         l_run += p;
         pb[4 * u + e] = (__bf16)p;
       }
-    const uint32_t va = lds_addr(my) + buf * kBuf;
-    u32x2 vf[DB][2];
+    // V through the wave's own LDS tile, to be read transposed (LDS operations
+    // of a wave complete in order: no wait between).
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      vf[db][0] = lds_read_tr16<0>(va + voff[db]);
-      vf[db][1] = lds_read_tr16<16 * TL::kRowBytes>(va + voff[db]);
-    }
-    lds_wait<0>();
+    for (int i = 0; i < kVLoads; ++i)
+      *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, lane % TL::kSlots)) = kt.v[i];
+    const uint32_t va = lds_addr(my);
+    constexpr int kHalf = DB < 4 ? DB : 4;  // blocks whose V is read at once
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      lds_bind(vf[db][0]);
-      lds_bind(vf[db][1]);
-      const u32x4 v4 = {vf[db][0][0], vf[db][0][1], vf[db][1][0], vf[db][1][1]};
-      acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb, acc[db], 0, 0, 0);
+    for (int d0 = 0; d0 < DB; d0 += kHalf) {
+      u32x2 vf[kHalf][2];
+#pragma unroll
+      for (int x = 0; x < kHalf; ++x) {
+        const uint32_t at = va + (voff ^ ((d0 + x) << 5));
+        vf[x][0] = lds_read_tr16<0>(at);
+        vf[x][1] = lds_read_tr16<16 * TL::kRowBytes>(at);
+      }
+      lds_wait<0>();
+#pragma unroll
+      for (int x = 0; x < kHalf; ++x) {
+        lds_bind(vf[x][0]);
+        lds_bind(vf[x][1]);
+        const u32x4 v4 = {vf[x][0][0], vf[x][0][1], vf[x][1][0], vf[x][1][1]};
+        acc[d0 + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb, acc[d0 + x], 0, 0, 0);
+      }
     }
   };
 
-  if (wv < ntile) {
-    uint32_t row = look_up(wv);
-    KeyFrag<KC> ka, kb;
-    load_v(row, 0);
-    load_k(row, ka);
-    row = look_up(wv + kPgWaves);  // clamped to the split's last key
-    asm volatile("" ::: "memory");  // the counted waits below rely on this order
-    __builtin_amdgcn_sched_barrier(0);
-    // While a tile is computed the next one's loads are under way: all but
-    // those have to have landed (the look-up is the youngest and is waited for
-    // by its use).
-    auto step = [&](int tile, int buf, const KeyFrag<KC>& cur, KeyFrag<KC>& nxt) {
-      if (tile + kPgWaves < ntile) {
-        load_v(row, buf ^ 1);
-        load_k(row, nxt);
-        row = look_up(tile + 2 * kPgWaves);
-        wait_loads<kVLoads + 2 * KC + 1>();
-      } else {
-        wait_loads<0>();
+  for (int c0 = k0; c0 < ke; c0 += kOneRows) {
+    const int keys = min(ke - c0, kOneRows), ntile = (keys + kTile - 1) / kTile;
+    if (c0 > k0) __syncthreads();  // every wave is done with the rows before
+    // Rows past the split's end, up to a whole tile, are its last.
+    for (int i = tid; i < ntile * kTile; i += kPgThreads) {
+      const int pos = base + min(c0 + i, ke - 1) * P.r;
+      sm.row[i] = cache_row(a, table_entry(a, table, pos), hk, pos);
+    }
+    __syncthreads();
+    if (wv >= ntile) continue;
+    // While a tile is computed the next one's loads are under way.  A wave's
+    // last tile is a branch of its own, so that at every use of a tile it is
+    // known which loads are younger.
+    KeyTile<D> ta, tb;
+    request(wv * kTile, ta);
+    for (int tile = wv;;) {
+      if (tile + kPgWaves >= ntile) {
+        compute(c0 + tile * kTile, ta);
+        break;
       }
-      __builtin_amdgcn_sched_barrier(0);
-      compute(tile, buf, cur);
-    };
-    for (int tile = wv;; tile += 2 * kPgWaves) {
-      step(tile, 0, ka, kb);
-      if (tile + kPgWaves >= ntile) break;
-      step(tile + kPgWaves, 1, kb, ka);
-      if (tile + 2 * kPgWaves >= ntile) break;
+      request((tile + kPgWaves) * kTile, tb);
+      compute(c0 + tile * kTile, ta);
+      tile += kPgWaves;
+      if (tile + kPgWaves >= ntile) {
+        compute(c0 + tile * kTile, tb);
+        break;
+      }
+      request((tile + kPgWaves) * kTile, ta);
+      compute(c0 + tile * kTile, tb);
+      tile += kPgWaves;
     }
   }
 
-  // The waves' partial rows meet in LDS, each in its wave's own V buffers.
+  // The waves' partial rows meet in LDS, each in its wave's own V tile.
   l_run = sum_over_groups(l_run);
   float* jo = reinterpret_cast<float*>(my);
 #pragma unroll
-  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(jo + m * kJoin + 16 * db + 4 * grp) = acc[db];
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(jo + join_at(m, 4 * db + grp)) = acc[db];
   if (grp == 0) {
     sml[wv][0][m] = m_run;
     sml[wv][1][m] = l_run;
@@ -387,9 +479,9 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
     for (int w = 0; w < kPgWaves; ++w) {
       const float f = __builtin_amdgcn_exp2f(sml[w][0][r] - mt);
       l += f * sml[w][1][r];
-      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(sv[w]) + r * kJoin + d);
+      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(sv[w]) + join_at(r, d / 4));
     }
-    const int64_t at = (row0 + kh.first + (m0 + r) * P.r) * a.one_slots + it.slot;
+    const int64_t at = (row0 + kh.first + (m0 + r) * P.r) * a.one_slots + P.one_slot + it.split;
     o *= l > 0.0f ? 1.0f / l : 0.0f;
     *reinterpret_cast<f32x4*>(a.ws + a.one_row + (at * D + d) * 4) = o;
     if (d == 0) reinterpret_cast<float*>(a.ws + a.one_rec)[at] = mt + __builtin_amdgcn_logf(l);
@@ -406,24 +498,28 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
   __shared__ float sml[2][kGroups];
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   OneItem it;
-  if (!one_item(a, launch_index(), it, a.H)) return;
-  int pi = 0;
-  for (int i = 1; i < a.npat; ++i)
-    if (it.slot >= a.pat[i].one_slot) pi = i;
+  if (!one_item(a, launch_index(), it)) return;
+  const int pi = it.pi;
   const PagedPattern& P = a.pat[pi];
   Token tk;
   if (!single_token(a, it.e, lane, tk)) return;
-  const int head = it.hk, hk = head / a.G;
-  const int g = P.fw.div(tk.pos), loc = tk.pos - g * P.w;
-  const int tq = P.fr.div(loc), rho = loc - tq * P.r;
-  if (head - static_cast<int>(P.fr.div(head)) * P.r != rho) return;
-  const int n = tq + 1, per = split_keys_of(P, n), k0 = (it.slot - P.one_slot) * per;
+  const Lattice lat = lattice_of(P, tk.pos);
+  const int64_t kept = lat.rho + static_cast<int64_t>(it.head) * P.r;
+  if (kept >= a.H) return;
+  const int head = static_cast<int>(kept), hk = head / a.G;
+  const int n = own_keys(a, P, pi == a.full, tk.pos, lat), per = split_keys_of(P, n), k0 = it.split * per;
   if (k0 >= n) return;
   const int ke = min(k0 + per, n);
   const int grp = tid / kLanes, ch = tid % kLanes;
   const f32x4 q = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) + tk.tok * a.qs + head * D + 4 * ch);
   const int32_t* table = a.table + static_cast<int64_t>(tk.b) * a.max_pages;
-  const int base = g * P.w + rho;
+  const int base = lat.first;
+  unsigned with = 0;  // patterns whose keys this one reads too
+  if (pi == a.full && a.npat > 1) {
+    const PagedPattern Q = a.pat[lane & 15];  // a pattern per lane
+    with = static_cast<unsigned>(
+        __ballot(lane < a.npat && lane != pi && head_offset(Q, head) == lattice_of(Q, tk.pos).rho));
+  }
   float m_run = kLowest, l_run = 0.0f;
   f32x4 acc = f32x4{0, 0, 0, 0};
   for (int t0 = k0; t0 < ke; t0 += kUnroll * kGroups) {
@@ -431,7 +527,8 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int t = min(t0 + u * kGroups + grp, ke - 1);
-      const int64_t at = static_cast<int64_t>(cache_row(a, table, hk, base + t * P.r)) * D + 4 * ch;
+      const int pos = base + t * P.r;
+      const int64_t at = static_cast<int64_t>(cache_row(a, table_entry(a, table, pos), hk, pos)) * D + 4 * ch;
       k[u] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.kc) + at);
       v[u] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.vc) + at);
     }
@@ -448,9 +545,22 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
     m_run = mx;
     l_run *= alpha;
     acc *= alpha;
+    float count[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) count[u] = 1.0f;
+    for (unsigned rest = with; rest; rest &= rest - 1) {
+      const PagedPattern& Q = a.pat[__builtin_ctz(rest)];
+      const int d = base + t0 + grp - lattice_of(Q, tk.pos).first;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int x = d + u * kGroups;
+        const int q = Q.fr.div(max(x, 0));
+        count[u] += x >= 0 && q * Q.r == x ? 1.0f : 0.0f;
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const float p = __builtin_amdgcn_exp2f(s[u] - m_run);
+      const float p = __builtin_amdgcn_exp2f(s[u] - m_run) * count[u];
       l_run += p;
       acc += p * v[u];
     }
@@ -473,7 +583,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
     l += f * sml[1][w];
     o += f * *reinterpret_cast<const f32x4*>(&so[w][4 * ch]);
   }
-  const int64_t at = (static_cast<int64_t>(it.e) * a.H + head) * a.one_slots + it.slot;
+  const int64_t at = (static_cast<int64_t>(it.e) * a.H + head) * a.one_slots + P.one_slot + it.split;
   o *= l > 0.0f ? 1.0f / l : 0.0f;
   *reinterpret_cast<f32x4*>(a.ws + a.one_row + (at * D + 4 * ch) * 4) = o;
   if (ch == 0) reinterpret_cast<float*>(a.ws + a.one_rec)[at] = mt + __builtin_amdgcn_logf(l);
@@ -539,10 +649,13 @@ __device__ inline bool query_tile(const PagedArgs& a, const PagedPattern& P, int
   return false;
 }
 
+constexpr int kTileRows = 4096;  // keys whose rows are looked up at once (three workgroups of D = 64 fit a CU)
+
 template <int D>
 struct SmemTile {
   __attribute__((aligned(16))) u16 k[2][kPagedKeyTile * D];
   __attribute__((aligned(16))) u16 v[2][kPagedKeyTile * D];
+  uint32_t row[kTileRows];  // cache rows of the keys, a chunk at a time
 };
 
 template <int D>
@@ -553,14 +666,15 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
   constexpr int kLoads = BN * TL::kSlots / 64 / kPgWaves;
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int pi = 0;
-  for (int i = 1; i < a.npat; ++i)
-    if (idx >= a.pat[i].item_begin) pi = i;
-  const PagedPattern& P = a.pat[pi];
-  // Heads next to each other, later (longer) tiles first.
+  const PagedPattern& P = a.pat[pattern_at(a.item_begin, idx)];
+  // Unit u = (run of tiles, head) runs on XCD u mod 8, whose L2 then serves the
+  // run's keys after their first fetch; later (longer) tiles first.
   const int local = idx - P.item_begin;
-  const int rest = local / a.H, head = local - rest * a.H;
-  const int ti = rest / P.tile_splits, sp = rest - ti * P.tile_splits;
+  const int k8 = local >> 3, unit8 = P.tile_unit.div(k8);
+  const int within = k8 - unit8 * P.tile_unit.d, unit = unit8 * 8 + (local & 7);
+  const int run = a.fheads.div(unit), head = unit - run * a.H;
+  const int in_run = P.tile_split.div(within), sp = within - in_run * P.tile_split.d;
+  const int ti = run * P.unit_tiles + in_run;
   if (ti >= P.tiles) return;
   QueryTile qt;
   if (!query_tile(a, P, P.tiles - 1 - ti, lane, qt)) return;
@@ -577,7 +691,7 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
   if (q0 >= qend) return;
   const int hk = head / a.G;
   // this split's keys
-  const int per = ((qend + P.tile_splits - 1) / P.tile_splits + BN - 1) / BN * BN;
+  const int per = (static_cast<int>(P.tile_split.div(qend + P.tile_split.d - 1)) + BN - 1) / BN * BN;
   const int kb = sp * per, ke = min(kb + per, qend);
   const int slot = P.tile_slot + sp;
   const int base = gs + off;  // position of t = 0
@@ -607,18 +721,13 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
     lrow[i] = s / TL::kSlots;
     lslot[i] = (s % TL::kSlots) ^ TL::swz(lrow[i]);
   }
-  const int ntile = (ke - kb + BN - 1) / BN;
-  uint32_t row[kLoads];
-  auto look_up = [&](int jt) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) row[i] = cache_row(a, table, hk, base + min(kb + jt * BN + lrow[i], ke - 1) * P.r);
-  };
-  auto load_tile = [&](int buf) {
+  // Tile jt of the chunk whose rows are in LDS.
+  auto load_tile = [&](int jt, int buf) {
     char* kl = reinterpret_cast<char*>(&sm.k[buf][0]);
     char* vl = reinterpret_cast<char*>(&sm.v[buf][0]);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int64_t at = static_cast<int64_t>(row[i]) * TL::kRowBytes + lslot[i] * 16;
+      const uint64_t at = static_cast<uint64_t>(sm.row[jt * BN + lrow[i]]) * TL::kRowBytes + lslot[i] * 16;
       const int lds_off = 1024 * (wv * kLoads + i);
       __builtin_amdgcn_global_load_lds(a.kc + at, (lds_void*)(kl + lds_off), 16, 0, 0);
       __builtin_amdgcn_global_load_lds(a.vc + at, (lds_void*)(vl + lds_off), 16, 0, 0);
@@ -634,9 +743,6 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
       const int d = db * 32 + tr_d;
       vtr_off[db][t] = TL::offset(8 * t + 4 * hi + tr_r, d >> 3) + (d & 7) * 2;
     }
-  look_up(0);
-  load_tile(0);
-  look_up(1);  // past the end: the last key again
   bf16x8 qreg[KC];
 #pragma unroll
   for (int c = 0; c < KC; ++c) qreg[c] = __builtin_bit_cast(bf16x8, qraw[c]);
@@ -646,14 +752,19 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
   for (int db = 0; db < DB; ++db) acc_o[db] = f32x16{};
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
+  for (int c0 = kb; c0 < ke; c0 += kTileRows) {
+  const int ntile = (min(ke - c0, kTileRows) + BN - 1) / BN;
+  for (int i = tid; i < ntile * BN; i += kPgThreads) {  // past the split's end: its last key
+    const int pos = base + min(c0 + i, ke - 1) * P.r;
+    sm.row[i] = cache_row(a, table_entry(a, table, pos), hk, pos);
+  }
+  __syncthreads();
+  load_tile(0, 0);
   wait_loads<0>();
   __syncthreads();
   for (int jt = 0; jt < ntile; ++jt) {
-    const int cur = jt & 1, k0 = kb + jt * BN;
-    if (jt + 1 < ntile) {
-      load_tile(cur ^ 1);
-      look_up(jt + 2);
-    }
+    const int cur = jt & 1, k0 = c0 + jt * BN;
+    if (jt + 1 < ntile) load_tile(jt + 1, cur ^ 1);
     const char* kl = reinterpret_cast<const char*>(&sm.k[cur][0]);
     const char* vl = reinterpret_cast<const char*>(&sm.v[cur][0]);
     if (k0 <= wq_lo + 31 && wq_lo < qend) {  // not all keys after this wave's queries
@@ -741,6 +852,7 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
     wait_loads<0>();
     __syncthreads();
   }
+  }
 
   // The wave's 32 rows as fp16 times a power of two per row (within 2^-11 of
   // the row's largest element: beside bf16 outputs), staged so that whole rows
@@ -784,7 +896,8 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
 
 // One launch for both: the tiles first, as they take longer.
 template <int D, bool kTiles>
-__global__ __launch_bounds__(kPgThreads) void paged_attn(PagedArgs a) {
+__global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_attn(PagedArgs a) {
+  touch(a);
   const int idx = launch_index();
   if constexpr (kTiles) {
     union Smem {
@@ -802,8 +915,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_attn(PagedArgs a) {
 
 // ---------------------------------------------------------------------------
 // The join: a row's partials, of every pattern that keeps it and every split,
-// mixed by their denominators.  D/8 lanes read a partial row; kSubs partials
-// of a row at a time, so that their loads are under way together.
+// mixed by their denominators.
 // ---------------------------------------------------------------------------
 __device__ inline void put8(u16* p, const f32x8& v) {
   bf16x8 b;
@@ -813,103 +925,209 @@ __device__ inline void put8(u16* p, const f32x8& v) {
 }
 __device__ inline void put8(float* p, const f32x8& v) { *reinterpret_cast<f32x8*>(p) = v; }
 
-template <typename T, int D, bool kTiles>
-__global__ __launch_bounds__(kPgThreads) void paged_join(PagedArgs a) {
-  constexpr int kLanes = D / 8;
-  constexpr int kSubs = kTiles ? 4 : 64 / kLanes;
-  constexpr int kRows = 64 / kLanes / kSubs;  // rows of a wave
-  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
-  const int ch = lane % kLanes, sub = lane / kLanes % kSubs, mine = lane / (kLanes * kSubs);
-  const int row0 = (launch_index() * kPgWaves + __builtin_amdgcn_readfirstlane(tid >> 6)) * kRows;
-  const int total = a.T * a.H;
-  if (row0 >= total) return;
-  int toks[kRows];
-  Sequence sq[kRows];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) toks[i] = min(row0 + i, total - 1) / a.H;
-  find_sequences(a, toks, lane, sq);
-  int tok = toks[0], pos = position_of(a, sq[0], toks[0]), begin = sq[0].begin, n = sq[0].end - begin, b = sq[0].b;
-#pragma unroll
-  for (int i = 1; i < kRows; ++i)
-    if (mine == i) {
-      tok = toks[i];
-      pos = position_of(a, sq[i], tok);
-      begin = sq[i].begin;
-      n = sq[i].end - begin;
-      b = sq[i].b;
-    }
-  const int row = row0 + mine;
-  const int head = row - tok * a.H;
-  const bool single = !kTiles || n <= a.few;
-  const int64_t e = a.by_token ? tok : static_cast<int64_t>(b) * a.few + (tok - begin);
-  const float* one_rec = reinterpret_cast<const float*>(a.ws + a.one_rec) + (e * a.H + head) * a.one_slots;
-  const float* one_row = reinterpret_cast<const float*>(a.ws + a.one_row) + (e * a.H + head) * a.one_slots * D;
-
+// A running mixture: m the largest log-sum-exp (log2 units) so far, l and acc
+// the sums of the weights 2^(x - m) and of the weighted rows.
+struct Mix {
   float m = -INFINITY, l = 0.0f;
   f32x8 acc = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-  if (pos >= 0 && row < total) {
-    for (int want = sub;; want += kSubs) {  // the want-th partial of the row
-      int slot = -1, before = 0;
-      for (int i = 0; i < a.npat; ++i) {
-        const PagedPattern& P = a.pat[i];
-        const int g = P.fw.div(pos), loc = pos - g * P.w;
-        const int t = P.fr.div(loc), rho = loc - t * P.r;
-        if (head - static_cast<int>(P.fr.div(head)) * P.r != rho) continue;
-        const int used = single ? t / split_keys_of(P, t + 1) + 1 : P.tile_splits;
-        if (want >= before && want < before + used) slot = (single ? P.one_slot : P.tile_slot) + want - before;
-        before += used;
-      }
-      if (slot < 0) break;
-      float x, scale = 1.0f;
-      f32x8 o;
-      if (single) {
-        x = one_rec[slot];
-        o = *reinterpret_cast<const f32x8*>(one_row + static_cast<int64_t>(slot) * D + ch * 8);
-      } else {
-        const int64_t at = static_cast<int64_t>(slot) * total + row;
-        const f32x2 r = reinterpret_cast<const f32x2*>(a.ws + a.tile_rec)[at];
-        const f16x8 h = *reinterpret_cast<const f16x8*>(a.ws + a.tile_row + (at * D + ch * 8) * 2);
-        x = r[0];
-        scale = r[1];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) o[c] = static_cast<float>(h[c]);
-      }
-      if (x == -INFINITY) continue;  // a split without a visible key: its row is not read
-      const float mn = fmaxf(m, x);
-      const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(x - mn);
-      m = mn;
-      l = l * f0 + f1;
-      acc = acc * f0 + o * (f1 * scale);
+  __device__ void add(float x, float scale, const f32x8& o) {  // row o * scale with weight 2^x > 0
+    const float mn = fmaxf(m, x);
+    const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(x - mn);
+    m = mn;
+    l = l * f0 + f1;
+    acc = acc * f0 + o * (f1 * scale);
+  }
+};
+template <typename T, int D>
+__device__ inline void put_row(const PagedArgs& a, int tok, int head, int ch, const Mix& x) {
+  const float inv = x.l > 0.0f ? 1.0f / x.l : 0.0f;
+  put8(static_cast<T*>(a.out) + (static_cast<int64_t>(tok) * a.H + head) * D + ch * 8, x.acc * inv);
+  if (ch == 0)
+    a.lse[static_cast<int64_t>(head) * a.T + tok] = x.l > 0.0f ? (x.m + __builtin_amdgcn_logf(x.l)) * kLn2 : -INFINITY;
+}
+
+// Single tokens: a wave per row (or a workgroup, kTogether), D/8 lanes across a
+// partial and as many partials at a time as fit: a row has tens of them.
+template <typename T, int D, bool kTogether>
+__device__ inline void join_singles(const PagedArgs& a, int group) {
+  constexpr int kLanes = D / 8, kSubs = 64 / kLanes;
+  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
+  const int ch = lane % kLanes, sub = lane / kLanes;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = kTogether ? group : group * kPgWaves + wv;
+  const int e = a.fheads.div(row), head = row - e * a.H;
+  if (e >= a.singles) return;
+  Token tk;
+  const bool there = single_token(a, e, lane, tk);
+  if (!there && a.few < a.T) return;  // not this launch part's (see join_tiles)
+  // How many partials each pattern has of the row, a pattern per lane, and
+  // their running sum: partial c is slot first + c of the pattern with upto > c.
+  static_assert(DA_MAX_PATTERNS == 16, "a pattern per lane");
+  const PagedPattern P = a.pat[lane & 15];
+  int upto = 0, first = 0;
+  if (there && (lane & 15) < a.npat) {
+    const Lattice x = lattice_of(P, tk.pos);
+    if (head_offset(P, head) == x.rho) {
+      const int n = own_keys(a, P, (lane & 15) == a.full, tk.pos, x);
+      upto = n > 0 ? (n - 1) / split_keys_of(P, n) + 1 : 0;
     }
   }
+  first = P.one_slot + upto;
 #pragma unroll
-  for (int x = kLanes; x < kLanes * kSubs; x <<= 1) {
-    const float mo = __shfl_xor(m, x, 64), lo = __shfl_xor(l, x, 64);
-    const float mn = fmaxf(m, mo);
-    const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
-    const float f1 = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
-    m = mn;
-    l = l * f0 + lo * f1;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c] = acc[c] * f0 + __shfl_xor(acc[c], x, 64) * f1;
+  for (int x = 1; x < 16; x <<= 1) {
+    const int o = __shfl_up(upto, x, 16);
+    if ((lane & 15) >= x) upto += o;
   }
-  if (sub != 0 || row >= total) return;
-  acc *= l > 0.0f ? 1.0f / l : 0.0f;
-  put8(static_cast<T*>(a.out) + static_cast<int64_t>(row) * D + ch * 8, acc);
-  if (ch == 0) a.lse[static_cast<int64_t>(head) * a.T + tok] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  first -= upto;
+  const int count = __builtin_amdgcn_readlane(upto, 15);
+  const int64_t at = (static_cast<int64_t>(e) * a.H + head) * a.one_slots;
+  const float* rec = reinterpret_cast<const float*>(a.ws + a.one_rec) + at;
+  const float* part = reinterpret_cast<const float*>(a.ws + a.one_row) + at * D + ch * 8;
+  Mix x;
+  constexpr int kAtOnce = kTogether ? kSubs * kPgWaves : kSubs;
+  for (int c0 = kTogether ? kSubs * wv : 0; c0 < count; c0 += kAtOnce) {
+    const int c = c0 + sub;
+    int slot = 0;
+    for (int i = a.npat - 1; i >= 0; --i)
+      if (c < __builtin_amdgcn_readlane(upto, i)) slot = __builtin_amdgcn_readlane(first, i) + c;
+    if (c < count) x.add(rec[slot], 1.0f, *reinterpret_cast<const f32x8*>(part + static_cast<int64_t>(slot) * D));
+  }
+  auto meet = [&](float mo, float lo, auto&& other) {
+    const float mn = fmaxf(x.m, mo);
+    const float f0 = x.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.m - mn);
+    const float f1 = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
+    x.m = mn;
+    x.l = x.l * f0 + lo * f1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.acc[i] = x.acc[i] * f0 + other(i) * f1;
+  };
+#pragma unroll
+  for (int s = kLanes; s < 64; s <<= 1)
+    meet(__shfl_xor(x.m, s, 64), __shfl_xor(x.l, s, 64), [&](int i) { return __shfl_xor(x.acc[i], s, 64); });
+  if constexpr (kTogether) {
+    __shared__ __attribute__((aligned(16))) float rows[kPgWaves][D];
+    __shared__ float ml[kPgWaves][2];
+    if (sub == 0) *reinterpret_cast<f32x8*>(&rows[wv][ch * 8]) = x.acc;
+    if (lane == 0) {
+      ml[wv][0] = x.m;
+      ml[wv][1] = x.l;
+    }
+    __syncthreads();
+    if (wv != 0) return;
+#pragma unroll
+    for (int w = 1; w < kPgWaves; ++w) meet(ml[w][0], ml[w][1], [&](int i) { return rows[w][ch * 8 + i]; });
+  }
+  if (sub == 0) put_row<T, D>(a, a.by_token ? e : tk.tok, head, ch, x);
+}
+
+// Tokens of tiles, and those of no sequence: D/8 lanes a row, head by head and
+// token by token, the loads of all patterns before their use.  kPats bounds the
+// patterns at compile time.
+template <int D, int kPats>
+__device__ inline void join_tiles(const PagedArgs& a, int group) {
+  constexpr int kLanes = D / 8;
+  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
+  const int ch = tid % kLanes;
+  const int total = a.T * a.H, row = min(group * (kPgThreads / kLanes) + tid / kLanes, total - 1);
+  const int tok = a.fheads.div(row), head = row - tok * a.H;
+  // The sequences of the wave's first and last token; a wave across more looks
+  // for each lane's.
+  const int ends[2] = {__builtin_amdgcn_readfirstlane(tok), __builtin_amdgcn_readlane(tok, 63)};
+  Sequence sq[2];
+  find_sequences(a, ends, lane, sq);
+  Sequence s = tok == ends[1] ? sq[1] : sq[0];
+  if ((sq[0].b != sq[1].b || sq[0].b < 0) && tok != ends[0] && tok != ends[1]) {
+    int lo = max(sq[0].b, 0), hi = sq[1].b < 0 ? a.B - 1 : sq[1].b;
+    while (lo < hi) {  // the last sequence that begins at or before tok
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.start[mid] <= tok) lo = mid;
+      else hi = mid - 1;
+    }
+    s = Sequence{lo, a.start[lo], a.start[lo + 1], a.lens[lo]};
+  }
+  const int pos = tok >= s.begin ? position_of(a, s, tok) : -1;
+  if (pos >= 0 && s.end - s.begin <= a.few) return;  // computed by itself
+  Mix x;
+  if (pos >= 0) {
+    int64_t at[kPats];
+    int splits = 0;
+#pragma unroll
+    for (int i = 0; i < kPats; ++i) {
+      at[i] = -1;
+      if (i >= a.npat) continue;
+      const PagedPattern& P = a.pat[i];
+      if (head_offset(P, head) != lattice_of(P, pos).rho) continue;
+      at[i] = static_cast<int64_t>(P.tile_slot) * total + row;
+      splits = max(splits, static_cast<int>(P.tile_split.d));
+    }
+    for (int sp = 0; sp < splits; ++sp) {
+      f32x2 rec[kPats];
+      f16x8 o[kPats];
+#pragma unroll
+      for (int i = 0; i < kPats; ++i) {
+        rec[i] = f32x2{-INFINITY, 0.0f};
+        if (at[i] < 0 || sp >= static_cast<int>(a.pat[i].tile_split.d)) continue;
+        const int64_t r = at[i] + static_cast<int64_t>(sp) * total;
+        rec[i] = reinterpret_cast<const f32x2*>(a.ws + a.tile_rec)[r];
+        o[i] = *reinterpret_cast<const f16x8*>(a.ws + a.tile_row + (r * D + ch * 8) * 2);
+      }
+#pragma unroll
+      for (int i = 0; i < kPats; ++i) {
+        if (rec[i][0] == -INFINITY) continue;  // a split without a visible key: its row holds nothing
+        f32x8 f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) f[c] = static_cast<float>(o[i][c]);
+        x.add(rec[i][0], rec[i][1], f);
+      }
+    }
+  }
+  if (group * (kPgThreads / kLanes) + tid / kLanes < total) put_row<u16, D>(a, tok, head, ch, x);
+}
+
+// kTogether: the waves of a workgroup share a single token's row.
+template <typename T, int D, bool kTogether>
+__global__ __launch_bounds__(kPgThreads) void paged_join(PagedArgs a) {
+  touch(a);
+  join_singles<T, D, kTogether>(a, launch_index());
+}
+// The rows of tiles first, then the single tokens'.
+template <int D, int kPats>
+__global__ __launch_bounds__(kPgThreads) void paged_join_all(PagedArgs a) {
+  touch(a);
+  const int group = launch_index();
+  if (group < a.join_groups) join_tiles<D, kPats>(a, group);
+  else join_singles<u16, D, false>(a, group - a.join_groups);
+}
+
+// Rows of single tokens: a workgroup each below this many (tens of partials
+// that one wave reads in several rounds: 12 rows of a token at 32K tokens took
+// 10.0 us a wave each, 5.6 a workgroup each), a wave each from there.
+constexpr int64_t kShared = 512;
+template <typename T, int D>
+void launch_join(int64_t rows, const PagedArgs& a, hipStream_t stream) {
+  const dim3 threads(kPgThreads);
+  if (rows < kShared) hipLaunchKernelGGL((paged_join<T, D, true>), grid_of(rows), threads, 0, stream, a);
+  else hipLaunchKernelGGL((paged_join<T, D, false>), grid_of((rows + kPgWaves - 1) / kPgWaves), threads, 0, stream, a);
 }
 
 template <int D>
-void launch_all(const PagedPlan& p, const PagedArgs& a, hipStream_t stream) {
+void launch_all(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
   const dim3 threads(kPgThreads), grid = grid_of(p.tile_items + p.one_items);
-  if (p.dtype == DA_F32) hipLaunchKernelGGL(paged_one_f32<D>, grid, threads, 0, stream, a);
-  else if (p.all_few) hipLaunchKernelGGL((paged_attn<D, false>), grid, threads, 0, stream, a);
-  else hipLaunchKernelGGL((paged_attn<D, true>), grid, threads, 0, stream, a);
-  const int64_t rows = p.T * p.H, few = (rows + kPgWaves - 1) / kPgWaves;
-  constexpr int kPerGroup = kPgWaves * (64 / (D / 8) / 4);  // rows of a workgroup beside tiles
-  if (p.dtype == DA_F32) hipLaunchKernelGGL((paged_join<float, D, false>), grid_of(few), threads, 0, stream, a);
-  else if (p.all_few) hipLaunchKernelGGL((paged_join<u16, D, false>), grid_of(few), threads, 0, stream, a);
-  else hipLaunchKernelGGL((paged_join<u16, D, true>), grid_of((rows + kPerGroup - 1) / kPerGroup), threads, 0, stream, a);
+  const int64_t singles = p.singles * p.H;
+  if (p.dtype == DA_F32) {
+    hipLaunchKernelGGL(paged_one_f32<D>, grid, threads, 0, stream, a);
+    launch_join<float, D>(singles, a, stream);
+  } else if (p.all_few) {
+    hipLaunchKernelGGL((paged_attn<D, false>), grid, threads, 0, stream, a);
+    launch_join<u16, D>(singles, a, stream);
+  } else {
+    hipLaunchKernelGGL((paged_attn<D, true>), grid, threads, 0, stream, a);
+    constexpr int kRows = kPgThreads / (D / 8);
+    a.join_groups = static_cast<int32_t>((p.T * p.H + kRows - 1) / kRows);
+    const dim3 join = grid_of(a.join_groups + (singles + kPgWaves - 1) / kPgWaves);
+    if (p.npat <= 5) hipLaunchKernelGGL((paged_join_all<D, 5>), join, threads, 0, stream, a);
+    else hipLaunchKernelGGL((paged_join_all<D, DA_MAX_PATTERNS>), join, threads, 0, stream, a);
+  }
 }
 
 }  // namespace
@@ -943,14 +1161,22 @@ hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, con
   a.by_token = p.by_token;
   a.few = static_cast<int32_t>(p.few);
   a.tile_items = static_cast<int32_t>(p.tile_items);
-  const int64_t per_token = p.dtype == DA_F32 ? p.H : p.Hkv * ((a.G + kPagedGroupRows - 1) / kPagedGroupRows);
-  a.units = static_cast<int32_t>(p.singles * per_token);
   a.one_slots = static_cast<int32_t>(p.one_slots);
   a.reach = static_cast<uint32_t>(p.max_pages * p.page);
-  a.fslots = make_fastdiv(static_cast<uint32_t>(p.one_slots));
-  a.funits = make_fastdiv(static_cast<uint32_t>(per_token));
+  a.one_items = static_cast<int32_t>(p.one_items);
+  a.singles = static_cast<int32_t>(p.singles);
+  a.fheads = make_fastdiv(static_cast<uint32_t>(p.H));
   a.scale_log2 = p.scale * kLog2e;
   std::copy(p.pat, p.pat + p.npat, a.pat);
+  a.full = p.full;
+  if (p.full >= 0) {
+    a.full_w = p.pat[p.full].w;
+    a.full_fw = p.pat[p.full].fw;
+  }
+  for (int i = 0; i < DA_MAX_PATTERNS; ++i) {
+    a.one_begin[i] = i < p.npat ? p.pat[i].one_begin : 0x7fffffff;
+    a.item_begin[i] = i < p.npat ? p.pat[i].item_begin : 0x7fffffff;
+  }
   if (p.D == 32) launch_all<32>(p, a, stream);
   else if (p.D == 64) launch_all<64>(p, a, stream);
   else launch_all<128>(p, a, stream);

@@ -205,22 +205,28 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   p.dtype = static_cast<int>(dtype);
   while ((int64_t{1} << p.page_log2) < page) ++p.page_log2;
   p.npat = static_cast<int>(num_patterns);
+  p.full = -1;
   p.scale = softmax_scale > 0.0f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(double(D)));
   const int64_t reach = max_pages * page;  // positions that the table holds
   p.all_few = dtype == DA_F32 || std::min(max_new, T) <= kPagedFew;
   p.few = p.all_few ? T : B == 1 ? 0 : kPagedFew;
   p.by_token = p.all_few || T <= B * p.few;
   p.singles = p.by_token ? T : B * p.few;
-  const int64_t G = H / Hkv;
-  const int64_t units = dtype == DA_F32 ? p.singles * H : p.singles * Hkv * ((G + kPagedGroupRows - 1) / kPagedGroupRows);
-  // Workgroups with work if every listed token were there (a pattern's rows
-  // belong to one head in r), and of the tiles.
+  // A single token's workgroups for one split: key heads with a kept query head,
+  // in blocks of kPagedGroupRows query heads (float32: query heads).  A token
+  // belongs to the heads of one residue mod r.
+  const int64_t G = dtype == DA_F32 ? 1 : H / Hkv, key_heads = H / G;
+  auto one_heads = [&](int64_t r) {
+    if (r >= G) return std::min(key_heads, (H + r - 1) / r);
+    return key_heads * (((G + r - 1) / r + kPagedGroupRows - 1) / kPagedGroupRows);
+  };
+  // Workgroups with work, of the listed tokens and of the tiles.
   double one_busy = 0.0, tile_busy = 0.0;
   for (int i = 0; i < p.npat; ++i) {
-    const double r = static_cast<double>(patterns[i].r);
-    one_busy += units * std::min(1.0, (dtype == DA_F32 ? 1.0 : double(G)) / r);
-    tile_busy += H * std::ceil(double(T) / r / kPagedRows);
+    one_busy += static_cast<double>(p.singles) * one_heads(patterns[i].r);
+    tile_busy += H * std::ceil(double(T) / patterns[i].r / kPagedRows);
   }
+  int64_t one_items = 0;
   int64_t items = 0;
   for (int i = 0; i < p.npat; ++i) {
     PagedPattern& t = p.pat[i];
@@ -229,28 +235,39 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     t.r = static_cast<int32_t>(std::min(patterns[i].r, kMost - 1));
     t.fw = make_fastdiv(static_cast<uint32_t>(t.w));
     t.fr = make_fastdiv(static_cast<uint32_t>(t.r));
+    if (t.r == 1 && (p.full < 0 || t.w > p.pat[p.full].w)) p.full = i;
     const int64_t keys = (t.w + int64_t{t.r} - 1) / t.r;  // of a row, at most
     const int64_t one = std::max<int64_t>(
-        1, std::min({static_cast<int64_t>(4096.0 / std::max(1.0, one_busy)), (keys + 127) / 128, int64_t{64}}));
+        1, std::min({static_cast<int64_t>(4096.0 / std::max(1.0, one_busy)), (keys + 255) / 256, int64_t{64}}));
     t.one_split = make_fastdiv(static_cast<uint32_t>(one));
     t.one_slot = static_cast<int32_t>(p.one_slots);
     p.one_slots += one;
+    t.one_heads = make_fastdiv(static_cast<uint32_t>(one_heads(patterns[i].r)));
+    if (one_items >= kMost) return DA_EINVAL;
+    t.one_begin = static_cast<int32_t>(one_items);
+    one_items += (p.singles * one_heads(patterns[i].r) + 7) / 8 * 8 * one;  // units XCD by XCD
     if (p.all_few) continue;
     const int64_t ts = std::max<int64_t>(
-        1, std::min({static_cast<int64_t>(512.0 / std::max(1.0, tile_busy)), (keys + 511) / 512, int64_t{16}}));
-    t.tile_splits = static_cast<int32_t>(ts);
+        1, std::min({static_cast<int64_t>(2048.0 / std::max(1.0, tile_busy)), (keys + 511) / 512, int64_t{16}}));
+    t.tile_split = make_fastdiv(static_cast<uint32_t>(ts));
     t.tile_slot = static_cast<int32_t>(p.tile_slots);
     p.tile_slots += ts;
     // A sequence of n tokens touches at most n / w + 2 segments, each with one
     // tile more than its rows fill.
     const int64_t tiles = std::min(T, T / (int64_t{t.r} * kPagedRows) + T / t.w + 2 * B + 2);
-    if (items + tiles * H * ts >= kMost) return DA_EINVAL;
+    // Units are dealt to the XCDs: up to 16 tiles, fewer where there would not
+    // be eight units each.
+    const int64_t unit = std::max<int64_t>(1, std::min<int64_t>(16, tiles * H / 64));
+    const int64_t units = ((tiles + unit - 1) / unit * H + 7) / 8 * 8;
+    if (items + units * unit * ts >= kMost) return DA_EINVAL;
+    t.tile_unit = make_fastdiv(static_cast<uint32_t>(unit * ts));
+    t.unit_tiles = static_cast<int32_t>(unit);
     t.tiles = static_cast<int32_t>(tiles);
     t.item_begin = static_cast<int32_t>(items);
-    items += tiles * H * ts;
+    items += units * unit * ts;
   }
-  p.tile_items = (items + 7) / 8 * 8;  // the single tokens' workgroups after them keep their XCDs
-  p.one_items = (units + 7) / 8 * 8 * p.one_slots;
+  p.tile_items = items;
+  p.one_items = one_items;
   if (p.one_items + p.tile_items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
   uint64_t off = 0;
   auto take = [&off](uint64_t bytes) {

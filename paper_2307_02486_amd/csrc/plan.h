@@ -125,7 +125,11 @@ struct PagedPattern {
   FastDiv fw, fr;            // divisions by them
   FastDiv one_split;         // division by the splits of a single token's keys
   int32_t one_slot;          // its first slot there
-  int32_t tile_splits;       // splits of a tile's keys
+  int32_t one_begin;         // its first workgroup among the single tokens'
+  FastDiv one_heads;         // division by a token's workgroups for one split
+  FastDiv tile_split;        // division by the splits of a tile's keys
+  FastDiv tile_unit;         // division by the workgroups of a unit: tiles of one head next to each other, with their splits
+  int32_t unit_tiles;        // a unit's tiles
   int32_t tile_slot;         // its first slot there
   int32_t tiles;             // bound on the pattern's query tiles per head
   int32_t item_begin;        // its first workgroup among the tiles'
@@ -137,6 +141,7 @@ struct PagedPlan {
   float scale;
   bool all_few;              // every token by itself
   bool by_token;             // single tokens are listed by token, else as (sequence, token < few)
+  int full;                  // the pattern with r = 1 and the longest segment, or -1
   int64_t few;               // new tokens up to which a sequence's are computed by themselves
   int64_t singles;           // tokens listed for the first way
   int64_t one_slots, tile_slots;

@@ -416,16 +416,42 @@ def _token_stride(name: str, t: torch.Tensor, lead: int, dtype, device) -> int:
     return H * D if step is None else step
 
 
-def _qk_shapes(q: torch.Tensor, k: torch.Tensor, q_weight, k_weight):
-    if q.device.type != "cuda":
+# The sizes and strides of a call, validated and with what follows from them,
+# by the shapes (at most 256 of each operator; nothing of a tensor is kept).
+_HEADS: dict = {}
+_APPENDS: dict = {}
+_PAGED: dict = {}
+
+
+def _keep(known: dict, key, value):
+    if len(known) >= 256:
+        known.clear()
+    known[key] = value
+    return value
+
+
+def _qk_call(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor):
+    """(B, N, H, Hkv, D, q's and k's token strides, dtype code) of a head norm's inputs."""
+    key = (q.shape, k.shape, q.stride(), k.stride(), q.dtype)
+    call = _HEADS.get(key)
+    if call is None:
+        if q.device.type != "cuda":
+            raise RuntimeError("the head norms run on the GPU only; q must be a device tensor")
+        if q.dim() != 4 or k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
+            raise ValueError("q and k must be [B, N, H, D] and [B, N, Hkv, D]")
+        B, N, H, D = q.shape
+        call = _keep(_HEADS, key, (B, N, H, k.shape[2], D, _token_stride("q", q, 2, q.dtype, q.device),
+                                   _token_stride("k", k, 2, q.dtype, k.device), _dtype_code(q.dtype), (D,)))
+    dev, dt = q.get_device(), q.dtype
+    if dev < 0:
         raise RuntimeError("the head norms run on the GPU only; q must be a device tensor")
-    if q.dim() != 4 or k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
-        raise ValueError("q and k must be [B, N, H, D] and [B, N, Hkv, D]")
-    B, N, H, D = q.shape
-    _check_like("q_weight", q_weight, (D,), q.dtype, q.device)
-    _check_like("k_weight", k_weight, (D,), q.dtype, q.device)
-    qs, ks = _token_stride("q", q, 2, q.dtype, q.device), _token_stride("k", k, 2, q.dtype, q.device)
-    return B, N, H, k.shape[2], D, qs, ks
+    if k.dtype != dt or k.get_device() != dev:
+        raise ValueError(f"k must be a {dt} tensor on {q.device}")
+    if q_weight.shape != call[8] or k_weight.shape != call[8] or q_weight.dtype != dt or k_weight.dtype != dt \
+            or q_weight.get_device() != dev or k_weight.get_device() != dev \
+            or not q_weight.is_contiguous() or not k_weight.is_contiguous():
+        raise ValueError(f"q_weight and k_weight must be contiguous {dt} tensors of shape {call[8]} on {q.device}")
+    return call
 
 
 def qk_norm_xpos(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor,
@@ -436,14 +462,14 @@ def qk_norm_xpos(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_wei
     N // 2), in one pass.  The heads of a token are contiguous and the tokens
     evenly spaced.  Returns new contiguous (q_out, k_out).  Enqueued on `stream`."""
     lib = _lib.load()
-    B, N, H, Hkv, D, qs, ks = _qk_shapes(q, k, q_weight, k_weight)
+    B, N, H, Hkv, D, qs, ks, dcode, _ = _qk_call(q, k, q_weight, k_weight)
     qo = torch.empty((B, N, H, D), dtype=q.dtype, device=q.device)
     ko = torch.empty((B, N, Hkv, D), dtype=q.dtype, device=q.device)
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
     rc = lib.dilated_attn_qk_norm_xpos(q.data_ptr(), k.data_ptr(), q_weight.data_ptr(), k_weight.data_ptr(),
                                        qo.data_ptr(), ko.data_ptr(), B, N, H, Hkv, D, qs, ks, float(eps),
                                        N // 2 if center is None else int(center), float(base), float(gamma),
-                                       float(scale_base), _dtype_code(q.dtype), raw)
+                                       float(scale_base), dcode, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, [qo, ko])
@@ -458,9 +484,9 @@ def qk_norm_xpos_bwd(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor
     and the contiguous gradients of its outputs; the float32 workspace comes
     from torch's caching allocator."""
     lib = _lib.load()
-    B, N, H, Hkv, D, qs, ks = _qk_shapes(q, k, q_weight, k_weight)
-    _check_like("dq_out", dq_out, (B, N, H, D), q.dtype, q.device)
-    _check_like("dk_out", dk_out, (B, N, Hkv, D), q.dtype, q.device)
+    B, N, H, Hkv, D, qs, ks, dcode, _ = _qk_call(q, k, q_weight, k_weight)
+    _check_like("dq_out", dq_out, q.shape, q.dtype, q.device)
+    _check_like("dk_out", dk_out, k.shape, q.dtype, q.device)
     need = _workspace_bytes("dilated_attn_qk_norm_xpos_bwd_workspace", B, N, D)
     dq, dk = torch.empty_like(dq_out), torch.empty_like(dk_out)
     dqw, dkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
@@ -469,33 +495,41 @@ def qk_norm_xpos_bwd(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor
     rc = lib.dilated_attn_qk_norm_xpos_bwd(
         dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), q_weight.data_ptr(), k_weight.data_ptr(),
         dq.data_ptr(), dk.data_ptr(), dqw.data_ptr(), dkw.data_ptr(), B, N, H, Hkv, D, qs, ks, float(eps),
-        N // 2 if center is None else int(center), float(base), float(gamma), float(scale_base),
-        _dtype_code(q.dtype), ws.data_ptr(), need, raw)
+        N // 2 if center is None else int(center), float(base), float(gamma), float(scale_base), dcode,
+        ws.data_ptr(), need, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, [dq, dk, dqw, dkw, ws])
     return dq, dk, dqw, dkw
 
 
-def _paged_cache(q_dtype, device, D: int, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
-                 seq_lens: torch.Tensor, q_start: torch.Tensor):
-    """The da_paged_cache_t of a call, its sequence count and key heads."""
+def _cache_shape(k_cache: torch.Tensor, block_table: torch.Tensor, D: int):
+    """(B, Hkv, num_pages, page_size, max_pages) of a cache and its table."""
     if k_cache.dim() != 4:
         raise ValueError("k_cache and v_cache must be [num_pages, Hkv, page_size, D]")
     pages, Hkv, page, Dc = k_cache.shape
     if Dc != D:
         raise ValueError(f"k_cache holds heads of {Dc}, the call has heads of {D}")
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _check_like(name, t, k_cache.shape, q_dtype, device)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages]")
     B, max_pages = block_table.shape
-    _check_like("block_table", block_table, (B, max_pages), torch.int32, device)
-    _check_like("seq_lens", seq_lens, (B,), torch.int32, device)
-    _check_like("q_start", q_start, (B + 1,), torch.int32, device)
-    args = _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-                               q_start.data_ptr(), pages, page, max_pages)
-    return args, B, Hkv
+    return B, Hkv, pages, page, max_pages
+
+
+def _check_cache(dev: int, dtype, B: int, k_cache, v_cache, block_table, seq_lens, q_start):
+    """Refuse cache tensors of another type, device, shape or layout than the call's."""
+    i32 = torch.int32
+    if dev < 0 or k_cache.get_device() != dev or v_cache.get_device() != dev or block_table.get_device() != dev \
+            or seq_lens.get_device() != dev or q_start.get_device() != dev:
+        raise ValueError("the cache, block_table, seq_lens and q_start must be on the tokens' device")
+    if k_cache.dtype != dtype or v_cache.dtype != dtype or v_cache.shape != k_cache.shape \
+            or not k_cache.is_contiguous() or not v_cache.is_contiguous():
+        raise ValueError(f"k_cache and v_cache must be contiguous {dtype} tensors of one shape")
+    if block_table.dtype != i32 or seq_lens.dtype != i32 or q_start.dtype != i32 \
+            or seq_lens.shape != (B,) or q_start.shape != (B + 1,) or not block_table.is_contiguous() \
+            or not seq_lens.is_contiguous() or not q_start.is_contiguous():
+        raise ValueError(f"block_table, seq_lens and q_start must be contiguous int32 tensors of shapes "
+                         f"[{B}, max_pages], [{B}] and [{B + 1}]")
 
 
 def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
@@ -514,33 +548,51 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
     v_cache [num_pages, Hkv, page_size, D], page_size a power of two.  `center`
     is the xPos centre, the same for the life of a cache.  Enqueued on `stream`."""
     lib = _lib.load()
-    if k.device.type != "cuda":
+    key = (None if q is None else (q.shape, q.stride()), k.shape, k.stride(), v.shape, v.stride(), k.dtype,
+           k_cache.shape, block_table.shape)
+    call = _APPENDS.get(key)
+    if call is None:
+        if k.device.type != "cuda":
+            raise RuntimeError("cache_append runs on the GPU only; k must be a device tensor")
+        if k.dim() != 3 or v.shape != k.shape:
+            raise ValueError("k and v must be [T, Hkv, D]")
+        T, Hkv, D = k.shape
+        ks, vs = _token_stride("k", k, 1, k.dtype, k.device), _token_stride("v", v, 1, v.dtype, v.device)
+        B, cached, pages, page, max_pages = _cache_shape(k_cache, block_table, D)
+        if cached != Hkv:
+            raise ValueError(f"the cache has {cached} key heads, k has {Hkv}")
+        H, qs = Hkv, Hkv * D
+        if q is not None:
+            if q.dim() != 3 or q.shape[0] != T or q.shape[2] != D:
+                raise ValueError("q must be [T, H, D] for the tokens of k")
+            H, qs = q.shape[1], _token_stride("q", q, 1, q.dtype, q.device)
+        call = _keep(_APPENDS, key, (T, B, H, Hkv, D, qs, ks, vs, _dtype_code(k.dtype), pages, page, max_pages))
+    T, B, H, Hkv, D, qs, ks, vs, dcode, pages, page, max_pages = call
+    dev, dt = k.get_device(), k.dtype
+    if dev < 0:
         raise RuntimeError("cache_append runs on the GPU only; k must be a device tensor")
-    if k.dim() != 3 or v.shape != k.shape:
-        raise ValueError("k and v must be [T, Hkv, D]")
-    T, Hkv, D = k.shape
-    ks, vs = _token_stride("k", k, 1, k.dtype, k.device), _token_stride("v", v, 1, k.dtype, k.device)
-    cache, B, cached_heads = _paged_cache(k.dtype, k.device, D, k_cache, v_cache, block_table, seq_lens, q_start)
-    if cached_heads != Hkv:
-        raise ValueError(f"the cache has {cached_heads} key heads, k has {Hkv}")
-    H, qs, qo = Hkv, Hkv * D, None
+    _check_cache(dev, dt, B, k_cache, v_cache, block_table, seq_lens, q_start)
+    if v.dtype != dt or v.get_device() != dev:
+        raise ValueError(f"v must be a {dt} tensor on {k.device}")
+    qo = None
     if q is not None:
-        qs = _token_stride("q", q, 1, k.dtype, k.device)
-        H = q.shape[1]
-        if q.shape != (T, H, D):
-            raise ValueError("q must be [T, H, D] for the tokens of k")
-        qo = torch.empty((T, H, D), dtype=k.dtype, device=k.device)
+        if q.dtype != dt or q.get_device() != dev:
+            raise ValueError(f"q must be a {dt} tensor on {k.device}")
+        qo = torch.empty((T, H, D), dtype=dt, device=k.device)
     elif q_weight is not None:
         raise ValueError("q_weight without q")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _check_like(name, w, (D,), k.dtype, k.device)
+    if q_weight is not None:
+        _check_like("q_weight", q_weight, (D,), dt, k.device)
+    if k_weight is not None:
+        _check_like("k_weight", k_weight, (D,), dt, k.device)
+    cache = _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                                q_start.data_ptr(), pages, page, max_pages)
     raw = _raw_stream(k.device) if stream is None else stream.cuda_stream
     rc = lib.dilated_attn_cache_append(
         None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
         None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-        None if qo is None else qo.data_ptr(), ctypes.byref(cache), T, B, H, Hkv, D, qs, ks, vs, float(eps),
-        int(bool(rotate)), int(center), float(base), float(gamma), float(scale_base), _dtype_code(k.dtype), raw)
+        None if qo is None else qo.data_ptr(), cache, T, B, H, Hkv, D, qs, ks, vs, float(eps),
+        1 if rotate else 0, int(center), float(base), float(gamma), float(scale_base), dcode, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     if qo is not None:
@@ -575,15 +627,29 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
     Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor of
     at least paged_workspace_bytes."""
     lib = _lib.load()
-    if q.device.type != "cuda":
+    patterns = tuple(patterns)
+    shapes = (q.shape, q.stride(), q.dtype, k_cache.shape, block_table.shape, max_new)
+    try:
+        call = _PAGED.get((shapes, patterns))
+    except TypeError:  # patterns given as lists
+        call = None
+    if call is None:
+        if q.device.type != "cuda":
+            raise RuntimeError("paged_attn runs on the GPU only; q must be a device tensor")
+        if q.dim() != 3:
+            raise ValueError("q must be [T, H, D]")
+        T, H, D = q.shape
+        B, Hkv, pages, page, max_pages = _cache_shape(k_cache, block_table, D)
+        dcode, pats = _dtype_code(q.dtype), _pattern_key(patterns)
+        new = T if max_new is None else int(max_new)
+        need = _paged_workspace((T, B, H, Hkv, D, pages, page, max_pages, new), pats, dcode)
+        call = _keep(_PAGED, (shapes, pats), (T, B, H, Hkv, D, _token_stride("q", q, 1, q.dtype, q.device), dcode, pages,
+                                              page, max_pages, new, max(need, 16), *_pattern_array_cached(pats)))
+    T, B, H, Hkv, D, qs, dcode, pages, page, max_pages, new, need, arr, n = call
+    dev = q.get_device()
+    if dev < 0:
         raise RuntimeError("paged_attn runs on the GPU only; q must be a device tensor")
-    qs = _token_stride("q", q, 1, q.dtype, q.device)
-    T, H, D = q.shape
-    cache, B, Hkv = _paged_cache(q.dtype, q.device, D, k_cache, v_cache, block_table, seq_lens, q_start)
-    dcode = _dtype_code(q.dtype)
-    pats = _pattern_key(patterns)
-    new = T if max_new is None else int(max_new)
-    need = _paged_workspace((T, B, H, Hkv, D, cache.num_pages, cache.page_size, cache.max_pages, new), pats, dcode)
+    _check_cache(dev, q.dtype, B, k_cache, v_cache, block_table, seq_lens, q_start)
     owned = []
     if out is None:
         out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
@@ -596,15 +662,17 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
     else:
         _check_like("lse", lse, (H, T), torch.float32, q.device)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        workspace, nbytes = torch.empty(need, dtype=torch.uint8, device=q.device), need
         owned.append(workspace)
-    elif workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
-    arr, n = _pattern_array_cached(pats)
+    else:
+        if workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
+        nbytes = workspace.numel()
+    cache = _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                                q_start.data_ptr(), pages, page, max_pages)
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
-    rc = lib.dilated_attn_paged_fwd(q.data_ptr(), ctypes.byref(cache), out.data_ptr(), lse.data_ptr(), T, B, H, Hkv,
-                                    D, qs, new, arr, n, dcode, float(scale or 0.0), workspace.data_ptr(),
-                                    workspace.numel(), raw)
+    rc = lib.dilated_attn_paged_fwd(q.data_ptr(), cache, out.data_ptr(), lse.data_ptr(), T, B, H, Hkv, D, qs, new, arr,
+                                    n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, owned)
