@@ -141,14 +141,14 @@ int dilated_attn_cache_append(const void* q, const void* k, const void* v, const
  * max_new     the most new tokens of any sequence, as far as the caller knows,
  *             or T: it only helps to choose the launches (a launch for
  *             sequences with many new tokens is left out where none has more
- *             than 8), results are right whatever it says.
+ *             than 4), results are right whatever it says.
  * patterns, softmax_scale: as for dilated_attn_fwd.
  * workspace   device scratch of at least the bytes that
  *             dilated_attn_paged_workspace reports for the same sizes.
  *
  * DA_BF16: scores as exact products summed in float32; probabilities rounded
  * to bf16 for the product with v, summed in float32; a sequence's tokens by
- * themselves (at most 8 new ones) mix float32 partial rows, otherwise a
+ * themselves (at most 4 new ones) mix float32 partial rows, otherwise a
  * pattern's rows are kept as in dilated_attn_fwd; out rounded once.  DA_F32
  * computes in float32 throughout.  Results are finite under the conditions of
  * dilated_attn_fwd for the sequence's own tokens; what lies in the pool beyond

@@ -33,7 +33,7 @@ namespace {
 
 constexpr int kPgThreads = 256;
 constexpr int kPgWaves = kPgThreads / 64;
-constexpr float kLowest = -1.0e30f;  // finite "minus infinity" of a running maximum
+constexpr float kLowest = -3.402823466e38f;  // a running maximum of no score: the lowest finite value
 constexpr float kSlack = 8.0f;       // a score this far above its row's reference (log2) moves it
 
 struct PagedArgs {
@@ -46,7 +46,7 @@ struct PagedArgs {
   int64_t qs;  // elements between tokens of q
   int64_t one_rec, one_row, tile_rec, tile_row;  // byte offsets in the workspace
   int32_t T, B, H, Hkv, G, npat, num_pages, max_pages, page_log2;
-  int32_t by_token, few, singles, one_slots, tile_items, one_items, join_groups;
+  int32_t few, singles, one_slots, one_items, tile_items, grid, join_groups;
   uint32_t reach;     // positions the table holds
   FastDiv fheads;     // division by H
   float scale_log2;
@@ -54,9 +54,9 @@ struct PagedArgs {
   // longest such segment), or -1, and its segment length.
   int32_t full, full_w;
   FastDiv full_fw;
-  // Where each pattern's workgroups begin, beyond all others' for
-  // patterns that are not there: found without a loop over the records.
-  int32_t one_begin[DA_MAX_PATTERNS], item_begin[DA_MAX_PATTERNS];
+  // Where each pattern's workgroups begin, beyond all others' for patterns that
+  // are not there: found without a loop over the records.
+  int32_t one_begin[DA_MAX_PATTERNS], tile_begin[DA_MAX_PATTERNS];
   PagedPattern pat[DA_MAX_PATTERNS];
 };
 
@@ -150,25 +150,60 @@ __device__ inline int position_of(const PagedArgs& a, const Sequence& sq, int to
   return sq.b >= 0 && tok < sq.end && p >= 0 && p < a.reach ? static_cast<int>(p) : -1;
 }
 
-// A listed token: its row of q, its sequence and position.  False: not there,
-// not in the cache, or computed in tiles.
+// Entry i of start, held to the call's tokens: what a tile reads and writes stays in bounds.
+__device__ inline int token_row(const PagedArgs& a, int i) { return max(0, min(a.start[i], a.T)); }
+
+// This thread's number, opaque to the compiler: in the loop over a workgroup's
+// items what follows from it would otherwise be formed before the loop and held
+// in registers over all of it (which then spill).
+__device__ inline int thread_id() {
+  int tid = __builtin_amdgcn_workitem_id_x();
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
+// Running sum over the wave's lanes.
+__device__ inline int running_sum(int v, int lane) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int o = __shfl_up(v, s, 64);
+    if (lane >= s) v += o;
+  }
+  return v;
+}
+
+// A listed token: its row of q, its sequence and position.  kMixed: number e of
+// those in sequences of at most a.few new tokens; otherwise row e of the call.
+// False: not there, or not in the table.
 struct Token {
   int tok, b, pos;
 };
+template <bool kMixed>
 __device__ inline bool single_token(const PagedArgs& a, int e, int lane, Token& t) {
-  Sequence sq[1];
-  if (a.by_token) {
+  Sequence sq[1] = {Sequence{-1, 0, 0, 0}};
+  if constexpr (!kMixed) {
     const int tok[1] = {e};
     t.tok = e;
     find_sequences(a, tok, lane, sq);
   } else {
-    const int b = e / a.few;
-    sq[0] = Sequence{b, a.start[b], a.start[b + 1], a.lens[b]};
-    t.tok = sq[0].begin + (e - b * a.few);
+    t.tok = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      const int b = min(b0 + lane, a.B - 1), begin = token_row(a, b), end = token_row(a, b + 1), len = a.lens[b];
+      const int n = b0 + lane < a.B && end - begin <= a.few ? max(end - begin, 0) : 0;
+      const int upto = running_sum(n, lane), total = __builtin_amdgcn_readlane(upto, 63);
+      if (e < total) {
+        const int l = __builtin_ctzll(__ballot(upto > e));
+        sq[0] = Sequence{b0 + l, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(end, l),
+                         __builtin_amdgcn_readlane(len, l)};
+        t.tok = sq[0].end - (__builtin_amdgcn_readlane(upto, l) - e);
+        break;
+      }
+      e -= total;
+    }
   }
   t.b = sq[0].b;
   t.pos = position_of(a, sq[0], t.tok);
-  return t.pos >= 0 && t.tok >= 0 && t.tok < a.T && static_cast<int64_t>(sq[0].end) - sq[0].begin <= a.few;
+  return t.pos >= 0;
 }
 
 // The heads of key head hk's group that pattern P keeps at segment-local
@@ -214,32 +249,28 @@ __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
 
-// A workgroup's place among the single tokens' items, pattern by pattern: unit
-// u = (token e, number of its block of heads) runs with all its splits on XCD u
-// mod 8 (dealt out split by split over the XCDs, the 472 MB of 8 sequences with
-// heads of 128 took 105 us instead of 90).
+// A workgroup's place among a pattern's items for single tokens: unit u = (token
+// e, number of its block of heads) runs with all its splits on XCD u mod 8
+// (dealt out split by split over the XCDs, the 472 MB of 8 sequences with heads
+// of 128 took 105 us instead of 90).  False: past the tokens' end.
 struct OneItem {
   int pi, split, e, head;
 };
-__device__ inline bool one_item(const PagedArgs& a, int idx, OneItem& it) {
-  if (idx >= a.one_items) return false;
-  it.pi = pattern_at(a.one_begin, idx);
-  const PagedPattern& P = a.pat[it.pi];
-  const int local = idx - P.one_begin;
+__device__ inline bool one_item(const PagedArgs& a, int pi, int local, int tokens, OneItem& it) {
+  const PagedPattern& P = a.pat[pi];
   const int j = local >> 3, block8 = P.one_split.div(j);
   const int unit = block8 * 8 + (local & 7);
+  it.pi = pi;
   it.split = j - block8 * P.one_split.d;
   it.e = P.one_heads.div(unit);
   it.head = unit - it.e * P.one_heads.d;
-  return it.e < a.singles;
+  return it.e < tokens;
 }
 
-// A wave's 32-key tile on its way: two blocks of 16 keys as operands, and V's
-// rows as they come.
+// A wave's 32 keys of K on their way: two blocks of 16 as operands.
 template <int D>
-struct KeyTile {
+struct KeyFrag {
   u32x4 k[2][D / 32];
-  u32x4 v[D / 16];
 };
 
 constexpr int kOneTile = 32;    // keys of a wave's tile
@@ -252,8 +283,8 @@ struct SmemOne {
   uint32_t row[kOneRows];  // cache rows of the split's keys, a chunk at a time
 };
 
-template <int D>
-__device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm) {
+template <int D, bool kMixed>
+__device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, SmemOne<D>& sm) {
   constexpr int KC = D / 32, DB = D / 16, kTile = kOneTile;
   using TL = TileLayout<D>;
   constexpr int kVLoads = kTile * TL::kSlots / 64;
@@ -263,14 +294,12 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
   auto& sv = sm.v;
   auto& sml = sm.ml;
 
-  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
+  const int tid = thread_id(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  OneItem it;
-  if (!one_item(a, idx, it)) return;
   const int pi = it.pi;
   const PagedPattern& P = a.pat[pi];
   Token tk;
-  if (!single_token(a, it.e, lane, tk)) return;
+  if (!single_token<kMixed>(a, it.e, lane, tk)) return;
   const Lattice lat = lattice_of(P, tk.pos);
   // Dilations of a group's size and above keep one head of a group at most: the
   // head-th kept one; below, every group has some, in blocks.
@@ -319,16 +348,19 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
   const int vrow = lane / TL::kSlots;
   char* my = sv[wv];
   // Requests the 32 keys from `key` on (counted within the chunk whose rows are in LDS).
-  auto request = [&](int key, KeyTile<D>& kt) {
+  auto request_k = [&](int key, KeyFrag<D>& kf) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const char* p = a.kc + (static_cast<int64_t>(sm.row[key + 16 * u + m]) * TL::kRowBytes + 16 * grp);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) kt.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+      for (int c = 0; c < KC; ++c) kf.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
     }
+  };
+  u32x4 vreg[kVLoads];
+  auto request_v = [&](int key) {
 #pragma unroll
     for (int i = 0; i < kVLoads; ++i)
-      kt.v[i] = *reinterpret_cast<const u32x4*>(
+      vreg[i] = *reinterpret_cast<const u32x4*>(
           a.vc + (static_cast<int64_t>(sm.row[key + kVStep * i + vrow]) * TL::kRowBytes + (lane % TL::kSlots) * 16));
   };
   // V^T operand: lane's d = 16 db + (lane & 15), keys 4 grp + 0..3 and 16 more.
@@ -343,15 +375,15 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
 
-  // first: the tile's first key (t)
-  auto compute = [&](int first, const KeyTile<D>& kt) {
+  // first: the tile's first key (t); next: the next tile's, within the chunk, < 0: none
+  auto compute = [&](int first, const KeyFrag<D>& kf, int next) {
     f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       const bf16x8 qf = __builtin_bit_cast(bf16x8, sm.q[c][lane]);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt.k[u][c]), qf, s[u], 0, 0, 0);
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf.k[u][c]), qf, s[u], 0, 0, 0);
     }
     const int left = ke - first - 4 * grp;  // keys from this lane's first on
 #pragma unroll
@@ -401,7 +433,8 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
     // of a wave complete in order: no wait between).
 #pragma unroll
     for (int i = 0; i < kVLoads; ++i)
-      *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, lane % TL::kSlots)) = kt.v[i];
+      *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, lane % TL::kSlots)) = vreg[i];
+    if (next >= 0) request_v(next);
     const uint32_t va = lds_addr(my);
     constexpr int kHalf = DB < 4 ? DB : 4;  // blocks whose V is read at once
 #pragma unroll
@@ -434,25 +467,28 @@ __device__ inline void single_tokens(const PagedArgs& a, int idx, SmemOne<D>& sm
     }
     __syncthreads();
     if (wv >= ntile) continue;
-    // While a tile is computed the next one's loads are under way.  A wave's
-    // last tile is a branch of its own, so that at every use of a tile it is
-    // known which loads are younger.
-    KeyTile<D> ta, tb;
-    request(wv * kTile, ta);
+    // While a tile is computed the next one's loads are under way, K's from its
+    // start, V's from where its own V has left the registers.  A wave's last tile
+    // is a branch of its own, so that at every use of K it is known which loads
+    // are younger.
+    KeyFrag<D> ka, kb;
+    request_k(wv * kTile, ka);
+    request_v(wv * kTile);
     for (int tile = wv;;) {
+      const int next = (tile + kPgWaves) * kTile;
       if (tile + kPgWaves >= ntile) {
-        compute(c0 + tile * kTile, ta);
+        compute(c0 + tile * kTile, ka, -1);
         break;
       }
-      request((tile + kPgWaves) * kTile, tb);
-      compute(c0 + tile * kTile, ta);
+      request_k(next, kb);
+      compute(c0 + tile * kTile, ka, next);
       tile += kPgWaves;
       if (tile + kPgWaves >= ntile) {
-        compute(c0 + tile * kTile, tb);
+        compute(c0 + tile * kTile, kb, -1);
         break;
       }
-      request((tile + kPgWaves) * kTile, ta);
-      compute(c0 + tile * kTile, tb);
+      request_k(next + kPgWaves * kTile, ka);
+      compute(c0 + tile * kTile, kb, next + kPgWaves * kTile);
       tile += kPgWaves;
     }
   }
@@ -497,12 +533,13 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
   __shared__ __attribute__((aligned(16))) float so[kGroups][D];
   __shared__ float sml[2][kGroups];
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
-  OneItem it;
-  if (!one_item(a, launch_index(), it)) return;
-  const int pi = it.pi;
+  const int idx = launch_index();
+  if (idx >= a.one_items) return;
+  const int pi = pattern_at(a.one_begin, idx);
   const PagedPattern& P = a.pat[pi];
+  OneItem it;
   Token tk;
-  if (!single_token(a, it.e, lane, tk)) return;
+  if (!one_item(a, pi, idx - P.one_begin, a.singles, it) || !single_token<false>(a, it.e, lane, tk)) return;
   const Lattice lat = lattice_of(P, tk.pos);
   const int64_t kept = lat.rho + static_cast<int64_t>(it.head) * P.r;
   if (kept >= a.H) return;
@@ -592,50 +629,49 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
 // ---------------------------------------------------------------------------
 // Tiles of query rows
 // ---------------------------------------------------------------------------
-// Entry i of start, held to the call's tokens: what a tile reads and writes stays in bounds.
-__device__ inline int token_row(const PagedArgs& a, int i) { return max(0, min(a.start[i], a.T)); }
-
-// The query tile `tile` of pattern P among all sequences' (for any head: a
-// head's offset only moves the rows within a tile).
+// The new tokens of sequences computed in tiles, sequence b0 + lane: positions
+// [c0, c1), empty for the others.
+struct Chunk {
+  int c0, c1;
+};
+__device__ inline Chunk chunk_of(const PagedArgs& a, int b0, int lane) {
+  const int b = min(b0 + lane, a.B - 1);
+  const int n = token_row(a, b + 1) - token_row(a, b), len = a.lens[b];
+  const int c1 = max(0, static_cast<int>(min(static_cast<uint32_t>(max(len, 0)), a.reach)));
+  const int c0 = max(0, static_cast<int>(min(static_cast<int64_t>(len) - n, static_cast<int64_t>(c1))));
+  return b0 + lane < a.B && n > a.few ? Chunk{c0, c1} : Chunk{0, 0};
+}
+// Query tiles of pattern P over `len` >= 1 positions of a segment, and over a
+// sequence's new tokens, segment by segment (for any head: its offset only
+// moves the rows within a tile).
+__device__ inline int tiles_of(const PagedPattern& P, int len) {
+  return static_cast<int>(P.fr.div(len - 1)) / static_cast<int>(kPagedRows) + 1;
+}
+__device__ inline int tiles_of(const PagedPattern& P, const Chunk& c) {
+  if (c.c1 <= c.c0) return 0;
+  const int g0 = P.fw.div(c.c0), g1 = P.fw.div(c.c1 - 1);
+  return g0 == g1 ? tiles_of(P, c.c1 - c.c0)
+                  : tiles_of(P, (g0 + 1) * P.w - c.c0) + (g1 - g0 - 1) * tiles_of(P, P.w) + tiles_of(P, c.c1 - g1 * P.w);
+}
+// Tile `tile` of pattern P among all sequences'.
 struct QueryTile {
   int b, g, j;  // sequence, segment, tile of the segment's new rows
-  int c0, c1;   // positions of the sequence's new tokens
+  Chunk c;
 };
 __device__ inline bool query_tile(const PagedArgs& a, const PagedPattern& P, int tile, int lane, QueryTile& qt) {
-  constexpr int BM = kPagedRows;
-  auto tiles_of = [&](int len) { return static_cast<int>(P.fr.div(len - 1)) / BM + 1; };  // len >= 1
   for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    int cnt = 0, c0 = 0, c1 = 0;
-    if (b < a.B) {
-      const int64_t n = token_row(a, b + 1) - token_row(a, b);
-      const int64_t len = a.lens[b];
-      c1 = static_cast<int>(max(int64_t{0}, min(len, static_cast<int64_t>(a.reach))));
-      c0 = static_cast<int>(max(int64_t{0}, min(len - n, static_cast<int64_t>(c1))));
-      if (n > a.few && c1 > c0) {
-        const int g0 = P.fw.div(c0), g1 = P.fw.div(c1 - 1);
-        cnt = g0 == g1 ? tiles_of(c1 - c0)
-                       : tiles_of((g0 + 1) * P.w - c0) + (g1 - g0 - 1) * tiles_of(P.w) + tiles_of(c1 - g1 * P.w);
-      }
-    }
-    int upto = cnt;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int o = __shfl_up(upto, s, 64);
-      if (lane >= s) upto += o;
-    }
-    const int total = __shfl(upto, 63, 64);
+    const Chunk c = chunk_of(a, b0, lane);
+    const int cnt = tiles_of(P, c), upto = running_sum(cnt, lane), total = __builtin_amdgcn_readlane(upto, 63);
     if (tile < total) {
       const int l = __builtin_ctzll(__ballot(upto > tile));
       qt.b = b0 + l;
-      int j = tile - (__shfl(upto, l, 64) - __shfl(cnt, l, 64));
-      qt.c0 = __shfl(c0, l, 64);
-      qt.c1 = __shfl(c1, l, 64);
-      qt.g = P.fw.div(qt.c0);
-      const int g1 = P.fw.div(qt.c1 - 1);
-      const int first = qt.g == g1 ? 0x7fffffff : tiles_of((qt.g + 1) * P.w - qt.c0);
+      qt.c = Chunk{__builtin_amdgcn_readlane(c.c0, l), __builtin_amdgcn_readlane(c.c1, l)};
+      int j = tile - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(cnt, l));
+      qt.g = P.fw.div(qt.c.c0);
+      const int g1 = P.fw.div(qt.c.c1 - 1);
+      const int first = qt.g == g1 ? 0x7fffffff : tiles_of(P, (qt.g + 1) * P.w - qt.c.c0);
       if (j >= first) {
-        const int per = tiles_of(P.w);
+        const int per = tiles_of(P, P.w);
         j -= first;
         const int skip = min(j / per, g1 - qt.g - 1);
         qt.g += 1 + skip;
@@ -649,6 +685,11 @@ __device__ inline bool query_tile(const PagedArgs& a, const PagedPattern& P, int
   return false;
 }
 
+// A workgroup's place among a pattern's items for tiles.
+struct TileItem {
+  int pi, tile, head, split;
+};
+
 constexpr int kTileRows = 4096;  // keys whose rows are looked up at once (three workgroups of D = 64 fit a CU)
 
 template <int D>
@@ -659,32 +700,21 @@ struct SmemTile {
 };
 
 template <int D>
-__device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm) {
+__device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemTile<D>& sm) {
   constexpr int BM = kPagedRows, BN = kPagedKeyTile;
   constexpr int KC = D / 16, DB = D / 32;
   using TL = TileLayout<D>;
   constexpr int kLoads = BN * TL::kSlots / 64 / kPgWaves;
-  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
+  const int tid = thread_id(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const PagedPattern& P = a.pat[pattern_at(a.item_begin, idx)];
-  // Unit u = (run of tiles, head) runs on XCD u mod 8, whose L2 then serves the
-  // run's keys after their first fetch; later (longer) tiles first.
-  const int local = idx - P.item_begin;
-  const int k8 = local >> 3, unit8 = P.tile_unit.div(k8);
-  const int within = k8 - unit8 * P.tile_unit.d, unit = unit8 * 8 + (local & 7);
-  const int run = a.fheads.div(unit), head = unit - run * a.H;
-  const int in_run = P.tile_split.div(within), sp = within - in_run * P.tile_split.d;
-  const int ti = run * P.unit_tiles + in_run;
-  if (ti >= P.tiles) return;
+  const PagedPattern& P = a.pat[it.pi];
+  const int head = it.head, sp = it.split;
   QueryTile qt;
-  if (!query_tile(a, P, P.tiles - 1 - ti, lane, qt)) return;
-  qt.b = __builtin_amdgcn_readfirstlane(qt.b);
-  qt.g = __builtin_amdgcn_readfirstlane(qt.g);
-  qt.j = __builtin_amdgcn_readfirstlane(qt.j);
+  if (!query_tile(a, P, it.tile, lane, qt)) return;
   const int gs = qt.g * P.w;
   const int off = head - static_cast<int>(P.fr.div(head)) * P.r;
-  const int lo = max(__builtin_amdgcn_readfirstlane(qt.c0) - gs, 0);
-  const int hi_pos = min(__builtin_amdgcn_readfirstlane(qt.c1) - gs, P.w);
+  const int lo = max(qt.c.c0 - gs, 0);
+  const int hi_pos = min(qt.c.c1 - gs, P.w);
   auto first_at = [&](int x) { return x > off ? static_cast<int>(P.fr.div(x - off - 1)) + 1 : 0; };  // first t at or after x
   const int q0 = first_at(lo) + qt.j * BM;
   const int qend = min(q0 + BM, first_at(hi_pos));
@@ -894,22 +924,109 @@ __device__ inline void query_tiles(const PagedArgs& a, int idx, SmemTile<D>& sm)
   }
 }
 
-// One launch for both: the tiles first, as they take longer.
-template <int D, bool kTiles>
-__global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_attn(PagedArgs a) {
+// Where item `local` of a pattern with `tiles` query tiles per head stands, in
+// units of `run` tiles of one head with their splits: unit u runs on XCD u mod
+// 8, whose L2 then serves the run's keys after their first fetch; later (longer)
+// tiles first.  False: padding.
+__device__ inline bool tile_item(const PagedArgs& a, int pi, int local, int tiles, int run, int splits, TileItem& it) {
+  const int j = local >> 3, per = run * splits, unit8 = j / per, within = j - unit8 * per;
+  const int u = unit8 * 8 + (local & 7), r = a.fheads.div(u), in_run = within / splits;
+  it = TileItem{pi, tiles - 1 - (r * run + in_run), u - r * a.H, within - in_run * splits};
+  return it.tile >= 0;
+}
+
+// Every token a single one.
+template <int D>
+__global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_singles(PagedArgs a) {
+  __shared__ SmemOne<D> sm;
   touch(a);
   const int idx = launch_index();
-  if constexpr (kTiles) {
-    union Smem {
-      SmemTile<D> tile;
-      SmemOne<D> one;
-    };
-    __shared__ Smem sm;
-    if (idx < a.tile_items) query_tiles<D>(a, idx, sm.tile);
-    else single_tokens<D>(a, idx - a.tile_items, sm.one);
-  } else {
-    __shared__ SmemOne<D> sm;
-    single_tokens<D>(a, idx, sm);
+  if (idx >= a.one_items) return;
+  const int pi = pattern_at(a.one_begin, idx);
+  OneItem it;
+  if (one_item(a, pi, idx - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, false>(a, it, sm);
+}
+
+template <int D>
+union SmemMixed {
+  SmemTile<D> tile;
+  SmemOne<D> one;
+  int count[DA_MAX_PATTERNS + 1];
+};
+
+// Tiles and single tokens in one launch, the tiles first, as they take longer:
+// every item that the sizes allow.
+template <int D>
+__global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_mixed(PagedArgs a) {
+  __shared__ SmemMixed<D> sm;
+  touch(a);
+  const int idx = launch_index();
+  if (idx < a.tile_items) {
+    const int pi = pattern_at(a.tile_begin, idx);
+    const PagedPattern& P = a.pat[pi];
+    TileItem it;
+    if (tile_item(a, pi, idx - P.tile_begin, P.tiles, P.run, P.tile_split.d, it)) query_tiles<D>(a, it, sm.tile);
+  } else if (idx - a.tile_items < a.one_items) {
+    const int pi = pattern_at(a.one_begin, idx - a.tile_items);
+    OneItem it;
+    if (one_item(a, pi, idx - a.tile_items - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, true>(a, it, sm.one);
+  }
+}
+
+// The same in a launch as large as the sizes let expect: how many tiles and
+// single tokens there are is known on the device only, so every workgroup counts
+// them (a pattern per wave in turn, then per lane) and takes those items that
+// are its index plus a multiple of the launch.  16 sequences with 1015 new
+// tokens, 1000 of them one sequence's, have 840 items where their sizes allow
+// 8200 (64 -> 49 us); 64 sequences with one of 2048 259 -> 99 us.  Counted again
+// for each item: held in registers over an item the counts would spill, and most
+// workgroups have one.  (The loop takes more registers than paged_mixed.)
+template <int D>
+__global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps(PagedArgs a) {
+  __shared__ SmemMixed<D> sm;
+  touch(a);
+  const int idx = launch_index();
+  for (int item = idx, items = idx + 1; item < items; item += a.grid) {
+    const int tid = thread_id(), lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int i = wv; i <= a.npat; i += kPgWaves) {  // the last: single tokens
+      int cnt = 0;
+      for (int b0 = 0; b0 < a.B; b0 += 64) {
+        if (i < a.npat) {
+          cnt += tiles_of(a.pat[i], chunk_of(a, b0, lane));
+        } else if (b0 + lane < a.B) {
+          const int n = token_row(a, b0 + lane + 1) - token_row(a, b0 + lane);
+          cnt += n <= a.few ? max(n, 0) : 0;
+        }
+      }
+      const int all = running_sum(cnt, lane);
+      if (lane == 63) sm.count[i] = all;
+    }
+    __syncthreads();
+    // Lane i: pattern i's tiles, the tiles of a unit (see the plan), its items.
+    const int pat = min(lane, a.npat - 1), tiles = sm.count[pat], tokens = sm.count[a.npat];
+    const PagedPattern P = a.pat[pat];
+    const int splits = P.tile_split.d, run = max(1, min(16, static_cast<int>(static_cast<int64_t>(tiles) * a.H / 64)));
+    const int units = ((tiles + run - 1) / run * a.H + 7) & ~7;
+    const int singles = ((tokens * static_cast<int>(P.one_heads.d) + 7) & ~7) * P.one_split.d;
+    const int mine = lane < a.npat ? units * run * splits : 0, ones = lane < a.npat ? singles : 0;
+    const int tile_end = running_sum(mine, lane), one_end = running_sum(ones, lane);
+    const int tile_items = __builtin_amdgcn_readlane(tile_end, 63);
+    items = tile_items + __builtin_amdgcn_readlane(one_end, 63);
+    __syncthreads();  // the counts are read
+    if (item < tile_items) {
+      const int pi = __builtin_ctzll(__ballot(tile_end > item));
+      const int begin = __builtin_amdgcn_readlane(tile_end, pi) - __builtin_amdgcn_readlane(mine, pi);
+      TileItem it;
+      if (tile_item(a, pi, item - begin, __builtin_amdgcn_readlane(tiles, pi), __builtin_amdgcn_readlane(run, pi),
+                    __builtin_amdgcn_readlane(splits, pi), it))
+        query_tiles<D>(a, it, sm.tile);
+    } else if (item < items) {
+      const int pi = __builtin_ctzll(__ballot(one_end > item - tile_items));
+      const int begin = tile_items + __builtin_amdgcn_readlane(one_end, pi) - __builtin_amdgcn_readlane(ones, pi);
+      OneItem it;
+      if (one_item(a, pi, item - begin, tokens, it)) single_tokens<D, true>(a, it, sm.one);
+    }
+    __syncthreads();  // the item is done with its LDS
   }
 }
 
@@ -930,7 +1047,8 @@ __device__ inline void put8(float* p, const f32x8& v) { *reinterpret_cast<f32x8*
 struct Mix {
   float m = -INFINITY, l = 0.0f;
   f32x8 acc = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
-  __device__ void add(float x, float scale, const f32x8& o) {  // row o * scale with weight 2^x > 0
+  __device__ void add(float x, float scale, const f32x8& o) {  // row o * scale with weight 2^x
+    if (x == -INFINITY) return;  // no visible key, or none with a finite score: the row is not there
     const float mn = fmaxf(m, x);
     const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(x - mn);
     m = mn;
@@ -948,7 +1066,7 @@ __device__ inline void put_row(const PagedArgs& a, int tok, int head, int ch, co
 
 // Single tokens: a wave per row (or a workgroup, kTogether), D/8 lanes across a
 // partial and as many partials at a time as fit: a row has tens of them.
-template <typename T, int D, bool kTogether>
+template <typename T, int D, bool kMixed, bool kTogether>
 __device__ inline void join_singles(const PagedArgs& a, int group) {
   constexpr int kLanes = D / 8, kSubs = 64 / kLanes;
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
@@ -958,8 +1076,8 @@ __device__ inline void join_singles(const PagedArgs& a, int group) {
   const int e = a.fheads.div(row), head = row - e * a.H;
   if (e >= a.singles) return;
   Token tk;
-  const bool there = single_token(a, e, lane, tk);
-  if (!there && a.few < a.T) return;  // not this launch part's (see join_tiles)
+  const bool there = single_token<kMixed>(a, e, lane, tk);
+  if (kMixed && !there) return;  // a row of join_tiles, if of any
   // How many partials each pattern has of the row, a pattern per lane, and
   // their running sum: partial c is slot first + c of the pattern with upto > c.
   static_assert(DA_MAX_PATTERNS == 16, "a pattern per lane");
@@ -1017,7 +1135,7 @@ __device__ inline void join_singles(const PagedArgs& a, int group) {
 #pragma unroll
     for (int w = 1; w < kPgWaves; ++w) meet(ml[w][0], ml[w][1], [&](int i) { return rows[w][ch * 8 + i]; });
   }
-  if (sub == 0) put_row<T, D>(a, a.by_token ? e : tk.tok, head, ch, x);
+  if (sub == 0) put_row<T, D>(a, tk.tok, head, ch, x);
 }
 
 // Tokens of tiles, and those of no sequence: D/8 lanes a row, head by head and
@@ -1073,7 +1191,7 @@ __device__ inline void join_tiles(const PagedArgs& a, int group) {
       }
 #pragma unroll
       for (int i = 0; i < kPats; ++i) {
-        if (rec[i][0] == -INFINITY) continue;  // a split without a visible key: its row holds nothing
+        if (rec[i][0] == -INFINITY) continue;
         f32x8 f;
 #pragma unroll
         for (int c = 0; c < 8; ++c) f[c] = static_cast<float>(o[i][c]);
@@ -1088,7 +1206,7 @@ __device__ inline void join_tiles(const PagedArgs& a, int group) {
 template <typename T, int D, bool kTogether>
 __global__ __launch_bounds__(kPgThreads) void paged_join(PagedArgs a) {
   touch(a);
-  join_singles<T, D, kTogether>(a, launch_index());
+  join_singles<T, D, false, kTogether>(a, launch_index());
 }
 // The rows of tiles first, then the single tokens'.
 template <int D, int kPats>
@@ -1096,7 +1214,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_join_all(PagedArgs a) {
   touch(a);
   const int group = launch_index();
   if (group < a.join_groups) join_tiles<D, kPats>(a, group);
-  else join_singles<u16, D, false>(a, group - a.join_groups);
+  else join_singles<u16, D, true, false>(a, group - a.join_groups);
 }
 
 // Rows of single tokens: a workgroup each below this many (tens of partials
@@ -1112,16 +1230,17 @@ void launch_join(int64_t rows, const PagedArgs& a, hipStream_t stream) {
 
 template <int D>
 void launch_all(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
-  const dim3 threads(kPgThreads), grid = grid_of(p.tile_items + p.one_items);
+  const dim3 threads(kPgThreads), grid = grid_of(p.grid);
   const int64_t singles = p.singles * p.H;
   if (p.dtype == DA_F32) {
     hipLaunchKernelGGL(paged_one_f32<D>, grid, threads, 0, stream, a);
     launch_join<float, D>(singles, a, stream);
   } else if (p.all_few) {
-    hipLaunchKernelGGL((paged_attn<D, false>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL(paged_singles<D>, grid, threads, 0, stream, a);
     launch_join<u16, D>(singles, a, stream);
   } else {
-    hipLaunchKernelGGL((paged_attn<D, true>), grid, threads, 0, stream, a);
+    if (p.steps) hipLaunchKernelGGL(paged_mixed_steps<D>, grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL(paged_mixed<D>, grid, threads, 0, stream, a);
     constexpr int kRows = kPgThreads / (D / 8);
     a.join_groups = static_cast<int32_t>((p.T * p.H + kRows - 1) / kRows);
     const dim3 join = grid_of(a.join_groups + (singles + kPgWaves - 1) / kPgWaves);
@@ -1158,9 +1277,9 @@ hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, con
   a.num_pages = static_cast<int32_t>(p.num_pages);
   a.max_pages = static_cast<int32_t>(p.max_pages);
   a.page_log2 = p.page_log2;
-  a.by_token = p.by_token;
   a.few = static_cast<int32_t>(p.few);
   a.tile_items = static_cast<int32_t>(p.tile_items);
+  a.grid = static_cast<int32_t>(p.grid);
   a.one_slots = static_cast<int32_t>(p.one_slots);
   a.reach = static_cast<uint32_t>(p.max_pages * p.page);
   a.one_items = static_cast<int32_t>(p.one_items);
@@ -1175,7 +1294,7 @@ hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, con
   }
   for (int i = 0; i < DA_MAX_PATTERNS; ++i) {
     a.one_begin[i] = i < p.npat ? p.pat[i].one_begin : 0x7fffffff;
-    a.item_begin[i] = i < p.npat ? p.pat[i].item_begin : 0x7fffffff;
+    a.tile_begin[i] = i < p.npat ? p.pat[i].tile_begin : 0x7fffffff;
   }
   if (p.D == 32) launch_all<32>(p, a, stream);
   else if (p.D == 64) launch_all<64>(p, a, stream);

@@ -210,8 +210,7 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   const int64_t reach = max_pages * page;  // positions that the table holds
   p.all_few = dtype == DA_F32 || std::min(max_new, T) <= kPagedFew;
   p.few = p.all_few ? T : B == 1 ? 0 : kPagedFew;
-  p.by_token = p.all_few || T <= B * p.few;
-  p.singles = p.by_token ? T : B * p.few;
+  p.singles = std::min(T, p.all_few ? T : B * p.few);
   // A single token's workgroups for one split: key heads with a kept query head,
   // in blocks of kPagedGroupRows query heads (float32: query heads).  A token
   // belongs to the heads of one residue mod r.
@@ -226,7 +225,7 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     one_busy += static_cast<double>(p.singles) * one_heads(patterns[i].r);
     tile_busy += H * std::ceil(double(T) / patterns[i].r / kPagedRows);
   }
-  int64_t one_items = 0;
+  int64_t one_items = 0, expected = 0;
   int64_t items = 0;
   for (int i = 0; i < p.npat; ++i) {
     PagedPattern& t = p.pat[i];
@@ -253,22 +252,26 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     t.tile_slot = static_cast<int32_t>(p.tile_slots);
     p.tile_slots += ts;
     // A sequence of n tokens touches at most n / w + 2 segments, each with one
-    // tile more than its rows fill.
+    // tile more than its rows fill.  Units are dealt to the XCDs: up to 16 tiles,
+    // fewer where there would not be eight units each.
     const int64_t tiles = std::min(T, T / (int64_t{t.r} * kPagedRows) + T / t.w + 2 * B + 2);
-    // Units are dealt to the XCDs: up to 16 tiles, fewer where there would not
-    // be eight units each.
-    const int64_t unit = std::max<int64_t>(1, std::min<int64_t>(16, tiles * H / 64));
-    const int64_t units = ((tiles + unit - 1) / unit * H + 7) / 8 * 8;
-    if (items + units * unit * ts >= kMost) return DA_EINVAL;
-    t.tile_unit = make_fastdiv(static_cast<uint32_t>(unit * ts));
-    t.unit_tiles = static_cast<int32_t>(unit);
+    if (tiles >= kMost / H / ts) return DA_EINVAL;
+    const int64_t run = std::max<int64_t>(1, std::min<int64_t>(16, tiles * H / 64));
+    if (items >= kMost) return DA_EINVAL;
     t.tiles = static_cast<int32_t>(tiles);
-    t.item_begin = static_cast<int32_t>(items);
-    items += units * unit * ts;
+    t.run = static_cast<int32_t>(run);
+    t.tile_begin = static_cast<int32_t>(items);
+    items += ((tiles + run - 1) / run * H + 7) / 8 * 8 * run * ts;
+    expected += (T / (int64_t{t.r} * kPagedRows) + 2) * H * ts + std::min(T, B) * one_heads(patterns[i].r) * one;
   }
-  p.tile_items = items;
+  if (one_items >= kMost || one_items + items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
   p.one_items = one_items;
-  if (p.one_items + p.tile_items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
+  p.tile_items = items;
+  // Where the sizes allow many more items than they let expect, the launch is
+  // as large as the latter.
+  const int64_t likely = std::max<int64_t>(1024, expected);
+  p.steps = !p.all_few && 2 * (one_items + items) > 3 * likely;
+  p.grid = p.steps ? (likely + 7) / 8 * 8 : one_items + items;
   uint64_t off = 0;
   auto take = [&off](uint64_t bytes) {
     const uint64_t at = off;

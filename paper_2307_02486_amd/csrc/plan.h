@@ -112,10 +112,12 @@ int make_plan(int64_t B, int64_t N, int64_t H, int64_t D, const da_pattern_t* pa
 // Attention over a paged cache.  A sequence's new tokens are computed in one of
 // two ways: each token by itself (all its keys' splits in parallel), or in
 // tiles of kept query rows.  A sequence of at most kPagedFew new tokens takes
-// the first, unless it is the call's only one.  Both write one partial row per
-// (token, head) and slot, a slot being one split of one pattern's keys, and the
-// join reads them.
-constexpr int64_t kPagedFew = 8;
+// the first, unless it is the call's only one.  (64 sequences of 500 to 8000
+// tokens, the paper's patterns, 12 heads of 64: 4 tokens each by themselves 131
+// us, 8 tokens 225, in tiles 9 tokens 175; 4 sequences at 31500: 8 tokens 46 us,
+// 16 in tiles 37.)  Both write one partial row per (token, head) and slot, a
+// slot being one split of one pattern's keys, and the join reads them.
+constexpr int64_t kPagedFew = 4;
 constexpr int64_t kPagedRows = 128;      // query rows of a tile
 constexpr int64_t kPagedKeyTile = 64;    // its keys at a time
 constexpr int64_t kPagedGroupRows = 16;  // query heads of one key head that a token's workgroup holds
@@ -128,11 +130,9 @@ struct PagedPattern {
   int32_t one_begin;         // its first workgroup among the single tokens'
   FastDiv one_heads;         // division by a token's workgroups for one split
   FastDiv tile_split;        // division by the splits of a tile's keys
-  FastDiv tile_unit;         // division by the workgroups of a unit: tiles of one head next to each other, with their splits
-  int32_t unit_tiles;        // a unit's tiles
   int32_t tile_slot;         // its first slot there
-  int32_t tiles;             // bound on the pattern's query tiles per head
-  int32_t item_begin;        // its first workgroup among the tiles'
+  int32_t tiles, run;        // bound on its query tiles per head; tiles of a unit (next to each other, of one head)
+  int32_t tile_begin;        // its first workgroup among the tiles'
 };
 
 struct PagedPlan {
@@ -140,12 +140,13 @@ struct PagedPlan {
   int dtype, page_log2, npat;
   float scale;
   bool all_few;              // every token by itself
-  bool by_token;             // single tokens are listed by token, else as (sequence, token < few)
   int full;                  // the pattern with r = 1 and the longest segment, or -1
   int64_t few;               // new tokens up to which a sequence's are computed by themselves
-  int64_t singles;           // tokens listed for the first way
+  int64_t singles;           // tokens computed by themselves, at most
   int64_t one_slots, tile_slots;
-  int64_t one_items, tile_items;  // workgroups
+  int64_t one_items, tile_items;  // workgroups of the single tokens and of the tiles, at most
+  int64_t grid;              // of the launch
+  bool steps;                // its workgroups step through the items that there are
   uint64_t one_rec_off, one_row_off, tile_rec_off, tile_row_off, workspace_bytes;
   PagedPattern pat[DA_MAX_PATTERNS];
 };

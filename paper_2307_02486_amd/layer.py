@@ -8,6 +8,11 @@ the standard attention replaced by dilated attention).
     a  = dilated attention of q, k, v               (dilated_attn_fwd / _bwd)
     y  = out_proj(LN_sub(a as [B, N, E]))           (Magneto's sub-LayerNorm)
 
+With qk_norm the heads of q and k are RMS-normed before xPos, in the same pass
+(dilated_attn_qk_norm_xpos).  `step` is the layer for serving: new tokens of
+several sequences against a paged cache (dilated_attn_cache_append,
+dilated_attn_paged_fwd).
+
 The residual connection belongs to the block around the layer.  The
 attention and xPos run in the library's HIP kernels (their backward passes
 too), and so do, in bf16, the LayerNorms (dilated_attn_layernorm_fwd / _bwd)
@@ -23,7 +28,8 @@ from typing import Sequence, Tuple
 import torch
 from torch.autograd import forward_ad
 
-from .ops import dilated_attn, dilated_attn_bwd, layer_norm, layer_norm_bwd, wgrad, xpos
+from .ops import (cache_append, dilated_attn, dilated_attn_bwd, layer_norm, layer_norm_bwd, paged_attn, qk_norm_xpos,
+                  qk_norm_xpos_bwd, wgrad, xpos)
 
 
 def _plain() -> bool:
@@ -68,6 +74,21 @@ class XPosFunction(torch.autograd.Function):
     def backward(ctx, dy):
         sign, center, base, gamma, scale_base = ctx.args
         return xpos(dy.contiguous(), sign, True, center, base, gamma, scale_base), None, None, None, None, None
+
+
+class QKNormXPosFunction(torch.autograd.Function):
+    """Differentiable RMS norm of the heads of q and k and xPos, in one pass each way."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, eps, center, base, gamma, scale_base):
+        q, k = q.contiguous(), k.contiguous()
+        ctx.save_for_backward(q, k, q_weight, k_weight)
+        ctx.args = (eps, center, base, gamma, scale_base)
+        return qk_norm_xpos(q, k, q_weight, k_weight, *ctx.args)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        return (*qk_norm_xpos_bwd(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, *ctx.args), *(None,) * 5)
 
 
 def _weight_grads(dy2: torch.Tensor, x2: torch.Tensor):
@@ -165,15 +186,19 @@ class LongNetAttention(torch.nn.Module):
     patterns is the list of (segment length w, dilation r).  xPos uses
     rotation base `xpos_base`, gamma `xpos_gamma`, scale base
     `xpos_scale_base` and the sequence's middle position as its centre.
+    qk_norm (with xPos only) adds the RMS norms of the query and key heads,
+    weights [head_dim] each, eps `qk_eps`.
     """
 
     def __init__(self, embed_dim: int, num_heads: int, patterns: Sequence[Tuple[int, int]],
                  causal: bool = True, use_xpos: bool = True, xpos_base: float = 10000.0,
                  xpos_gamma: float = 0.4, xpos_scale_base: float = 512.0, eps: float = 1e-5,
-                 device=None, dtype=torch.bfloat16):
+                 device=None, dtype=torch.bfloat16, qk_norm: bool = False, qk_eps: float = 1e-6):
         super().__init__()
         if embed_dim % num_heads:
             raise ValueError("embed_dim must be a multiple of num_heads")
+        if qk_norm and not use_xpos:
+            raise ValueError("qk_norm goes with xPos (use_xpos=True)")
         self.embed_dim, self.num_heads = embed_dim, num_heads
         self.head_dim = embed_dim // num_heads
         self.patterns, self.causal = list(patterns), causal
@@ -186,6 +211,11 @@ class LongNetAttention(torch.nn.Module):
         self.v_proj = torch.nn.Linear(embed_dim, embed_dim, **kw)
         self.ln_sub = torch.nn.LayerNorm(embed_dim, eps=eps, **kw)
         self.out_proj = torch.nn.Linear(embed_dim, embed_dim, **kw)
+        self.qk_norm, self.qk_eps = qk_norm, qk_eps
+        self.q_norm = self.k_norm = None
+        if qk_norm:
+            self.q_norm = torch.nn.Parameter(torch.ones(self.head_dim, **kw))
+            self.k_norm = torch.nn.Parameter(torch.ones(self.head_dim, **kw))
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         B, N, E = x.shape
@@ -195,25 +225,51 @@ class LongNetAttention(torch.nn.Module):
         if _plain():
             q, k, v = (_linear(m, u).view(B, N, H, D) for m in projs)
             q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
-            if self.use_xpos:  # in place: q and k are the projections' own outputs
+            if self.qk_norm:
+                q, k = qk_norm_xpos(q, k, self.q_norm, self.k_norm, self.qk_eps, N // 2, *self.xpos_args)
+            elif self.use_xpos:  # in place: q and k are the projections' own outputs
                 q = xpos(q, 1, False, N // 2, *self.xpos_args, out=q)
                 k = xpos(k, -1, False, N // 2, *self.xpos_args, out=k)
             a = dilated_attn(q, k, v, self.patterns, self.causal)[0]
             return _linear(self.out_proj, _layer_norm(self.ln_sub, a.view(B, N, E)))
         q, k, v = (y.view(B, N, H, D) for y in QKVFunction.apply(u, *(p for m in projs for p in (m.weight, m.bias))))
-        if self.use_xpos:
+        if self.qk_norm:
+            q, k = QKNormXPosFunction.apply(q, k, self.q_norm, self.k_norm, self.qk_eps, N // 2, *self.xpos_args)
+        elif self.use_xpos:
             base, gamma, scale_base = self.xpos_args
             q = XPosFunction.apply(q, 1, N // 2, base, gamma, scale_base)
             k = XPosFunction.apply(k, -1, N // 2, base, gamma, scale_base)
         a = DilatedAttentionFunction.apply(q, k, v, self.patterns, self.causal, None)
         return _linear(self.out_proj, _layer_norm(self.ln_sub, a.reshape(B, N, E)))
 
+    @torch.no_grad()
+    def step(self, x: torch.Tensor, cache, batch, layer: int = 0) -> torch.Tensor:
+        """The layer on new tokens x [T, E] of the sequences of `batch`, whose
+        keys and values go to `cache` (a PagedCache and one of its batches, for
+        the cache's layer `layer`) and which attend to what is there of their
+        own sequence: what forward gives on whole sequences, row by row (up to
+        rounding: xPos is centred on the cache's centre).  Causal layers only,
+        without gradients."""
+        if not self.causal:
+            raise ValueError("step needs a causal layer: cached tokens do not see later ones")
+        T, H, D = x.shape[0], self.num_heads, self.head_dim
+        u = _layer_norm(self.ln_in, x)
+        q, k, v = (_linear(m, u).view(T, H, D) for m in (self.q_proj, self.k_proj, self.v_proj))
+        where = (cache.k[layer], cache.v[layer], batch.block_table, batch.seq_lens, batch.q_start)
+        q = cache_append(q, k, v, *where, self.q_norm, self.k_norm, self.qk_eps, self.use_xpos, cache.center,
+                         *self.xpos_args)
+        a = paged_attn(q, *where, self.patterns, max_new=batch.max_new)[0]
+        return _linear(self.out_proj, _layer_norm(self.ln_sub, a.view(T, H * D)))
+
     def float64_params(self) -> dict:
         """The parameters as float64 NumPy arrays, keyed ln_in_g, ln_in_b, wq,
-        bq, wk, bk, wv, bv, ln_sub_g, ln_sub_b, wo, bo."""
+        bq, wk, bk, wv, bv, ln_sub_g, ln_sub_b, wo, bo, and q_norm, k_norm where
+        the heads are normed."""
         p = {"ln_in_g": self.ln_in.weight, "ln_in_b": self.ln_in.bias,
              "wq": self.q_proj.weight, "bq": self.q_proj.bias, "wk": self.k_proj.weight, "bk": self.k_proj.bias,
              "wv": self.v_proj.weight, "bv": self.v_proj.bias,
              "ln_sub_g": self.ln_sub.weight, "ln_sub_b": self.ln_sub.bias,
              "wo": self.out_proj.weight, "bo": self.out_proj.bias}
+        if self.qk_norm:
+            p.update(q_norm=self.q_norm, k_norm=self.k_norm)
         return {kk: vv.detach().to("cpu", torch.float64).numpy() for kk, vv in p.items()}

@@ -622,7 +622,7 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
     dilated_attn gives on its sequence.  H is a multiple of the cache's heads.
 
     max_new, the most new tokens of any sequence if the caller knows it,
-    spares the launches for long ones where it is at most 8.  Returns (out
+    spares what only longer ones need where it is at most 4.  Returns (out
     [T, H, D], lse [H, T] float32); a token of no sequence has zeros and -inf.
     Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor of
     at least paged_workspace_bytes."""

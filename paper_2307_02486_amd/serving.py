@@ -1,0 +1,78 @@
+"""A paged cache of keys and values for LongNetAttention.step: pools of pages on
+the GPU for every layer, one page table for all of them, kept on the host."""
+from __future__ import annotations
+
+from typing import NamedTuple, Sequence
+
+import torch
+
+
+class Batch(NamedTuple):
+    """The sequences of one step, as cache_append and paged_attn take them:
+    int32 device tensors [B, max_pages], [B] and [B + 1], and the most new
+    tokens of a sequence."""
+    block_table: torch.Tensor
+    seq_lens: torch.Tensor
+    q_start: torch.Tensor
+    max_new: int
+
+
+class PagedCache:
+    """Pages of page_size tokens (a power of two) for `layers` attention layers.
+
+    k and v are lists with a tensor [num_pages, num_heads, page_size, head_dim]
+    per layer; page p of every layer belongs to the same sequence.  A sequence
+    holds at most max_pages pages.  `center` is the xPos centre of every
+    position (the middle of the reach by default), fixed for the cache's life.
+    """
+
+    def __init__(self, num_pages: int, page_size: int, max_pages: int, num_heads: int, head_dim: int,
+                 layers: int = 1, center: int | None = None, device=None, dtype=torch.bfloat16):
+        if page_size < 1 or page_size & (page_size - 1):
+            raise ValueError("page_size must be a power of two")
+        if num_pages < 1 or max_pages < 1 or layers < 1:
+            raise ValueError("num_pages, max_pages and layers must be at least 1")
+        shape = (num_pages, num_heads, page_size, head_dim)
+        self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
+        self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
+        self.page_size, self.max_pages = page_size, max_pages
+        self.center = max_pages * page_size // 2 if center is None else center
+        self.device = self.k[0].device
+        self._free = list(range(num_pages - 1, -1, -1))
+        self._pages: dict = {}
+        self._length: dict = {}
+
+    def length(self, sequence) -> int:
+        """Tokens that the cache holds of a sequence (any hashable name)."""
+        return self._length.get(sequence, 0)
+
+    def release(self, sequence):
+        """Forget a sequence; its pages go back to the pool."""
+        self._free += self._pages.pop(sequence, [])
+        self._length.pop(sequence, None)
+
+    def extend(self, sequences: Sequence, new: Sequence[int]) -> Batch:
+        """Room for `new` more tokens of each sequence (named for the first time,
+        it is empty), and the batch of a step in which they come.  Every layer
+        then takes this batch once."""
+        if len(set(sequences)) != len(sequences) or len(new) != len(sequences) or not len(new):
+            raise ValueError("sequences must be different ones, with a number of new tokens each")
+        if min(new) < 0:
+            raise ValueError("the numbers of new tokens must not be negative")
+        lengths = [self.length(s) + n for s, n in zip(sequences, new)]
+        need = [-(-n // self.page_size) for n in lengths]
+        short = [n - len(self._pages.get(s, ())) for s, n in zip(sequences, need)]
+        if max(need) > self.max_pages:
+            raise ValueError(f"a sequence of {max(lengths)} tokens is beyond {self.max_pages} pages of {self.page_size}")
+        if sum(short) > len(self._free):
+            raise RuntimeError(f"{sum(short)} pages are needed and {len(self._free)} are free")
+        table = torch.zeros((len(need), self.max_pages), dtype=torch.int32)
+        for i, (s, n, more) in enumerate(zip(sequences, lengths, short)):
+            pages = self._pages.setdefault(s, [])
+            pages += [self._free.pop() for _ in range(more)]
+            self._length[s] = n
+            table[i, : len(pages)] = torch.tensor(pages, dtype=torch.int32)
+        start = torch.zeros(len(need) + 1, dtype=torch.int32)
+        start[1:] = torch.tensor(new, dtype=torch.int32).cumsum(0)
+        lens = torch.tensor(lengths, dtype=torch.int32)
+        return Batch(table.to(self.device), lens.to(self.device), start.to(self.device), max(new))
