@@ -34,6 +34,7 @@ namespace {
 constexpr int kPgThreads = 256;
 constexpr int kPgWaves = kPgThreads / 64;
 constexpr float kLowest = -3.402823466e38f;  // a running maximum of no score: the lowest finite value
+constexpr float kSumSlack = 1024.0f;  // a half row's sum above it moves its reference (tiles)
 constexpr float kSlack = 8.0f;       // a score this far above its row's reference (log2) moves it
 
 struct PagedArgs {
@@ -162,14 +163,19 @@ __device__ inline int thread_id() {
   return tid;
 }
 
-// Running sum over the wave's lanes.
-__device__ inline int running_sum(int v, int lane) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int o = __shfl_up(v, s, 64);
-    if (lane >= s) v += o;
-  }
-  return v;
+// Running sum over the wave's lanes: within rows of 16 lanes by shifts on the
+// vector ALU, then the rows' last sums into the rows after them.
+template <int kCtrl, int kRows>
+__device__ inline int add_shifted(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, false);
+}
+__device__ inline int running_sum(int v) {
+  v = add_shifted<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v = add_shifted<0x112, 0xf>(v);
+  v = add_shifted<0x114, 0xf>(v);
+  v = add_shifted<0x118, 0xf>(v);
+  v = add_shifted<0x142, 0xa>(v);  // row_bcast 15 into rows 1 and 3
+  return add_shifted<0x143, 0xc>(v);  // row_bcast 31 into rows 2 and 3
 }
 
 // A listed token: its row of q, its sequence and position.  kMixed: number e of
@@ -190,7 +196,7 @@ __device__ inline bool single_token(const PagedArgs& a, int e, int lane, Token& 
     for (int b0 = 0; b0 < a.B; b0 += 64) {
       const int b = min(b0 + lane, a.B - 1), begin = token_row(a, b), end = token_row(a, b + 1), len = a.lens[b];
       const int n = b0 + lane < a.B && end - begin <= a.few ? max(end - begin, 0) : 0;
-      const int upto = running_sum(n, lane), total = __builtin_amdgcn_readlane(upto, 63);
+      const int upto = running_sum(n), total = __builtin_amdgcn_readlane(upto, 63);
       if (e < total) {
         const int l = __builtin_ctzll(__ballot(upto > e));
         sq[0] = Sequence{b0 + l, __builtin_amdgcn_readlane(begin, l), __builtin_amdgcn_readlane(end, l),
@@ -220,14 +226,30 @@ __device__ inline KeptHeads kept_heads(const PagedPattern& P, int hk, int G, int
 }
 
 // The table's entry for position pos of a sequence, and key head hk's row of the
-// cache there.  They are two steps so that the entry can be on its way while
-// earlier tiles are: taken together, the wait for the entry would be one for
-// the tile requested before it.  A page outside the pool reads the pool's last
-// page: in bounds, whatever the table holds.
+// cache there.  A page outside the pool reads the pool's last page: in bounds,
+// whatever the table holds.
 __device__ inline int table_entry(const PagedArgs& a, const int32_t* table, int pos) { return table[pos >> a.page_log2]; }
 __device__ inline uint32_t cache_row(const PagedArgs& a, int entry, int hk, int pos) {
   const uint32_t page = min(static_cast<uint32_t>(entry), static_cast<uint32_t>(a.num_pages - 1));
   return ((page * a.Hkv + hk) << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
+}
+// The cache rows of keys first .. first + n - 1 (positions base + t r) into row,
+// by a workgroup; keys past `last` are that one.  kAtOnce entries of a thread
+// are on their way together.
+template <int kAtOnce>
+__device__ inline void look_up_rows(const PagedArgs& a, const int32_t* table, int hk, int base, int r, int first,
+                                    int last, int n, int tid, uint32_t* row) {
+  for (int i0 = tid; i0 < n; i0 += kAtOnce * kPgThreads) {
+    int pos[kAtOnce], entry[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      pos[u] = base + min(first + i0 + u * kPgThreads, last) * r;
+      entry[u] = table_entry(a, table, pos[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+      if (i0 + u * kPgThreads < n) row[i0 + u * kPgThreads] = cache_row(a, entry[u], hk, pos[u]);
+  }
 }
 
 // Keys of split s of n keys: [first, end), whole 32-key tiles but the last.
@@ -460,11 +482,7 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
   for (int c0 = k0; c0 < ke; c0 += kOneRows) {
     const int keys = min(ke - c0, kOneRows), ntile = (keys + kTile - 1) / kTile;
     if (c0 > k0) __syncthreads();  // every wave is done with the rows before
-    // Rows past the split's end, up to a whole tile, are its last.
-    for (int i = tid; i < ntile * kTile; i += kPgThreads) {
-      const int pos = base + min(c0 + i, ke - 1) * P.r;
-      sm.row[i] = cache_row(a, table_entry(a, table, pos), hk, pos);
-    }
+    look_up_rows<4>(a, table, hk, base, P.r, c0, ke - 1, ntile * kTile, tid, sm.row);
     __syncthreads();
     if (wv >= ntile) continue;
     // While a tile is computed the next one's loads are under way, K's from its
@@ -659,30 +677,32 @@ struct QueryTile {
   Chunk c;
 };
 __device__ inline bool query_tile(const PagedArgs& a, const PagedPattern& P, int tile, int lane, QueryTile& qt) {
+  qt.b = -1;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     const Chunk c = chunk_of(a, b0, lane);
-    const int cnt = tiles_of(P, c), upto = running_sum(cnt, lane), total = __builtin_amdgcn_readlane(upto, 63);
+    const int cnt = tiles_of(P, c), upto = running_sum(cnt), total = __builtin_amdgcn_readlane(upto, 63);
     if (tile < total) {
       const int l = __builtin_ctzll(__ballot(upto > tile));
       qt.b = b0 + l;
       qt.c = Chunk{__builtin_amdgcn_readlane(c.c0, l), __builtin_amdgcn_readlane(c.c1, l)};
-      int j = tile - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(cnt, l));
-      qt.g = P.fw.div(qt.c.c0);
-      const int g1 = P.fw.div(qt.c.c1 - 1);
-      const int first = qt.g == g1 ? 0x7fffffff : tiles_of(P, (qt.g + 1) * P.w - qt.c.c0);
-      if (j >= first) {
-        const int per = tiles_of(P, P.w);
-        j -= first;
-        const int skip = min(j / per, g1 - qt.g - 1);
-        qt.g += 1 + skip;
-        j -= skip * per;
-      }
-      qt.j = j;
-      return true;
+      tile -= __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(cnt, l);
+      break;
     }
     tile -= total;
   }
-  return false;
+  if (qt.b < 0) return false;
+  qt.j = tile;
+  qt.g = P.fw.div(qt.c.c0);
+  const int g1 = P.fw.div(qt.c.c1 - 1);
+  const int first = qt.g == g1 ? 0x7fffffff : tiles_of(P, (qt.g + 1) * P.w - qt.c.c0);
+  if (qt.j >= first) {
+    const int per = tiles_of(P, P.w);
+    qt.j -= first;
+    const int skip = min(qt.j / per, g1 - qt.g - 1);
+    qt.g += 1 + skip;
+    qt.j -= skip * per;
+  }
+  return true;
 }
 
 // A workgroup's place among a pattern's items for tiles.
@@ -784,10 +804,7 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
   const float c2 = a.scale_log2;
   for (int c0 = kb; c0 < ke; c0 += kTileRows) {
   const int ntile = (min(ke - c0, kTileRows) + BN - 1) / BN;
-  for (int i = tid; i < ntile * BN; i += kPgThreads) {  // past the split's end: its last key
-    const int pos = base + min(c0 + i, ke - 1) * P.r;
-    sm.row[i] = cache_row(a, table_entry(a, table, pos), hk, pos);
-  }
+  look_up_rows<8>(a, table, hk, base, P.r, c0, ke - 1, ntile * BN, tid, sm.row);
   __syncthreads();
   load_tile(0, 0);
   wait_loads<0>();
@@ -827,14 +844,34 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
           for (int j = 0; j < 16; ++j)
             if (first + x * 32 + 8 * (j >> 2) + (j & 3) > 0) acc_s[x][j] = -INFINITY;
       }
-      float mx = acc_s[0][0];
+      // P = 2^(c S - m) for the reference m of the row so far, without looking
+      // for the tile's maximum: a tile whose probabilities of half a row sum to
+      // more than kSumSlack (or overflow: the first tile's do) has its scores
+      // still in registers and forms them again with its maximum as reference.
+      // Probabilities above 1 are held by bf16 and float32 as well as those below.
+      bf16x8 pb[2][2];
+      float lt;
+      auto probabilities = [&] {
+        const float negm = -m_run;
+        float lp[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) mx = fmaxf(mx, fmaxf(acc_s[x][j], acc_s[x][j + 1]));
-      mx *= c2;
-      if (__any(mx > m_run + kSlack)) {
-        const float m_new = fmaxf(m_run, fmaxf(mx, other_half(mx)));
+          for (int j = 0; j < 16; ++j) {
+            const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(acc_s[x][j], c2, negm));
+            lp[j & 3] += pe;
+            pb[x][j >> 3][j & 7] = (__bf16)pe;
+          }
+        lt = (lp[0] + lp[1]) + (lp[2] + lp[3]);
+      };
+      probabilities();
+      if (__any(!(lt <= kSumSlack))) {
+        float mx = acc_s[0][0];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) mx = fmaxf(mx, fmaxf(acc_s[x][j], acc_s[x][j + 1]));
+        const float m_new = fmaxf(m_run, fmaxf(mx, other_half(mx)) * c2);
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
         l_run *= alpha;
@@ -842,9 +879,9 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int j = 0; j < 16; ++j) acc_o[db][j] *= alpha;
+        probabilities();
       }
-      const float negm = -m_run;
-      float lp[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      l_run += lt;
       const uint32_t vaddr = lds_addr(vl);
       static_for<0, 2>([&](auto KB) {
         constexpr int kb2 = decltype(KB)::value;
@@ -860,24 +897,16 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
         });
         static_for<0, 2>([&](auto KK) {
           constexpr int kk = decltype(KK)::value;
-          bf16x8 pb;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(acc_s[kb2][8 * kk + e], c2, negm));
-            lp[e & 3] += pe;
-            pb[e] = (__bf16)pe;
-          }
           lds_wait<(1 - kk) * 2 * DB>();
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
             lds_bind(vf[kk][db][0]);
             lds_bind(vf[kk][db][1]);
             const u32x4 a4 = {vf[kk][db][0][0], vf[kk][db][0][1], vf[kk][db][1][0], vf[kk][db][1][1]};
-            acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a4), pb, acc_o[db], 0, 0, 0);
+            acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a4), pb[kb2][kk], acc_o[db], 0, 0, 0);
           }
         });
       });
-      l_run += (lp[0] + lp[1]) + (lp[2] + lp[3]);
     }
     wait_loads<0>();
     __syncthreads();
@@ -998,7 +1027,7 @@ __global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps
           cnt += n <= a.few ? max(n, 0) : 0;
         }
       }
-      const int all = running_sum(cnt, lane);
+      const int all = running_sum(cnt);
       if (lane == 63) sm.count[i] = all;
     }
     __syncthreads();
@@ -1009,7 +1038,7 @@ __global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps
     const int units = ((tiles + run - 1) / run * a.H + 7) & ~7;
     const int singles = ((tokens * static_cast<int>(P.one_heads.d) + 7) & ~7) * P.one_split.d;
     const int mine = lane < a.npat ? units * run * splits : 0, ones = lane < a.npat ? singles : 0;
-    const int tile_end = running_sum(mine, lane), one_end = running_sum(ones, lane);
+    const int tile_end = running_sum(mine), one_end = running_sum(ones);
     const int tile_items = __builtin_amdgcn_readlane(tile_end, 63);
     items = tile_items + __builtin_amdgcn_readlane(one_end, 63);
     __syncthreads();  // the counts are read
