@@ -257,6 +257,7 @@ struct HeadBwdArgs {
   float* part;  // [workgroups][2][D]: partial sums of both weights' gradients
   int64_t qs, ks, T;
   int32_t H, Hkv, center;
+  int32_t groups;  // workgroups: the launch packet, where the device could read it, is in host memory
   float eps;
   FastDiv fn;
 };
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(kHeadThreads, sizeof(T) == 2 ? 4 : 3) void heads_bw
 
   // A step is kRows heads of a token; the next step's rows, of this token or
   // the wave's next one, are loaded while a step is computed.
-  const int64_t stride = static_cast<int64_t>(__builtin_amdgcn_grid_size_x() / kHeadThreads) * kHeadWaves;
+  const int64_t stride = static_cast<int64_t>(a.groups) * kHeadWaves;
   int64_t tok = static_cast<int64_t>(__builtin_amdgcn_workgroup_id_x()) * kHeadWaves + wv;
   Raw nx{}, ndy{};
   auto load = [&](int64_t t, int r0) {
@@ -467,6 +468,7 @@ hipError_t launch_qk_norm_bwd(const QkNormCall& c, const void* dqo, const void* 
   a.eps = c.eps;
   a.fn = make_fastdiv(static_cast<uint32_t>(c.N));
   const int nwg = static_cast<int>(qk_norm_groups(a.T));
+  a.groups = nwg;
   if (c.dtype == DA_BF16) launch_bwd<u16>(a, c.rot, dqw, dkw, static_cast<int>(c.D), nwg, stream);
   else launch_bwd<float>(a, c.rot, dqw, dkw, static_cast<int>(c.D), nwg, stream);
   return hipGetLastError();
