@@ -1014,8 +1014,9 @@ template <int D>
 __global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps(PagedArgs a) {
   __shared__ SmemMixed<D> sm;
   touch(a);
-  const int idx = launch_index();
-  for (int item = idx, items = idx + 1; item < items; item += a.grid) {
+  const uint32_t idx = launch_index();  // below 2^31, as the items and the launch are
+  for (uint32_t index = idx, items = idx + 1; index < items; index += a.grid) {
+    const int item = static_cast<int>(index);
     const int tid = thread_id(), lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     for (int i = wv; i <= a.npat; i += kPgWaves) {  // the last: single tokens
       int cnt = 0;
@@ -1032,15 +1033,19 @@ __global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps
     }
     __syncthreads();
     // Lane i: pattern i's tiles, the tiles of a unit (see the plan), its items.
-    const int pat = min(lane, a.npat - 1), tiles = sm.count[pat], tokens = sm.count[a.npat];
+    // An array of starts that does not ascend can list a token twice: no more of
+    // either than the plan has room for.
+    const int pat = min(lane, a.npat - 1), tokens = min(sm.count[a.npat], a.singles);
     const PagedPattern P = a.pat[pat];
+    const int tiles = max(0, min(sm.count[pat], P.tiles));
     const int splits = P.tile_split.d, run = max(1, min(16, static_cast<int>(static_cast<int64_t>(tiles) * a.H / 64)));
     const int units = ((tiles + run - 1) / run * a.H + 7) & ~7;
     const int singles = ((tokens * static_cast<int>(P.one_heads.d) + 7) & ~7) * P.one_split.d;
     const int mine = lane < a.npat ? units * run * splits : 0, ones = lane < a.npat ? singles : 0;
     const int tile_end = running_sum(mine), one_end = running_sum(ones);
     const int tile_items = __builtin_amdgcn_readlane(tile_end, 63);
-    items = tile_items + __builtin_amdgcn_readlane(one_end, 63);
+    const int all_items = tile_items + __builtin_amdgcn_readlane(one_end, 63);
+    items = all_items;
     __syncthreads();  // the counts are read
     if (item < tile_items) {
       const int pi = __builtin_ctzll(__ballot(tile_end > item));
@@ -1049,7 +1054,7 @@ __global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps
       if (tile_item(a, pi, item - begin, __builtin_amdgcn_readlane(tiles, pi), __builtin_amdgcn_readlane(run, pi),
                     __builtin_amdgcn_readlane(splits, pi), it))
         query_tiles<D>(a, it, sm.tile);
-    } else if (item < items) {
+    } else if (item < all_items) {
       const int pi = __builtin_ctzll(__ballot(one_end > item - tile_items));
       const int begin = tile_items + __builtin_amdgcn_readlane(one_end, pi) - __builtin_amdgcn_readlane(ones, pi);
       OneItem it;

@@ -264,7 +264,8 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     items += ((tiles + run - 1) / run * H + 7) / 8 * 8 * run * ts;
     expected += (T / (int64_t{t.r} * kPagedRows) + 2) * H * ts + std::min(T, B) * one_heads(patterns[i].r) * one;
   }
-  if (one_items >= kMost || one_items + items >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
+  // (the device's own count of a launch that steps rounds its units of fewer tiles up by less than 16 each)
+  if (one_items >= kMost || one_items + items + 16 * H * p.tile_slots >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
   p.one_items = one_items;
   p.tile_items = items;
   // Where the sizes allow many more items than they let expect, the launch is

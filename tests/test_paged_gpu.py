@@ -336,3 +336,24 @@ def test_other_stream_and_graph_replays():
             want = call()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_starts_that_do_not_ascend_stay_in_bounds():
+    """q_start names rows twice, more of them than there are tokens: nothing past
+    the workspace and the outputs is written."""
+    from paper_2307_02486_amd import paged_attn, paged_workspace_bytes
+    note("[paged] starts that do not ascend")
+    T, B, H, page, width = 40, 60, 12, 16, 64
+    pats = [(64, 1), (128, 2), (256, 4), (512, 6), (512, 12)]
+    kc, vc = (workloads.make_random((8, H, page, 64), BF, 1.0, 21, "cuda", t) for t in (0, 1))
+    q = workloads.make_random((T, H, 64), BF, 1.0, 21, "cuda", 2)
+    table = torch.arange(B * width, dtype=torch.int32, device="cuda").view(B, width) % 8
+    lens = torch.full((B,), 300, dtype=torch.int32, device="cuda")
+    need = paged_workspace_bytes(T, B, H, H, 64, 8, page, width, pats)
+    for far in (4, T):  # tokens by themselves, in tiles
+        start = torch.tensor([far * (b % 2) for b in range(B + 1)], dtype=torch.int32, device="cuda")
+        guard = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+        out, lse = torch.zeros((T + 8, H, 64), dtype=BF, device="cuda"), torch.zeros((H + 1, T), device="cuda")
+        paged_attn(q, kc, vc, table, lens, start, pats, out=out[:T], lse=lse[:H], workspace=guard[:need])
+        torch.cuda.synchronize()
+        assert bool((guard[need:] == 0x5A).all()) and bool((out[T:] == 0).all()) and bool((lse[H:] == 0).all())
