@@ -648,16 +648,16 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
 // Tiles of query rows
 // ---------------------------------------------------------------------------
 // The new tokens of sequences computed in tiles, sequence b0 + lane: positions
-// [c0, c1), empty for the others.
+// [c0, c1), empty for the others; tok0: the token row of position 0.
 struct Chunk {
-  int c0, c1;
+  int c0, c1, tok0;
 };
 __device__ inline Chunk chunk_of(const PagedArgs& a, int b0, int lane) {
   const int b = min(b0 + lane, a.B - 1);
-  const int n = token_row(a, b + 1) - token_row(a, b), len = a.lens[b];
+  const int end = token_row(a, b + 1), n = end - token_row(a, b), len = a.lens[b];
   const int c1 = max(0, static_cast<int>(min(static_cast<uint32_t>(max(len, 0)), a.reach)));
   const int c0 = max(0, static_cast<int>(min(static_cast<int64_t>(len) - n, static_cast<int64_t>(c1))));
-  return b0 + lane < a.B && n > a.few ? Chunk{c0, c1} : Chunk{0, 0};
+  return b0 + lane < a.B && n > a.few ? Chunk{c0, c1, end - len} : Chunk{0, 0, 0};
 }
 // Query tiles of pattern P over `len` >= 1 positions of a segment, and over a
 // sequence's new tokens, segment by segment (for any head: its offset only
@@ -684,7 +684,8 @@ __device__ inline bool query_tile(const PagedArgs& a, const PagedPattern& P, int
     if (tile < total) {
       const int l = __builtin_ctzll(__ballot(upto > tile));
       qt.b = b0 + l;
-      qt.c = Chunk{__builtin_amdgcn_readlane(c.c0, l), __builtin_amdgcn_readlane(c.c1, l)};
+      qt.c = Chunk{__builtin_amdgcn_readlane(c.c0, l), __builtin_amdgcn_readlane(c.c1, l),
+                   __builtin_amdgcn_readlane(c.tok0, l)};
       tile -= __builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(cnt, l);
       break;
     }
@@ -745,7 +746,7 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
   const int kb = sp * per, ke = min(kb + per, qend);
   const int slot = P.tile_slot + sp;
   const int base = gs + off;  // position of t = 0
-  const int tok0 = token_row(a, qt.b + 1) - a.lens[qt.b];  // token row of position 0
+  const int tok0 = qt.c.tok0;
 
   const int qr = lane & 31, hi = lane >> 5;
   const int wq_lo = q0 + wv * 32, tq = wq_lo + qr;
@@ -1089,6 +1090,20 @@ struct Mix {
     l = l * f0 + f1;
     acc = acc * f0 + o * (f1 * scale);
   }
+  // Another mixture of the same row.
+  template <typename Other>
+  __device__ void meet(float mo, float lo, Other&& other) {
+    const float mn = fmaxf(m, mo);
+    const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+    const float f1 = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
+    m = mn;
+    l = l * f0 + lo * f1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = acc[i] * f0 + other(i) * f1;
+  }
+  __device__ void meet(int lanes) {  // of the lane `lanes` away (an exclusive or)
+    meet(__shfl_xor(m, lanes, 64), __shfl_xor(l, lanes, 64), [&](int i) { return __shfl_xor(acc[i], lanes, 64); });
+  }
 };
 template <typename T, int D>
 __device__ inline void put_row(const PagedArgs& a, int tok, int head, int ch, const Mix& x) {
@@ -1144,18 +1159,8 @@ __device__ inline void join_singles(const PagedArgs& a, int group) {
       if (c < __builtin_amdgcn_readlane(upto, i)) slot = __builtin_amdgcn_readlane(first, i) + c;
     if (c < count) x.add(rec[slot], 1.0f, *reinterpret_cast<const f32x8*>(part + static_cast<int64_t>(slot) * D));
   }
-  auto meet = [&](float mo, float lo, auto&& other) {
-    const float mn = fmaxf(x.m, mo);
-    const float f0 = x.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.m - mn);
-    const float f1 = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
-    x.m = mn;
-    x.l = x.l * f0 + lo * f1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.acc[i] = x.acc[i] * f0 + other(i) * f1;
-  };
-#pragma unroll
-  for (int s = kLanes; s < 64; s <<= 1)
-    meet(__shfl_xor(x.m, s, 64), __shfl_xor(x.l, s, 64), [&](int i) { return __shfl_xor(x.acc[i], s, 64); });
+  for (int s = kLanes; s < 64; s <<= 1) x.meet(s);
   if constexpr (kTogether) {
     __shared__ __attribute__((aligned(16))) float rows[kPgWaves][D];
     __shared__ float ml[kPgWaves][2];
@@ -1167,20 +1172,21 @@ __device__ inline void join_singles(const PagedArgs& a, int group) {
     __syncthreads();
     if (wv != 0) return;
 #pragma unroll
-    for (int w = 1; w < kPgWaves; ++w) meet(ml[w][0], ml[w][1], [&](int i) { return rows[w][ch * 8 + i]; });
+    for (int w = 1; w < kPgWaves; ++w) x.meet(ml[w][0], ml[w][1], [&](int i) { return rows[w][ch * 8 + i]; });
   }
   if (sub == 0) put_row<T, D>(a, tk.tok, head, ch, x);
 }
 
 // Tokens of tiles, and those of no sequence: D/8 lanes a row, head by head and
 // token by token, the loads of all patterns before their use.  kPats bounds the
-// patterns at compile time.
-template <int D, int kPats>
+// patterns at compile time; kSubs such groups of lanes share a row, each with
+// every kSubs-th split.
+template <int D, int kPats, int kSubs>
 __device__ inline void join_tiles(const PagedArgs& a, int group) {
-  constexpr int kLanes = D / 8;
+  constexpr int kLanes = D / 8, kRows = kPgThreads / (kLanes * kSubs);
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
-  const int ch = tid % kLanes;
-  const int total = a.T * a.H, row = min(group * (kPgThreads / kLanes) + tid / kLanes, total - 1);
+  const int ch = tid % kLanes, sub = tid / kLanes % kSubs;
+  const int total = a.T * a.H, row = min(group * kRows + tid / (kLanes * kSubs), total - 1);
   const int tok = a.fheads.div(row), head = row - tok * a.H;
   // The sequences of the wave's first and last token; a wave across more looks
   // for each lane's.
@@ -1212,7 +1218,7 @@ __device__ inline void join_tiles(const PagedArgs& a, int group) {
       at[i] = static_cast<int64_t>(P.tile_slot) * total + row;
       splits = max(splits, static_cast<int>(P.tile_split.d));
     }
-    for (int sp = 0; sp < splits; ++sp) {
+    for (int sp = sub; sp < splits; sp += kSubs) {
       f32x2 rec[kPats];
       f16x8 o[kPats];
 #pragma unroll
@@ -1233,7 +1239,9 @@ __device__ inline void join_tiles(const PagedArgs& a, int group) {
       }
     }
   }
-  if (group * (kPgThreads / kLanes) + tid / kLanes < total) put_row<u16, D>(a, tok, head, ch, x);
+#pragma unroll
+  for (int m = kLanes; m < kLanes * kSubs; m <<= 1) x.meet(m);
+  if (sub == 0 && group * kRows + tid / (kLanes * kSubs) < total) put_row<u16, D>(a, tok, head, ch, x);
 }
 
 // kTogether: the waves of a workgroup share a single token's row.
@@ -1243,11 +1251,11 @@ __global__ __launch_bounds__(kPgThreads) void paged_join(PagedArgs a) {
   join_singles<T, D, false, kTogether>(a, launch_index());
 }
 // The rows of tiles first, then the single tokens'.
-template <int D, int kPats>
+template <int D, int kPats, int kSubs>
 __global__ __launch_bounds__(kPgThreads) void paged_join_all(PagedArgs a) {
   touch(a);
   const int group = launch_index();
-  if (group < a.join_groups) join_tiles<D, kPats>(a, group);
+  if (group < a.join_groups) join_tiles<D, kPats, kSubs>(a, group);
   else join_singles<u16, D, true, false>(a, group - a.join_groups);
 }
 
@@ -1255,6 +1263,9 @@ __global__ __launch_bounds__(kPgThreads) void paged_join_all(PagedArgs a) {
 // that one wave reads in several rounds: 12 rows of a token at 32K tokens took
 // 10.0 us a wave each, 5.6 a workgroup each), a wave each from there.
 constexpr int64_t kShared = 512;
+// Rows of tiles: lane groups that share one whose keys are split, up to this many rows.
+constexpr int kJoinSubs = 4;
+constexpr int64_t kJoinShared = 8192;
 template <typename T, int D>
 void launch_join(int64_t rows, const PagedArgs& a, hipStream_t stream) {
   const dim3 threads(kPgThreads);
@@ -1275,11 +1286,14 @@ void launch_all(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
   } else {
     if (p.steps) hipLaunchKernelGGL(paged_mixed_steps<D>, grid, threads, 0, stream, a);
     else hipLaunchKernelGGL(paged_mixed<D>, grid, threads, 0, stream, a);
-    constexpr int kRows = kPgThreads / (D / 8);
-    a.join_groups = static_cast<int32_t>((p.T * p.H + kRows - 1) / kRows);
+    const bool share = p.T * p.H <= kJoinShared && p.tile_slots > p.npat;
+    const int64_t rows = kPgThreads / (D / 8) / (share ? kJoinSubs : 1);
+    a.join_groups = static_cast<int32_t>((p.T * p.H + rows - 1) / rows);
     const dim3 join = grid_of(a.join_groups + (singles + kPgWaves - 1) / kPgWaves);
-    if (p.npat <= 5) hipLaunchKernelGGL((paged_join_all<D, 5>), join, threads, 0, stream, a);
-    else hipLaunchKernelGGL((paged_join_all<D, DA_MAX_PATTERNS>), join, threads, 0, stream, a);
+    if (p.npat > 5 && share) hipLaunchKernelGGL((paged_join_all<D, DA_MAX_PATTERNS, kJoinSubs>), join, threads, 0, stream, a);
+    else if (p.npat > 5) hipLaunchKernelGGL((paged_join_all<D, DA_MAX_PATTERNS, 1>), join, threads, 0, stream, a);
+    else if (share) hipLaunchKernelGGL((paged_join_all<D, 5, kJoinSubs>), join, threads, 0, stream, a);
+    else hipLaunchKernelGGL((paged_join_all<D, 5, 1>), join, threads, 0, stream, a);
   }
 }
 

@@ -208,6 +208,17 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   p.full = -1;
   p.scale = softmax_scale > 0.0f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(double(D)));
   const int64_t reach = max_pages * page;  // positions that the table holds
+  // The patterns whose rows see the most keys come first, of equal ones those of
+  // longer segments (more of whose rows are far from their segment's begin): the
+  // launch begins with its longest items.
+  da_pattern_t sorted[DA_MAX_PATTERNS];
+  std::copy(patterns, patterns + num_patterns, sorted);
+  std::stable_sort(sorted, sorted + num_patterns, [reach](const da_pattern_t& x, const da_pattern_t& y) {
+    const int64_t wx = std::min(x.w, reach), wy = std::min(y.w, reach);
+    const int64_t kx = (wx - 1) / x.r, ky = (wy - 1) / y.r;
+    return kx != ky ? kx > ky : wx > wy;
+  });
+  patterns = sorted;
   p.all_few = dtype == DA_F32 || std::min(max_new, T) <= kPagedFew;
   p.few = p.all_few ? T : B == 1 ? 0 : kPagedFew;
   p.singles = std::min(T, p.all_few ? T : B * p.few);
@@ -251,10 +262,13 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     t.tile_split = make_fastdiv(static_cast<uint32_t>(ts));
     t.tile_slot = static_cast<int32_t>(p.tile_slots);
     p.tile_slots += ts;
-    // A sequence of n tokens touches at most n / w + 2 segments, each with one
-    // tile more than its rows fill.  Units are dealt to the XCDs: up to 16 tiles,
-    // fewer where there would not be eight units each.
-    const int64_t tiles = std::min(T, T / (int64_t{t.r} * kPagedRows) + T / t.w + 2 * B + 2);
+    // A sequence of n tokens touches at most (n - 1) / w + 2 segments, and m
+    // positions of one fill m / (128 r) tiles, rounded up.  (One sequence of 512
+    // tokens, the paper's patterns: 14 tiles a head where 9 are there; with 27
+    // the workgroups without work held up the others.)  Units are dealt to the
+    // XCDs: up to 16 tiles, fewer where there would not be eight units each.
+    const int64_t some = std::min(B, T), segments = (T - some) / t.w + 2 * some, fill = int64_t{t.r} * kPagedRows;
+    const int64_t tiles = std::min(T, segments + (T - segments) / fill);
     if (tiles >= kMost / H / ts) return DA_EINVAL;
     const int64_t run = std::max<int64_t>(1, std::min<int64_t>(16, tiles * H / 64));
     if (items >= kMost) return DA_EINVAL;

@@ -416,6 +416,11 @@ def _token_stride(name: str, t: torch.Tensor, lead: int, dtype, device) -> int:
     return H * D if step is None else step
 
 
+def _contiguous_like(t: torch.Tensor) -> torch.Tensor:
+    """An empty contiguous tensor of t's shape (half the host time of torch.empty with a shape and a device)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 # The sizes and strides of a call, validated and with what follows from them,
 # by the shapes (at most 256 of each operator; nothing of a tensor is kept).
 _HEADS: dict = {}
@@ -463,8 +468,7 @@ def qk_norm_xpos(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor, k_wei
     evenly spaced.  Returns new contiguous (q_out, k_out).  Enqueued on `stream`."""
     lib = _lib.load()
     B, N, H, Hkv, D, qs, ks, dcode, _ = _qk_call(q, k, q_weight, k_weight)
-    qo = torch.empty((B, N, H, D), dtype=q.dtype, device=q.device)
-    ko = torch.empty((B, N, Hkv, D), dtype=q.dtype, device=q.device)
+    qo, ko = _contiguous_like(q), _contiguous_like(k)
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
     rc = lib.dilated_attn_qk_norm_xpos(q.data_ptr(), k.data_ptr(), q_weight.data_ptr(), k_weight.data_ptr(),
                                        qo.data_ptr(), ko.data_ptr(), B, N, H, Hkv, D, qs, ks, float(eps),
@@ -578,7 +582,7 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
     if q is not None:
         if q.dtype != dt or q.get_device() != dev:
             raise ValueError(f"q must be a {dt} tensor on {k.device}")
-        qo = torch.empty((T, H, D), dtype=dt, device=k.device)
+        qo = _contiguous_like(q)
     elif q_weight is not None:
         raise ValueError("q_weight without q")
     if q_weight is not None:
@@ -652,17 +656,17 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
     _check_cache(dev, q.dtype, B, k_cache, v_cache, block_table, seq_lens, q_start)
     owned = []
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        out = _contiguous_like(q)
         owned.append(out)
     else:
         _check_like("out", out, (T, H, D), q.dtype, q.device)
     if lse is None:
-        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((H, T), dtype=torch.float32)
         owned.append(lse)
     else:
         _check_like("lse", lse, (H, T), torch.float32, q.device)
     if workspace is None:
-        workspace, nbytes = torch.empty(need, dtype=torch.uint8, device=q.device), need
+        workspace, nbytes = q.new_empty(need, dtype=torch.uint8), need
         owned.append(workspace)
     else:
         if workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
