@@ -104,6 +104,11 @@ __device__ inline int head_offset(const PagedPattern& P, int head) {
   return head - static_cast<int>(P.fr.div(head)) * P.r;
 }
 
+// The loads of these values begin before this point.  (A load whose value is used
+// under a condition only would move there: another round to memory after those
+// that the condition waits for.)
+__device__ inline void here(int& v) { asm volatile("" : "+v"(v)); }
+
 // A sequence's new tokens: rows begin .. end - 1 of the call, the last of its
 // length len.
 struct Sequence {
@@ -125,6 +130,7 @@ __device__ inline void find_sequences(const PagedArgs& a, const int (&tok)[kToke
     const int b = b0 + lane;
     start = a.start[min(b, a.B)];
     len = a.lens[min(b, a.B - 1)];
+    here(len);
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) n[i] += __popcll(__ballot(b <= a.B && start <= tok[i]));
   }
@@ -194,7 +200,9 @@ __device__ inline bool single_token(const PagedArgs& a, int e, int lane, Token& 
   } else {
     t.tok = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-      const int b = min(b0 + lane, a.B - 1), begin = token_row(a, b), end = token_row(a, b + 1), len = a.lens[b];
+      const int b = min(b0 + lane, a.B - 1), begin = token_row(a, b), end = token_row(a, b + 1);
+      int len = a.lens[b];
+      here(len);
       const int n = b0 + lane < a.B && end - begin <= a.few ? max(end - begin, 0) : 0;
       const int upto = running_sum(n), total = __builtin_amdgcn_readlane(upto, 63);
       if (e < total) {
@@ -246,6 +254,8 @@ __device__ inline void look_up_rows(const PagedArgs& a, const int32_t* table, in
       pos[u] = base + min(first + i0 + u * kPgThreads, last) * r;
       entry[u] = table_entry(a, table, pos[u]);
     }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) here(entry[u]);
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u)
       if (i0 + u * kPgThreads < n) row[i0 + u * kPgThreads] = cache_row(a, entry[u], hk, pos[u]);
