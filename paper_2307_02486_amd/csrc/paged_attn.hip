@@ -262,9 +262,11 @@ __device__ inline void look_up_rows(const PagedArgs& a, const int32_t* table, in
   }
 }
 
-// Keys of split s of n keys: [first, end), whole 32-key tiles but the last.
+// Keys of a split of n keys: whole 32-key tiles, and two of them for each wave
+// at least (64 tokens of 100 to 2000 cached, dense: 30.4 us without that, 28.9 with it).
+constexpr int kOneLeast = 256;
 __device__ inline int split_keys_of(const PagedPattern& P, int n) {
-  return (static_cast<int>(P.one_split.div(n + P.one_split.d - 1)) + 31) & ~31;
+  return max(kOneLeast, (static_cast<int>(P.one_split.div(n + P.one_split.d - 1)) + 31) & ~31);
 }
 
 __device__ inline float max_over_groups(float v) {  // over lanes 16 apart

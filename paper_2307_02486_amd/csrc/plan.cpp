@@ -230,12 +230,20 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     if (r >= G) return std::min(key_heads, (H + r - 1) / r);
     return key_heads * (((G + r - 1) / r + kPagedGroupRows - 1) / kPagedGroupRows);
   };
-  // Workgroups with work, of the listed tokens and of the tiles.
+  // Workgroups with work, of the tokens by themselves and of the tiles.  Beside
+  // tiles the tokens are taken to be one of each sequence.
+  const int64_t tokens = p.all_few ? p.singles : std::min(T, B);
   double one_busy = 0.0, tile_busy = 0.0;
   for (int i = 0; i < p.npat; ++i) {
-    one_busy += static_cast<double>(p.singles) * one_heads(patterns[i].r);
+    one_busy += static_cast<double>(tokens) * one_heads(patterns[i].r);
     tile_busy += H * std::ceil(double(T) / patterns[i].r / kPagedRows);
   }
+  // Splits of a token's keys: until there are about four workgroups for each
+  // place on the chip (768), half as many beside tiles.  More cost a start-up each
+  // (64 tokens of 1000 to 32767 cached: 72 us at 2 splits, 83 at 4), fewer leave
+  // the longest ones alone at the end (32 tokens of up to 30000, heads of 128: 102
+  // us at 24, 113 at 12).
+  const double one_target = p.all_few ? 3072.0 : 1536.0;
   int64_t one_items = 0, expected = 0;
   int64_t items = 0;
   for (int i = 0; i < p.npat; ++i) {
@@ -248,7 +256,7 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     if (t.r == 1 && (p.full < 0 || t.w > p.pat[p.full].w)) p.full = i;
     const int64_t keys = (t.w + int64_t{t.r} - 1) / t.r;  // of a row, at most
     const int64_t one = std::max<int64_t>(
-        1, std::min({static_cast<int64_t>(4096.0 / std::max(1.0, one_busy)), (keys + 255) / 256, int64_t{64}}));
+        1, std::min({static_cast<int64_t>(one_target / std::max(1.0, one_busy) + 0.5), (keys + 255) / 256, int64_t{64}}));
     t.one_split = make_fastdiv(static_cast<uint32_t>(one));
     t.one_slot = static_cast<int32_t>(p.one_slots);
     p.one_slots += one;
