@@ -12,7 +12,9 @@
 // and forms their angles and scales once per token instead of once per head
 // (float64 products and a reduction to a quarter turn: as much work as five
 // heads' rows).  Sums over a row are DPP exchanges within 16 lanes.  All bound
-// by HBM at training sizes, by the launch at decoding sizes.
+// by HBM at training sizes (gradients of 4 x 8192 tokens of 12 + 12 heads of 64:
+// 302 MB in 54-60 us, 5.0-5.6 TB/s; three prompts of 11800 tokens of 24 heads of 128
+// into a cache: 145 MB in 27 us, 5.3 TB/s), by the launch at decoding sizes (5.4 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -494,7 +494,7 @@ def qk_norm_xpos_bwd(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor
     need = _workspace_bytes("dilated_attn_qk_norm_xpos_bwd_workspace", B, N, D)
     dq, dk = torch.empty_like(dq_out), torch.empty_like(dk_out)
     dqw, dkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    ws = q.new_empty(need, dtype=torch.uint8)
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
     rc = lib.dilated_attn_qk_norm_xpos_bwd(
         dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), q_weight.data_ptr(), k_weight.data_ptr(),
