@@ -37,8 +37,9 @@ extern "C" {
  * stream      a hipStream_t (NULL = the default stream); asynchronous.
  *
  * Arithmetic in float32, angles and scale exponents formed and reduced in
- * float64; outputs rounded to dtype once.  All device pointers 16-byte
- * aligned.  Returns DA_OK or a negative code; errors launch nothing.
+ * float64; outputs rounded to dtype once.  A head's sum of squares has to be
+ * finite in float32 (elements below 1.6e18 are safe).  All device pointers
+ * 16-byte aligned.  Returns DA_OK or a negative code; errors launch nothing.
  */
 int dilated_attn_qk_norm_xpos(const void* q, const void* k, const void* qw, const void* kw, void* qo, void* ko,
                               int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride,
