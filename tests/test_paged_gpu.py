@@ -357,3 +357,23 @@ def test_starts_that_do_not_ascend_stay_in_bounds():
         paged_attn(q, kc, vc, table, lens, start, pats, out=out[:T], lse=lse[:H], workspace=guard[:need])
         torch.cuda.synchronize()
         assert bool((guard[need:] == 0x5A).all()) and bool((out[T:] == 0).all()) and bool((lse[H:] == 0).all())
+
+
+SPLIT = [
+    # keys in several splits: (new tokens, cached before, H, Hkv, D, page, patterns)
+    ([100], [1500], 3, 3, 64, 16, [(2048, 1), (2048, 2), (4096, 1), (1024, 1), (3000, 2), (5000, 3)]),  # few rows, six patterns
+    ([900], [700], 12, 4, 64, 64, [(2048, 1), (2048, 2), (4096, 1), (1024, 1), (3000, 2), (5000, 3)]),  # many rows
+    ([200], [1900], 6, 6, 32, 16, [(4096, 1), (1024, 3)]),
+    ([60, 1, 1], [1200, 3000, 40], 4, 2, 128, 32, [(512, 1), (4096, 1)]),
+    ([1, 1, 1], [5000, 300, 255], 6, 2, 64, 16, DENSE),
+]
+
+
+@pytest.mark.parametrize("case", SPLIT, ids=lambda c: str(c)[:60])
+def test_split_keys(case):
+    from paper_2307_02486_amd import paged_attn
+    new, before, H, Hkv, D, page, patterns = case
+    note(f"[paged] split {str(case)[:200]}")
+    q, kc, vc, dev, lens, start, seqs = setup(new, before, H, Hkv, D, page, BF)
+    for order in (patterns, patterns[::-1]):
+        compare(*paged_attn(q, kc, vc, *dev, order, max_new=max(new)), q, seqs, lens, start, order, BF, "split")
