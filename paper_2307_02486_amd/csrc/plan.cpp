@@ -244,6 +244,12 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   // the longest ones alone at the end (32 tokens of up to 30000, heads of 128: 102
   // us at 24, 113 at 12).
   const double one_target = p.all_few ? 3072.0 : 1536.0;
+  // A tile's keys are split until there are 2048 workgroups, and not below this
+  // many of the pattern's longest rows: an item's start-up is as long as ten key
+  // tiles.  (At 512, 768, 1024: 1000 new tokens among 15 single ones 38, 34.9, 33
+  // us, 1024 at 20000 35.3, 33.8, 32.7, 512 at 31500 28.2, 28.1, 28.9; 128 at 32000,
+  // whose launch leaves most of the chip idle, 21.0, 22.3, 25.6.)
+  const int64_t tile_least = tile_busy < 64.0 ? 512 : 768;
   int64_t one_items = 0, expected = 0;
   int64_t items = 0;
   for (int i = 0; i < p.npat; ++i) {
@@ -266,7 +272,7 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     one_items += (p.singles * one_heads(patterns[i].r) + 7) / 8 * 8 * one;  // units XCD by XCD
     if (p.all_few) continue;
     const int64_t ts = std::max<int64_t>(
-        1, std::min({static_cast<int64_t>(2048.0 / std::max(1.0, tile_busy)), (keys + 511) / 512, int64_t{16}}));
+        1, std::min({static_cast<int64_t>(2048.0 / std::max(1.0, tile_busy)), (keys + tile_least - 1) / tile_least, int64_t{16}}));
     t.tile_split = make_fastdiv(static_cast<uint32_t>(ts));
     t.tile_slot = static_cast<int32_t>(p.tile_slots);
     p.tile_slots += ts;
