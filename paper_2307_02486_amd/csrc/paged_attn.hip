@@ -821,114 +821,115 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
   for (int c0 = kb; c0 < ke; c0 += kTileRows) {
-  const int ntile = (min(ke - c0, kTileRows) + BN - 1) / BN;
-  look_up_rows<8>(a, table, hk, base, P.r, c0, ke - 1, ntile * BN, tid, sm.row);
-  __syncthreads();
-  load_tile(0, 0);
-  wait_loads<0>();
-  __syncthreads();
-  for (int jt = 0; jt < ntile; ++jt) {
-    const int cur = jt & 1, k0 = c0 + jt * BN;
-    if (jt + 1 < ntile) load_tile(jt + 1, cur ^ 1);
-    const char* kl = reinterpret_cast<const char*>(&sm.k[cur][0]);
-    const char* vl = reinterpret_cast<const char*>(&sm.v[cur][0]);
-    if (k0 <= wq_lo + 31 && wq_lo < qend) {  // not all keys after this wave's queries
-      constexpr int QG = D <= 64 ? 2 : 1;
-      f32x16 acc_s[2];
-#pragma unroll
-      for (int kb0 = 0; kb0 < 2; kb0 += QG) {
-        u32x4 kf[QG][KC];
-#pragma unroll
-        for (int x = 0; x < QG; ++x)
-#pragma unroll
-          for (int c = 0; c < KC; ++c)
-            kf[x][c] = *reinterpret_cast<const u32x4*>(kl + TL::offset((kb0 + x) * 32 + qr, 2 * c + hi));
-        __builtin_amdgcn_sched_barrier(0);  // keep the reads ahead of the MFMAs
-#pragma unroll
-        for (int x = 0; x < QG; ++x) {
-          acc_s[kb0 + x] = f32x16{};
-#pragma unroll
-          for (int c = 0; c < KC; ++c)
-            acc_s[kb0 + x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][c]), qreg[c],
-                                                                     acc_s[kb0 + x], 0, 0, 0);
-        }
-      }
-      if (k0 + BN - 1 > wq_lo || k0 + BN > ke) {  // mask keys after the query and past the split
-        int first = k0 + 4 * hi - min(tq_in, ke - 1);
-        asm volatile("" : "+v"(first));  // compares made here, not hoisted into scalar masks
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (first + x * 32 + 8 * (j >> 2) + (j & 3) > 0) acc_s[x][j] = -INFINITY;
-      }
-      // P = 2^(c S - m) for the reference m of the row so far, without looking
-      // for the tile's maximum: a tile whose probabilities of half a row sum to
-      // more than kSumSlack (or overflow: the first tile's do) has its scores
-      // still in registers and forms them again with its maximum as reference.
-      // Probabilities above 1 are held by bf16 and float32 as well as those below.
-      bf16x8 pb[2][2];
-      float lt;
-      auto probabilities = [&] {
-        const float negm = -m_run;
-        float lp[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(acc_s[x][j], c2, negm));
-            lp[j & 3] += pe;
-            pb[x][j >> 3][j & 7] = (__bf16)pe;
-          }
-        lt = (lp[0] + lp[1]) + (lp[2] + lp[3]);
-      };
-      probabilities();
-      if (__any(!(lt <= kSumSlack))) {
-        float mx = acc_s[0][0];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int j = 0; j < 16; j += 2) mx = fmaxf(mx, fmaxf(acc_s[x][j], acc_s[x][j + 1]));
-        const float m_new = fmaxf(m_run, fmaxf(mx, other_half(mx)) * c2);
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        m_run = m_new;
-        l_run *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) acc_o[db][j] *= alpha;
-        probabilities();
-      }
-      l_run += lt;
-      const uint32_t vaddr = lds_addr(vl);
-      static_for<0, 2>([&](auto KB) {
-        constexpr int kb2 = decltype(KB)::value;
-        u32x2 vf[2][DB][2];
-        static_for<0, 2>([&](auto KK) {
-          static_for<0, DB>([&](auto DBI) {
-            static_for<0, 2>([&](auto T) {
-              constexpr int kk = decltype(KK)::value, db = decltype(DBI)::value, t = decltype(T)::value;
-              constexpr int r0 = kb2 * 32 + 16 * kk;
-              vf[kk][db][t] = lds_read_tr16<r0 * TL::kRowBytes>(vaddr + vtr_off[db][t]);
-            });
-          });
-        });
-        static_for<0, 2>([&](auto KK) {
-          constexpr int kk = decltype(KK)::value;
-          lds_wait<(1 - kk) * 2 * DB>();
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            lds_bind(vf[kk][db][0]);
-            lds_bind(vf[kk][db][1]);
-            const u32x4 a4 = {vf[kk][db][0][0], vf[kk][db][0][1], vf[kk][db][1][0], vf[kk][db][1][1]};
-            acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a4), pb[kb2][kk], acc_o[db], 0, 0, 0);
-          }
-        });
-      });
-    }
+    const int ntile = (min(ke - c0, kTileRows) + BN - 1) / BN;
+    look_up_rows<8>(a, table, hk, base, P.r, c0, ke - 1, ntile * BN, tid, sm.row);
+    __syncthreads();
+    load_tile(0, 0);
     wait_loads<0>();
     __syncthreads();
-  }
+    for (int jt = 0; jt < ntile; ++jt) {
+      const int cur = jt & 1, k0 = c0 + jt * BN;
+      if (jt + 1 < ntile) load_tile(jt + 1, cur ^ 1);
+      const char* kl = reinterpret_cast<const char*>(&sm.k[cur][0]);
+      const char* vl = reinterpret_cast<const char*>(&sm.v[cur][0]);
+      if (k0 <= wq_lo + 31 && wq_lo < qend) {  // not all keys after this wave's queries
+        constexpr int QG = D <= 64 ? 2 : 1;
+        f32x16 acc_s[2];
+#pragma unroll
+        for (int kb0 = 0; kb0 < 2; kb0 += QG) {
+          u32x4 kf[QG][KC];
+#pragma unroll
+          for (int x = 0; x < QG; ++x)
+#pragma unroll
+            for (int c = 0; c < KC; ++c)
+              kf[x][c] = *reinterpret_cast<const u32x4*>(kl + TL::offset((kb0 + x) * 32 + qr, 2 * c + hi));
+          __builtin_amdgcn_sched_barrier(0);  // keep the reads ahead of the MFMAs
+#pragma unroll
+          for (int x = 0; x < QG; ++x) {
+            acc_s[kb0 + x] = f32x16{};
+#pragma unroll
+            for (int c = 0; c < KC; ++c)
+              acc_s[kb0 + x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][c]), qreg[c],
+                                                                       acc_s[kb0 + x], 0, 0, 0);
+          }
+        }
+        if (k0 + BN - 1 > wq_lo || k0 + BN > ke) {  // mask keys after the query and past the split
+          int first = k0 + 4 * hi - min(tq_in, ke - 1);
+          asm volatile("" : "+v"(first));  // compares made here, not hoisted into scalar masks
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (first + x * 32 + 8 * (j >> 2) + (j & 3) > 0) acc_s[x][j] = -INFINITY;
+        }
+        // P = 2^(c S - m) for the reference m of the row so far, without looking
+        // for the tile's maximum: a tile whose probabilities of half a row sum to
+        // more than kSumSlack (or overflow: the first tile's do) has its scores
+        // still in registers and forms them again with its maximum as reference.
+        // Probabilities above 1 are held by bf16 and float32 as well as those below.
+        bf16x8 pb[2][2];
+        float lt;
+        auto probabilities = [&] {
+          const float negm = -m_run;
+          float lp[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float pe = __builtin_amdgcn_exp2f(__builtin_fmaf(acc_s[x][j], c2, negm));
+              lp[j & 3] += pe;
+              pb[x][j >> 3][j & 7] = (__bf16)pe;
+            }
+          lt = (lp[0] + lp[1]) + (lp[2] + lp[3]);
+        };
+        probabilities();
+        if (__any(!(lt <= kSumSlack))) {
+          float mx = acc_s[0][0];
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) mx = fmaxf(mx, fmaxf(acc_s[x][j], acc_s[x][j + 1]));
+          const float m_new = fmaxf(m_run, fmaxf(mx, other_half(mx)) * c2);
+          const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          l_run *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc_o[db][j] *= alpha;
+          probabilities();
+        }
+        l_run += lt;
+        const uint32_t vaddr = lds_addr(vl);
+        static_for<0, 2>([&](auto KB) {
+          constexpr int kb2 = decltype(KB)::value;
+          u32x2 vf[2][DB][2];
+          static_for<0, 2>([&](auto KK) {
+            static_for<0, DB>([&](auto DBI) {
+              static_for<0, 2>([&](auto T) {
+                constexpr int kk = decltype(KK)::value, db = decltype(DBI)::value, t = decltype(T)::value;
+                constexpr int r0 = kb2 * 32 + 16 * kk;
+                vf[kk][db][t] = lds_read_tr16<r0 * TL::kRowBytes>(vaddr + vtr_off[db][t]);
+              });
+            });
+          });
+          static_for<0, 2>([&](auto KK) {
+            constexpr int kk = decltype(KK)::value;
+            lds_wait<(1 - kk) * 2 * DB>();
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              lds_bind(vf[kk][db][0]);
+              lds_bind(vf[kk][db][1]);
+              const u32x4 a4 = {vf[kk][db][0][0], vf[kk][db][0][1], vf[kk][db][1][0], vf[kk][db][1][1]};
+              acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a4), pb[kb2][kk],
+                                                                  acc_o[db], 0, 0, 0);
+            }
+          });
+        });
+      }
+      wait_loads<0>();
+      __syncthreads();
+    }
   }
 
   // The wave's 32 rows as fp16 times a power of two per row (within 2^-11 of
@@ -1280,7 +1281,8 @@ __global__ __launch_bounds__(kPgThreads) void paged_join_all(PagedArgs a) {
 // that one wave reads in several rounds: 12 rows of a token at 32K tokens took
 // 10.0 us a wave each, 5.6 a workgroup each), a wave each from there.
 constexpr int64_t kShared = 512;
-// Rows of tiles: lane groups that share one whose keys are split, up to this many rows.
+// Rows of tiles: lane groups that share one whose keys are split, up to this many
+// rows (6144 rows of 4 to 6 splits 9.4 -> 6.8 us, 12180 of 4 splits 7.0 -> 9.4).
 constexpr int kJoinSubs = 4;
 constexpr int64_t kJoinShared = 8192;
 template <typename T, int D>
@@ -1307,8 +1309,9 @@ void launch_all(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
     const int64_t rows = kPgThreads / (D / 8) / (share ? kJoinSubs : 1);
     a.join_groups = static_cast<int32_t>((p.T * p.H + rows - 1) / rows);
     const dim3 join = grid_of(a.join_groups + (singles + kPgWaves - 1) / kPgWaves);
-    if (p.npat > 5 && share) hipLaunchKernelGGL((paged_join_all<D, DA_MAX_PATTERNS, kJoinSubs>), join, threads, 0, stream, a);
-    else if (p.npat > 5) hipLaunchKernelGGL((paged_join_all<D, DA_MAX_PATTERNS, 1>), join, threads, 0, stream, a);
+    constexpr int kMost = DA_MAX_PATTERNS;
+    if (p.npat > 5 && share) hipLaunchKernelGGL((paged_join_all<D, kMost, kJoinSubs>), join, threads, 0, stream, a);
+    else if (p.npat > 5) hipLaunchKernelGGL((paged_join_all<D, kMost, 1>), join, threads, 0, stream, a);
     else if (share) hipLaunchKernelGGL((paged_join_all<D, 5, kJoinSubs>), join, threads, 0, stream, a);
     else hipLaunchKernelGGL((paged_join_all<D, 5, 1>), join, threads, 0, stream, a);
   }
