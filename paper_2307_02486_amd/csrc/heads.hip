@@ -8,13 +8,13 @@
 //   dx = rstd (dn w - xhat mean(dn w xhat)),   dw = sum over rows of dn xhat.
 //
 // One wave per token: D/8 lanes hold one head's row, eight elements each, and
-// a wave steps through the token's heads, so that a lane keeps its four pairs
-// and forms their angles and scales once per token instead of once per head
-// (float64 products and a reduction to a quarter turn: as much work as five
-// heads' rows).  Sums over a row are DPP exchanges within 16 lanes.  All bound
-// by HBM at training sizes (gradients of 4 x 8192 tokens of 12 + 12 heads of 64:
-// 302 MB in 54-60 us, 5.0-5.6 TB/s; three prompts of 11800 tokens of 24 heads of 128
-// into a cache: 145 MB in 27 us, 5.3 TB/s), by the launch at decoding sizes (5.4 us).
+// a wave steps through the token's heads, so that a lane keeps its four pairs,
+// whose angles and scales (float64 products and a reduction to a quarter turn: as
+// much work as a head's row) are formed once per token instead of once per head.
+// Sums over a row are DPP exchanges within 16 lanes.  All bound by HBM at training
+// sizes (gradients of 4 x 8192 tokens of 12 + 12 heads of 64: 302 MB in 53 us, 5.7
+// TB/s; three prompts of 11800 tokens of 24 heads of 128 into a cache: 145 MB in 25
+// us, 5.8 TB/s), by the launch at decoding sizes (5.3 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -36,21 +36,6 @@ struct HeadTab {
   double turn[kPairs];
   double l2z[kPairs];
 };
-// A lane's four pairs of it.
-struct LaneTab {
-  double turn[4], l2z[4];
-};
-template <int kPairs>
-__device__ inline LaneTab lane_tab(const HeadTab<kPairs>& tab, int pair0) {
-  LaneTab t;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    t.turn[e] = tab.turn[pair0 + e];
-    t.l2z[e] = tab.l2z[pair0 + e];
-  }
-  return t;
-}
-
 template <typename T> struct Raw8;
 template <> struct Raw8<u16> { typedef u32x4 type; };
 template <> struct Raw8<float> { typedef f32x8 type; };
@@ -96,29 +81,48 @@ __device__ inline float row_sum(float v) {
 struct Rotation {
   float cs[4], sn[4], up[4], down[4];
 };
-__device__ inline Rotation rotation(const LaneTab& tab, int pos, int rel) {
+// Formed a pair per lane, lane mod kPairs, whose constants turn and l2z are, and
+// handed through the wave's own LDS.  (Four pairs a lane, formed by every row's
+// lanes again: gradients of 4 x 8192 tokens 62.6 us instead of 61.5, three prompts
+// into a cache 29.0 instead of 28.4.)
+template <int kPairs>
+__device__ inline Rotation rotation(double turn, double l2z, int pos, int rel, f32x4 (&share)[kPairs], int lane,
+                                    int ch) {
+  // The angle in quarter turns, reduced in float64 to [-1/2, 1/2]: the
+  // float32 series below then have arguments of at most pi/4 and are exact
+  // to a rounding (first terms left out: x^11/11! < 2e-9, x^10/10! < 3e-8).
+  const double a = static_cast<double>(pos) * turn;
+  const double n = rint(a);
+  const int quad = static_cast<int>(n);
+  const float x = static_cast<float>(a - n) * 1.57079632679489662f, x2 = x * x;
+  const float s = x + x * x2 * (-1.0f / 6 + x2 * (1.0f / 120 + x2 * (-1.0f / 5040 + x2 * (1.0f / 362880))));
+  const float c = 1.0f + x2 * (-0.5f + x2 * (1.0f / 24 + x2 * (-1.0f / 720 + x2 * (1.0f / 40320))));
+  const float sq = quad & 1 ? c : s, cq = quad & 1 ? s : c;
+  const double z = static_cast<double>(rel) * l2z;
+  const double k = rint(z);
+  const float f = static_cast<float>(z - k);
+  f32x4 v;
+  v[0] = (quad + 1) & 2 ? -cq : cq;
+  v[1] = quad & 2 ? -sq : sq;
+  v[2] = ldexpf(__builtin_amdgcn_exp2f(f), static_cast<int>(k));
+  v[3] = ldexpf(__builtin_amdgcn_exp2f(-f), -static_cast<int>(k));
+  // Pair 4 c + e at e (kPairs / 4) + c: a row's lanes read 16 bytes each, side by
+  // side.  A wave's LDS operations complete in order; the fences are the compiler's.
+  const int pair = lane % kPairs;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (lane < kPairs) share[(pair & 3) * (kPairs / 4) + (pair >> 2)] = v;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
   Rotation r;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    // The angle in quarter turns, reduced in float64 to [-1/2, 1/2]: the
-    // float32 series below then have arguments of at most pi/4 and are exact
-    // to a rounding (first terms left out: x^11/11! < 2e-9, x^10/10! < 3e-8).
-    const double a = static_cast<double>(pos) * tab.turn[e];
-    const double n = rint(a);
-    const int quad = static_cast<int>(n);
-    const float x = static_cast<float>(a - n) * 1.57079632679489662f, x2 = x * x;
-    const float s =
-        x + x * x2 * (-1.0f / 6 + x2 * (1.0f / 120 + x2 * (-1.0f / 5040 + x2 * (1.0f / 362880))));
-    const float c = 1.0f + x2 * (-0.5f + x2 * (1.0f / 24 + x2 * (-1.0f / 720 + x2 * (1.0f / 40320))));
-    const float sq = quad & 1 ? c : s, cq = quad & 1 ? s : c;
-    r.sn[e] = quad & 2 ? -sq : sq;
-    r.cs[e] = (quad + 1) & 2 ? -cq : cq;
-    const double z = static_cast<double>(rel) * tab.l2z[e];
-    const double k = rint(z);
-    const float f = static_cast<float>(z - k);
-    r.up[e] = ldexpf(__builtin_amdgcn_exp2f(f), static_cast<int>(k));
-    r.down[e] = ldexpf(__builtin_amdgcn_exp2f(-f), -static_cast<int>(k));
+    const f32x4 t = share[e * (kPairs / 4) + ch];
+    r.cs[e] = t[0];
+    r.sn[e] = t[1];
+    r.up[e] = t[2];
+    r.down[e] = t[3];
   }
+  __builtin_amdgcn_wave_barrier();
   return r;
 }
 
@@ -169,7 +173,9 @@ __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a, HeadTab
     const T* p = row < nq ? q + row * D : row < nk ? k + (row - nq) * D : v + (row - nk) * D;
     return *reinterpret_cast<const Raw*>(p);
   };
-  const LaneTab lt = lane_tab(tab, ch * 4);
+  __shared__ __attribute__((aligned(16))) f32x4 share[kHeadWaves][D / 2];
+  const int wv = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_workitem_id_x() >> 6);
+  const double turn = tab.turn[lane % (D / 2)], l2z = tab.l2z[lane % (D / 2)];
   const int first = a.q ? 0 : nq;  // without queries their rows are passed over
   Raw x[kUnroll];
 #pragma unroll
@@ -199,7 +205,7 @@ __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a, HeadTab
   } else {
     pos = static_cast<int>(tok) - static_cast<int>(a.fn.div(static_cast<uint32_t>(tok)) * a.fn.d);
   }
-  const Rotation rt = rotation(lt, live ? pos : 0, live ? pos - a.center : 0);
+  const Rotation rt = rotation<D / 2>(turn, l2z, live ? pos : 0, live ? pos - a.center : 0, share[wv], lane, ch);
   const bool norm_q = a.qw != nullptr, norm_k = a.kw != nullptr;
   float wq[8], wk[8];
 #pragma unroll
@@ -269,6 +275,7 @@ __global__ __launch_bounds__(kHeadThreads, sizeof(T) == 2 ? 4 : 3) void heads_bw
   typedef typename Raw8<T>::type Raw;
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;
   __shared__ float red[kHeadWaves][2 * D];
+  __shared__ __attribute__((aligned(16))) f32x4 share[kHeadWaves][D / 2];
   const int tid = __builtin_amdgcn_workitem_id_x();
   const int lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int sub = lane / kLanes, ch = lane % kLanes;
@@ -298,10 +305,10 @@ __global__ __launch_bounds__(kHeadThreads, sizeof(T) == 2 ? 4 : 3) void heads_bw
     }
   };
   load(tok, 0);
-  const LaneTab lt = lane_tab(tab, ch * 4);
+  const double turn = tab.turn[lane % (D / 2)], l2z = tab.l2z[lane % (D / 2)];
   for (; tok < a.T; tok += stride) {
     const int pos = static_cast<int>(tok) - static_cast<int>(a.fn.div(static_cast<uint32_t>(tok)) * a.fn.d);
-    const Rotation rt = rotation(lt, pos, pos - a.center);
+    const Rotation rt = rotation<D / 2>(turn, l2z, pos, pos - a.center, share[wv], lane, ch);
     for (int r0 = 0; r0 < rows; r0 += kRows) {
       const Raw x = nx, dy = ndy;
       const bool last = r0 + kRows >= rows;
