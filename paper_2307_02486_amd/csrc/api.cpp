@@ -9,6 +9,7 @@
 
 #include "../../include/dilated_attn_paged.h"
 #include "kernels.h"
+#include "paged.h"
 #include "plan.h"
 
 namespace {

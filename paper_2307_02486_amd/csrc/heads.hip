@@ -21,6 +21,7 @@
 #include <cmath>
 
 #include "device_common.h"
+#include "paged.h"
 
 namespace da {
 namespace {

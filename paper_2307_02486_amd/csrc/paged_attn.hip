@@ -32,6 +32,7 @@
 #include <algorithm>
 
 #include "device_common.h"
+#include "paged.h"
 
 namespace da {
 namespace {
