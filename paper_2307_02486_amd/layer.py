@@ -249,7 +249,9 @@ class LongNetAttention(torch.nn.Module):
         the cache's layer `layer`) and which attend to what is there of their
         own sequence: what forward gives on whole sequences, row by row (up to
         rounding: xPos is centred on the cache's centre).  Causal layers only,
-        without gradients."""
+        without gradients and not under torch.jit.trace."""
+        if torch.jit.is_tracing():
+            raise RuntimeError("step cannot be traced: a trace sees nothing of the kernels that it calls")
         if not self.causal:
             raise ValueError("step needs a causal layer: cached tokens do not see later ones")
         T, H, D = x.shape[0], self.num_heads, self.head_dim
