@@ -255,6 +255,8 @@ class LongNetAttention(torch.nn.Module):
         if not self.causal:
             raise ValueError("step needs a causal layer: cached tokens do not see later ones")
         T, H, D = x.shape[0], self.num_heads, self.head_dim
+        if T == 0:
+            return torch.empty_like(x)
         u = _layer_norm(self.ln_in, x)
         q, k, v = (_linear(m, u).view(T, H, D) for m in (self.q_proj, self.k_proj, self.v_proj))
         where = (cache.k[layer], cache.v[layer], batch.block_table, batch.seq_lens, batch.q_start)

@@ -26,3 +26,13 @@ def test_step_refuses_to_be_traced():
     x = torch.zeros(3, 64, dtype=torch.bfloat16)
     with pytest.raises(RuntimeError, match="trace"):
         torch.jit.trace(lambda t: layer.step(t, cache, batch), (x,), check_trace=False)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+def test_step_without_new_tokens(dtype):
+    """No sequence has a new token: no rows in, none out."""
+    layer = make(dtype=dtype)
+    cache = cache_for(layer, dtype=dtype)
+    batch = cache.extend(["a", "b"], [0, 0])
+    y = layer.step(torch.zeros(0, 64, dtype=dtype), cache, batch)
+    assert y.shape == (0, 64) and y.dtype == dtype
