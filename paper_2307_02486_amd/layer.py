@@ -244,16 +244,20 @@ class LongNetAttention(torch.nn.Module):
 
     @torch.no_grad()
     def step(self, x: torch.Tensor, cache, batch, layer: int = 0) -> torch.Tensor:
-        """The layer on new tokens x [T, E] of the sequences of `batch`, whose
+        """The layer on the new tokens x [T, E] of the sequences of `batch`, whose
         keys and values go to `cache` (a PagedCache and one of its batches, for
         the cache's layer `layer`) and which attend to what is there of their
         own sequence: what forward gives on whole sequences, row by row (up to
-        rounding: xPos is centred on the cache's centre).  Causal layers only,
-        without gradients and not under torch.jit.trace."""
+        rounding: xPos is centred on the cache's centre).  Rows of x past the
+        batch's tokens are of no sequence.  Causal layers only, without
+        gradients and not under torch.jit.trace."""
         if torch.jit.is_tracing():
             raise RuntimeError("step cannot be traced: a trace sees nothing of the kernels that it calls")
         if not self.causal:
             raise ValueError("step needs a causal layer: cached tokens do not see later ones")
+        if x.dim() != 2 or x.shape[0] < (batch.tokens or 0) or x.shape[1] != self.embed_dim:
+            raise ValueError(f"x must be [T, {self.embed_dim}] with the batch's {batch.tokens} new tokens in its "
+                             f"first rows, not {list(x.shape)}")
         T, H, D = x.shape[0], self.num_heads, self.head_dim
         if T == 0:
             return torch.empty_like(x)

@@ -10,11 +10,12 @@ import torch
 class Batch(NamedTuple):
     """The sequences of one step, as cache_append and paged_attn take them:
     int32 device tensors [B, max_pages], [B] and [B + 1], and the most new
-    tokens of a sequence."""
+    tokens of a sequence; and all the new tokens (None: not known)."""
     block_table: torch.Tensor
     seq_lens: torch.Tensor
     q_start: torch.Tensor
     max_new: int
+    tokens: int | None = None
 
 
 class PagedCache:
@@ -75,4 +76,4 @@ class PagedCache:
         start = torch.zeros(len(need) + 1, dtype=torch.int32)
         start[1:] = torch.tensor(new, dtype=torch.int32).cumsum(0)
         lens = torch.tensor(lengths, dtype=torch.int32)
-        return Batch(table.to(self.device), lens.to(self.device), start.to(self.device), max(new))
+        return Batch(table.to(self.device), lens.to(self.device), start.to(self.device), max(new), sum(new))

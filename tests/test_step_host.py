@@ -36,3 +36,24 @@ def test_step_without_new_tokens(dtype):
     batch = cache.extend(["a", "b"], [0, 0])
     y = layer.step(torch.zeros(0, 64, dtype=dtype), cache, batch)
     assert y.shape == (0, 64) and y.dtype == dtype
+
+
+@pytest.mark.parametrize("shape", [(4, 64), (0, 64), (1, 5, 64), (64,), (5, 32)], ids=str)
+def test_step_refuses_rows_that_are_not_the_batch_s_tokens(shape):
+    """With fewer rows than new tokens the rest of the sequences would be read as
+    the pool's memory was."""
+    layer = make()
+    cache = cache_for(layer)
+    batch = cache.extend(["a", "b"], [3, 2])
+    with pytest.raises(ValueError, match="5 new tokens"):
+        layer.step(torch.zeros(shape, dtype=torch.bfloat16), cache, batch)
+
+
+def test_batch_of_four_fields():
+    """A batch that a caller puts together (tensors of a captured step, say) need
+    not tell its tokens."""
+    from paper_2307_02486_amd.serving import Batch
+    i = torch.zeros(1, dtype=torch.int32)
+    batch = Batch(i[None], i, torch.zeros(2, dtype=torch.int32), 1)
+    layer = make()
+    assert layer.step(torch.zeros(0, 64, dtype=torch.bfloat16), cache_for(layer), batch).shape == (0, 64)
