@@ -30,6 +30,7 @@ from torch.autograd import forward_ad
 
 from .ops import (cache_append, dilated_attn, dilated_attn_bwd, layer_norm, layer_norm_bwd, paged_attn, qk_norm_xpos,
                   qk_norm_xpos_bwd, wgrad, xpos)
+from .serving import check_xpos
 
 
 def _plain() -> bool:
@@ -261,6 +262,8 @@ class LongNetAttention(torch.nn.Module):
         T, H, D = x.shape[0], self.num_heads, self.head_dim
         if T == 0:
             return torch.empty_like(x)
+        if self.use_xpos:
+            check_xpos(batch.block_table.shape[1] * cache.k[layer].shape[2], cache.center, *self.xpos_args[1:])
         u = _layer_norm(self.ln_in, x)
         q, k, v = (_linear(m, u).view(T, H, D) for m in (self.q_proj, self.k_proj, self.v_proj))
         where = (cache.k[layer], cache.v[layer], batch.block_table, batch.seq_lens, batch.q_start)

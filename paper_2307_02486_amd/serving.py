@@ -2,9 +2,36 @@
 the GPU for every layer, one page table for all of them, kept on the host."""
 from __future__ import annotations
 
+import ctypes
+import functools
+import math
 from typing import NamedTuple, Sequence
 
 import torch
+
+
+def xpos_span(gamma: float, scale_base: float) -> int:
+    """How far from the xPos centre a position may lie: its scale is at most 2^64
+    or at least 2^-64 there (dilated_attn_xpos, which takes the parameters in
+    float32)."""
+    gamma, scale_base = ctypes.c_float(gamma).value, ctypes.c_float(scale_base).value
+    if not (0.0 < gamma < math.inf and 0.0 < scale_base < math.inf):
+        raise ValueError("xPos needs a positive gamma and scale base")
+    per = abs(math.log2(gamma / (1.0 + gamma)))
+    span = int(64.0 * scale_base / per) + 1
+    while span / scale_base * per > 64.0:
+        span -= 1
+    return span
+
+
+@functools.lru_cache(maxsize=256)
+def check_xpos(reach: int, center: int, gamma: float, scale_base: float):
+    """Refuse a table of `reach` positions that xPos centred at `center` does not span."""
+    span = xpos_span(gamma, scale_base)
+    if not 0 <= center < reach or max(center, reach - 1 - center) > span:
+        raise ValueError(f"xPos with gamma {gamma} and scale base {scale_base} spans {span} positions to each side of "
+                         f"its centre, {2 * span + 1} positions in all: a table of {reach} with its centre at {center} "
+                         f"does not fit")
 
 
 class Batch(NamedTuple):
@@ -25,19 +52,27 @@ class PagedCache:
     per layer; page p of every layer belongs to the same sequence.  A sequence
     holds at most max_pages pages.  `center` is the xPos centre of every
     position (the middle of the reach by default), fixed for the cache's life.
+
+    Layers with xPos serve sequences of at most 2 xpos_span(gamma, scale_base) + 1
+    positions (36261 with their defaults), and the whole table has to fit.  xpos,
+    the layers' (gamma, scale_base), checks that here; otherwise their first step
+    refuses.
     """
 
     def __init__(self, num_pages: int, page_size: int, max_pages: int, num_heads: int, head_dim: int,
-                 layers: int = 1, center: int | None = None, device=None, dtype=torch.bfloat16):
+                 layers: int = 1, center: int | None = None, device=None, dtype=torch.bfloat16,
+                 xpos: tuple | None = None):
         if page_size < 1 or page_size & (page_size - 1):
             raise ValueError("page_size must be a power of two")
         if num_pages < 1 or max_pages < 1 or layers < 1:
             raise ValueError("num_pages, max_pages and layers must be at least 1")
+        self.center = max_pages * page_size // 2 if center is None else center
+        if xpos is not None:
+            check_xpos(max_pages * page_size, self.center, *xpos)
         shape = (num_pages, num_heads, page_size, head_dim)
         self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
         self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
         self.page_size, self.max_pages = page_size, max_pages
-        self.center = max_pages * page_size // 2 if center is None else center
         self.device = self.k[0].device
         self._free = list(range(num_pages - 1, -1, -1))
         self._pages: dict = {}

@@ -57,3 +57,47 @@ def test_batch_of_four_fields():
     batch = Batch(i[None], i, torch.zeros(2, dtype=torch.int32), 1)
     layer = make()
     assert layer.step(torch.zeros(0, 64, dtype=torch.bfloat16), cache_for(layer), batch).shape == (0, 64)
+
+
+def append_accepts(reach, center, gamma, scale_base):
+    """Whether the library's append takes a table of `reach` positions (no tokens: nothing is launched)."""
+    from paper_2307_02486_amd import _lib
+    lib = _lib.load()
+    cache = _lib.PagedCacheArgs(0x1000000, 0x8000000, 0x3000000, 0x3100000, 0x3200000, 1, 1, reach)
+    rc = lib.dilated_attn_cache_append(None, None, None, None, None, None, cache, 0, 1, 2, 2, 32, 64, 64, 64, 0.0, 1,
+                                       center, 10000.0, gamma, scale_base, 1, None)
+    assert _lib.ERRORS[rc] in ("DA_OK", "DA_EINVAL")
+    return rc == 0
+
+
+@pytest.mark.parametrize("gamma, scale_base", [(0.4, 512.0), (0.4, 37.5), (2.0, 100.0), (0.1, 8192.0), (0.7, 0.3)])
+def test_the_reach_of_xpos_is_the_library_s(gamma, scale_base):
+    from paper_2307_02486_amd.serving import xpos_span
+    span = xpos_span(gamma, scale_base)
+    assert append_accepts(2 * span + 1, span, gamma, scale_base)
+    assert not append_accepts(2 * span + 2, span, gamma, scale_base)
+    assert not append_accepts(2 * span + 2, span + 1, gamma, scale_base)
+
+
+def test_caches_beyond_the_reach_of_xpos():
+    """With the layer's defaults a table of 566 pages of 64 is the largest: one
+    more is refused before the pool is there, and by step for a cache that was
+    not told of xPos; a layer without xPos takes any."""
+    for pages in (567, 1024):
+        with pytest.raises(ValueError, match="36261 positions"):
+            PagedCache(4, 64, pages, 2, 32, device="cpu", xpos=(0.4, 512.0))
+    for center in (-1, 64, 50):
+        with pytest.raises(ValueError, match="centre"):
+            PagedCache(4, 8, 8, 2, 32, device="cpu", center=center, xpos=(0.4, 1.0))
+    assert PagedCache(4, 64, 566, 2, 32, device="cpu", xpos=(0.4, 512.0)).center == 566 * 32
+    layer = make()
+    cache = cache_for(layer, page_size=64, max_pages=567)
+    batch = cache.extend(["a"], [1])
+    x = torch.zeros(1, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="36261 positions"):
+        layer.step(x, cache, batch)
+    with pytest.raises(RuntimeError, match="GPU only"):  # past this check
+        make(use_xpos=False, dtype=torch.float32).step(x.float(), cache, batch)
+    cache = cache_for(layer, page_size=64, max_pages=566)
+    with pytest.raises(RuntimeError, match="GPU only"):
+        make(dtype=torch.float32).step(x.float(), cache, cache.extend(["a"], [1]))
