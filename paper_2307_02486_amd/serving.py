@@ -37,12 +37,16 @@ def check_xpos(reach: int, center: int, gamma: float, scale_base: float):
 class Batch(NamedTuple):
     """The sequences of one step, as cache_append and paged_attn take them:
     int32 device tensors [B, max_pages], [B] and [B + 1], and the most new
-    tokens of a sequence; and all the new tokens (None: not known)."""
+    tokens of a sequence; and all the new tokens (None: not known), the sequences
+    with their new tokens, and the cache's number of the step."""
     block_table: torch.Tensor
     seq_lens: torch.Tensor
     q_start: torch.Tensor
     max_new: int
     tokens: int | None = None
+    sequences: tuple = ()
+    new: tuple = ()
+    number: int = 0
 
 
 class PagedCache:
@@ -77,6 +81,8 @@ class PagedCache:
         self._free = list(range(num_pages - 1, -1, -1))
         self._pages: dict = {}
         self._length: dict = {}
+        self._last: dict = {}  # the step in which a sequence was last extended
+        self._number = 0
 
     def length(self, sequence) -> int:
         """Tokens that the cache holds of a sequence (any hashable name)."""
@@ -86,11 +92,28 @@ class PagedCache:
         """Forget a sequence; its pages go back to the pool."""
         self._free += self._pages.pop(sequence, [])
         self._length.pop(sequence, None)
+        self._last.pop(sequence, None)
+
+    def retract(self, batch: Batch):
+        """Take back the extend that gave this batch: its sequences have their
+        earlier lengths again, and pages taken for it go back to the pool.  Only
+        while no other extend of one of them, nor a release, came since."""
+        if not batch.sequences or any(self._last.get(s) != batch.number for s in batch.sequences):
+            raise ValueError("not the last batch of all its sequences")
+        for s, n in zip(batch.sequences, batch.new):
+            self._length[s] -= n
+            pages, keep = self._pages[s], -(-self._length[s] // self.page_size)
+            self._free += reversed(pages[keep:])
+            del pages[keep:], self._last[s]
+            if self._length[s] == 0:
+                self.release(s)
 
     def extend(self, sequences: Sequence, new: Sequence[int]) -> Batch:
         """Room for `new` more tokens of each sequence (named for the first time,
         it is empty), and the batch of a step in which they come.  Every layer
-        then takes this batch once."""
+        then takes this batch once; if a layer does not (it raises, say), the
+        batch has to be taken back, or the next one attends to tokens that are
+        not there."""
         if len(set(sequences)) != len(sequences) or len(new) != len(sequences) or not len(new):
             raise ValueError("sequences must be different ones, with a number of new tokens each")
         if min(new) < 0:
@@ -102,13 +125,15 @@ class PagedCache:
             raise ValueError(f"a sequence of {max(lengths)} tokens is beyond {self.max_pages} pages of {self.page_size}")
         if sum(short) > len(self._free):
             raise RuntimeError(f"{sum(short)} pages are needed and {len(self._free)} are free")
+        self._number += 1
         table = torch.zeros((len(need), self.max_pages), dtype=torch.int32)
         for i, (s, n, more) in enumerate(zip(sequences, lengths, short)):
             pages = self._pages.setdefault(s, [])
             pages += [self._free.pop() for _ in range(more)]
-            self._length[s] = n
+            self._length[s], self._last[s] = n, self._number
             table[i, : len(pages)] = torch.tensor(pages, dtype=torch.int32)
         start = torch.zeros(len(need) + 1, dtype=torch.int32)
         start[1:] = torch.tensor(new, dtype=torch.int32).cumsum(0)
         lens = torch.tensor(lengths, dtype=torch.int32)
-        return Batch(table.to(self.device), lens.to(self.device), start.to(self.device), max(new), sum(new))
+        return Batch(table.to(self.device), lens.to(self.device), start.to(self.device), max(new), sum(new),
+                     tuple(sequences), tuple(new), self._number)

@@ -101,3 +101,59 @@ def test_caches_beyond_the_reach_of_xpos():
     cache = cache_for(layer, page_size=64, max_pages=566)
     with pytest.raises(RuntimeError, match="GPU only"):
         make(dtype=torch.float32).step(x.float(), cache, cache.extend(["a"], [1]))
+
+
+def state(cache):
+    return {s: (cache.length(s), tuple(p)) for s, p in cache._pages.items()}, sorted(cache._free)
+
+
+def test_a_batch_whose_step_failed_is_taken_back():
+    """Lengths and pages are as before extend: the next step does not attend to
+    tokens that were never written."""
+    layer = make()
+    cache = cache_for(layer)
+    cache.extend(["a", "b"], [5, 4])
+    before = state(cache)
+    batch = cache.extend(["b", "new", "a"], [5, 6, 0])
+    assert cache.length("new") == 6 and cache.length("b") == 9
+    with pytest.raises(ValueError):
+        layer.step(torch.zeros(3, 64, dtype=torch.bfloat16), cache, batch)
+    cache.retract(batch)
+    assert state(cache) == before and cache.length("new") == 0
+    with pytest.raises(ValueError):
+        cache.retract(batch)  # once
+    later = cache.extend(["b"], [1])
+    assert later.seq_lens.tolist() == [5]
+    batch = cache.extend(["b"], [2])
+    cache.extend(["b"], [1])
+    after = state(cache)
+    with pytest.raises(ValueError):
+        cache.retract(batch)  # others came since
+    cache.release("a")
+    with pytest.raises(ValueError):
+        cache.retract(later._replace(sequences=("b", "a"), new=(1, 1)))
+    assert state(cache)[0]["b"] == after[0]["b"]
+
+
+def test_only_whole_batches_are_taken_back():
+    from paper_2307_02486_amd.serving import Batch
+    cache = cache_for(make())
+    cache.extend(["a"], [3])
+    one = cache.extend(["a", "b"], [1, 2])
+    cache.release("b")
+    before = state(cache)
+    with pytest.raises(ValueError):
+        cache.retract(one)
+    assert state(cache) == before
+    with pytest.raises(ValueError):
+        cache.retract(Batch(one.block_table, one.seq_lens, one.q_start, 1))
+
+
+def test_a_sequence_of_the_same_name_and_length_is_another():
+    cache = cache_for(make())
+    batch = cache.extend(["a"], [3])
+    cache.release("a")
+    cache.extend(["a"], [3])
+    with pytest.raises(ValueError):
+        cache.retract(batch)
+    assert cache.length("a") == 3
