@@ -152,8 +152,9 @@ int dilated_attn_cache_append(const void* q, const void* k, const void* v, const
  * themselves (at most 4 new ones) mix float32 partial rows, otherwise a
  * pattern's rows are kept as in dilated_attn_fwd; out rounded once.  DA_F32
  * computes in float32 throughout.  Results are finite under the conditions of
- * dilated_attn_fwd for the sequence's own tokens; what lies in the pool beyond
- * a sequence's length is never used, whatever it holds.  The same call gives
+ * dilated_attn_fwd for the sequence's own tokens; a row that sees a key whose
+ * score is NaN or plus infinity is NaN in out and lse.  What lies in the pool
+ * beyond a sequence's length is never used, whatever it holds.  The same call gives
  * the same bits every time; keys are split by the sizes of the call, so a
  * sequence alone and in a batch can differ by the rounding of its sums.
  * Outputs and workspace must not overlap each other, q or the cache.

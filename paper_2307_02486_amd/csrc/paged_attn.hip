@@ -1096,13 +1096,24 @@ __device__ inline void put8(u16* p, const f32x8& v) {
 }
 __device__ inline void put8(float* p, const f32x8& v) { *reinterpret_cast<f32x8*>(p) = v; }
 
+// The bits of x, as the compiler cannot see through.  It takes floats for numbers
+// (and a comparison of their bits for one of floats): a NaN, that of a row with a
+// score that is NaN or plus infinity, may compare like any number.
+__device__ inline uint32_t bits_of(float x) {
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  asm("" : "+v"(u));
+  return u;
+}
+// Whether a record marks a row that is not there.
+__device__ inline bool no_row(float x) { return bits_of(x) == 0xff800000u; }
+
 // A running mixture: m the largest log-sum-exp (log2 units) so far, l and acc
 // the sums of the weights 2^(x - m) and of the weighted rows.
 struct Mix {
   float m = -INFINITY, l = 0.0f;
   f32x8 acc = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
   __device__ void add(float x, float scale, const f32x8& o) {  // row o * scale with weight 2^x
-    if (x == -INFINITY) return;  // no visible key, or none with a finite score: the row is not there
+    if (no_row(x)) return;  // no visible key, or none with a finite score: the row is not there
     const float mn = fmaxf(m, x);
     const float f0 = __builtin_amdgcn_exp2f(m - mn), f1 = __builtin_amdgcn_exp2f(x - mn);
     m = mn;
@@ -1128,8 +1139,10 @@ template <typename T, int D>
 __device__ inline void put_row(const PagedArgs& a, int tok, int head, int ch, const Mix& x) {
   const float inv = x.l > 0.0f ? 1.0f / x.l : 0.0f;
   put8(static_cast<T*>(a.out) + (static_cast<int64_t>(tok) * a.H + head) * D + ch * 8, x.acc * inv);
+  // l is zero where no partial was added, and there only: the largest adds one.
   if (ch == 0)
-    a.lse[static_cast<int64_t>(head) * a.T + tok] = x.l > 0.0f ? (x.m + __builtin_amdgcn_logf(x.l)) * kLn2 : -INFINITY;
+    a.lse[static_cast<int64_t>(head) * a.T + tok] =
+        bits_of(x.l) != 0 ? (x.m + __builtin_amdgcn_logf(x.l)) * kLn2 : -INFINITY;
 }
 
 // Single tokens: a wave per row (or a workgroup, kTogether), D/8 lanes across a
@@ -1250,7 +1263,7 @@ __device__ inline void join_tiles(const PagedArgs& a, int group) {
       }
 #pragma unroll
       for (int i = 0; i < kPats; ++i) {
-        if (rec[i][0] == -INFINITY) continue;
+        if (no_row(rec[i][0])) continue;
         f32x8 f;
 #pragma unroll
         for (int c = 0; c < 8; ++c) f[c] = static_cast<float>(o[i][c]);
