@@ -30,8 +30,7 @@ constexpr int kHeadThreads = 256;
 constexpr int kHeadWaves = kHeadThreads / 64;
 
 // Per pair i of kPairs: quarter turns per position and log2 zeta_i /
-// scale_base, in float64 (they multiply positions of up to millions).  Without
-// a rotation both are zero.
+// scale_base, in float64 (they multiply positions of up to millions).
 template <int kPairs>
 struct HeadTab {
   double turn[kPairs];
@@ -154,7 +153,10 @@ __device__ inline int sequence_of(const int32_t* start, int B, int tok, int lane
   return n > B ? -1 : n - 1;
 }
 
-template <typename T, int D, bool kCache>
+// kRotate false (with a cache): no rotation.  (Not one of zero angles: those would
+// make NaN of an infinite element's neighbour.  Nor a choice in the loop: three
+// prompts into a cache 29.2 us instead of 28.5.)
+template <typename T, int D, bool kCache, bool kRotate>
 __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a, HeadTab<D / 2> tab) {
   typedef typename Raw8<T>::type Raw;
   constexpr int kLanes = D / 8;        // lanes per row
@@ -206,7 +208,9 @@ __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a, HeadTab
   } else {
     pos = static_cast<int>(tok) - static_cast<int>(a.fn.div(static_cast<uint32_t>(tok)) * a.fn.d);
   }
-  const Rotation rt = rotation<D / 2>(turn, l2z, live ? pos : 0, live ? pos - a.center : 0, share[wv], lane, ch);
+  Rotation rt;
+  if constexpr (kRotate)
+    rt = rotation<D / 2>(turn, l2z, live ? pos : 0, live ? pos - a.center : 0, share[wv], lane, ch);
   const bool norm_q = a.qw != nullptr, norm_k = a.kw != nullptr;
   float wq[8], wk[8];
 #pragma unroll
@@ -236,11 +240,16 @@ __global__ __launch_bounds__(kHeadThreads) void heads_fwd(HeadFwdArgs a, HeadTab
       const float rstd = (is_q ? norm_q : norm_k) ? __builtin_amdgcn_rsqf(ss * (1.0f / D) + a.eps) : 1.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float s = is_q ? rt.up[e] : rt.down[e];
         const float n0 = f[2 * e] * rstd * (is_q ? wq[2 * e] : wk[2 * e]);
         const float n1 = f[2 * e + 1] * rstd * (is_q ? wq[2 * e + 1] : wk[2 * e + 1]);
-        y[2 * e] = s * (n0 * rt.cs[e] - n1 * rt.sn[e]);
-        y[2 * e + 1] = s * (n0 * rt.sn[e] + n1 * rt.cs[e]);
+        if constexpr (kRotate) {
+          const float s = is_q ? rt.up[e] : rt.down[e];
+          y[2 * e] = s * (n0 * rt.cs[e] - n1 * rt.sn[e]);
+          y[2 * e + 1] = s * (n0 * rt.sn[e] + n1 * rt.cs[e]);
+        } else {
+          y[2 * e] = n0;
+          y[2 * e + 1] = n1;
+        }
       }
       Raw o;
       pack(y, o);
@@ -407,13 +416,13 @@ template <int kPairs>
 const HeadTab<kPairs>& make_tab(const HeadRotation& r) {
   static thread_local HeadRotation known{};
   static thread_local HeadTab<kPairs> t{};
-  if (r.rotate != known.rotate || r.base != known.base || r.gamma != known.gamma || r.scale_base != known.scale_base) {
+  if (r.base != known.base || r.gamma != known.gamma || r.scale_base != known.scale_base) {
     known = r;
-    const double l2b = r.rotate ? std::log2(static_cast<double>(r.base)) : 0.0, gamma = r.gamma;
+    const double l2b = std::log2(static_cast<double>(r.base)), gamma = r.gamma;
     for (int i = 0; i < kPairs; ++i) {
       const double x = static_cast<double>(i) / kPairs;  // 2 i / D
-      t.turn[i] = r.rotate ? std::exp2(-x * l2b) * 0.63661977236758134308 : 0.0;  // 2 / pi
-      t.l2z[i] = r.rotate ? std::log2((x + gamma) / (1.0 + gamma)) / r.scale_base : 0.0;
+      t.turn[i] = std::exp2(-x * l2b) * 0.63661977236758134308;  // 2 / pi
+      t.l2z[i] = std::log2((x + gamma) / (1.0 + gamma)) / r.scale_base;
     }
   }
   return t;
@@ -421,8 +430,14 @@ const HeadTab<kPairs>& make_tab(const HeadRotation& r) {
 
 template <typename T, int D, bool kCache>
 void launch_fwd_d(const HeadFwdArgs& a, const HeadRotation& r, hipStream_t stream) {
-  hipLaunchKernelGGL((heads_fwd<T, D, kCache>), grid_of((a.T + kHeadWaves - 1) / kHeadWaves), dim3(kHeadThreads), 0,
-                     stream, a, make_tab<D / 2>(r));
+  const dim3 grid = grid_of((a.T + kHeadWaves - 1) / kHeadWaves), threads(kHeadThreads);
+  if constexpr (kCache) {
+    if (!r.rotate) {
+      hipLaunchKernelGGL((heads_fwd<T, D, true, false>), grid, threads, 0, stream, a, HeadTab<D / 2>{});
+      return;
+    }
+  }
+  hipLaunchKernelGGL((heads_fwd<T, D, kCache, true>), grid, threads, 0, stream, a, make_tab<D / 2>(r));
 }
 
 template <typename T, bool kCache>
