@@ -77,6 +77,20 @@ class XPosFunction(torch.autograd.Function):
         return xpos(dy.contiguous(), sign, True, center, base, gamma, scale_base), None, None, None, None, None
 
 
+class QKNormXPosGradFunction(torch.autograd.Function):
+    """The gradients of QKNormXPosFunction where they are recorded (create_graph):
+    they have no derivative, and one that is asked for is an error rather than a
+    missing term."""
+
+    @staticmethod
+    def forward(ctx, *args):
+        return qk_norm_xpos_bwd(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients of the head norms cannot be differentiated")
+
+
 class QKNormXPosFunction(torch.autograd.Function):
     """Differentiable RMS norm of the heads of q and k and xPos, in one pass each way."""
 
@@ -89,7 +103,8 @@ class QKNormXPosFunction(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dq, dk):
-        return (*qk_norm_xpos_bwd(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, *ctx.args), *(None,) * 5)
+        grads = QKNormXPosGradFunction.apply if torch.is_grad_enabled() else qk_norm_xpos_bwd
+        return (*grads(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors, *ctx.args), *(None,) * 5)
 
 
 def _weight_grads(dy2: torch.Tensor, x2: torch.Tensor):
