@@ -1035,6 +1035,7 @@ __global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps
   __shared__ SmemMixed<D> sm;
   touch(a);
   const uint32_t idx = launch_index();  // below 2^31, as the items and the launch are
+  if (idx >= static_cast<uint32_t>(a.grid)) return;  // its items are another's
   for (uint32_t index = idx, items = idx + 1; index < items; index += a.grid) {
     const int item = static_cast<int>(index);
     const int tid = thread_id(), lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
