@@ -1029,9 +1029,10 @@ __global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_mixed(Page
 // sizes allow: 16 sequences, one of them with 1000 new tokens, 50 -> 38 us; 40
 // with one of 500, 102 -> 63; 64 with one of 2048, 104 -> 74.  Counted again for
 // each item: held in registers over an item the counts would spill, and most
-// workgroups have one.  (The loop takes more registers than paged_mixed.)
+// workgroups have one.  (No least number of workgroups a CU: asking for 1, 2 or 3
+// of them is within 1 % at heads of 32, 64 and 128.)
 template <int D>
-__global__ __launch_bounds__(kPgThreads, D == 64 ? 3 : 1) void paged_mixed_steps(PagedArgs a) {
+__global__ __launch_bounds__(kPgThreads) void paged_mixed_steps(PagedArgs a) {
   __shared__ SmemMixed<D> sm;
   touch(a);
   const uint32_t idx = launch_index();  // below 2^31, as the items and the launch are
