@@ -11,10 +11,13 @@
 // a wave steps through the token's heads, so that a lane keeps its four pairs,
 // whose angles and scales (float64 products and a reduction to a quarter turn: as
 // much work as a head's row) are formed once per token instead of once per head.
-// Sums over a row are DPP exchanges within 16 lanes.  All bound by HBM at training
-// sizes (gradients of 4 x 8192 tokens of 12 + 12 heads of 64: 302 MB in 53 us, 5.7
-// TB/s; three prompts of 11800 tokens of 24 heads of 128 into a cache: 145 MB in 25
-// us, 5.8 TB/s), by the launch at decoding sizes (5.3 us).
+// Sums over a row are DPP exchanges within 16 lanes.  Bound by memory at training
+// sizes: on inputs that no cache holds, gradients of 4 x 8192 tokens of 12 + 12 heads
+// of 64 move 302 MB in 55 us (5.5 TB/s; float32 604 MB in 112), three prompts of 11800
+// tokens of 24 heads of 128 into a cache 145 MB in 29 us (4.9 TB/s; float32 290 MB in
+// 53).  The prompts again and again on the same inputs take 25 us: part of the
+// 145 MB then comes from the Infinity Cache.  Bound by the launch at decoding sizes
+// (5.3 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -23,10 +23,18 @@
 // query_tiles: a workgroup is 128 kept query rows of one (sequence, head,
 // segment) of a pattern against 64-key tiles in LDS.  Bound by the matrix cores
 // and the softmax's vector work where a launch is long (8192 tokens of 12 heads of
-// 64, dense: 103 GFLOP in 155 us), by the start-up of an item (8 us) and the tail
+// 64, dense: 103 GFLOP in 150 us), by the start-up of an item (8 us) and the tail
 // where it is short (4096 tokens at 28672, five patterns: 31.9 GFLOP in 59 us).
 // Both write normalised partial rows with their log-sum-exps; paged_join mixes
 // a row's partials.
+//
+// Fewer bits than float32, in bf16 calls only, each as in the forward pass:
+// probabilities are rounded to bf16 for the product with V, as its matrix
+// instruction takes them (their sums stay float32), and partial rows of tiles are
+// kept as fp16 times a power of two per row, half the bytes that the join reads
+// again (those of single tokens are float32).  An output as a whole is then within
+// 0.0020 to 0.0024 of float64's, relatively, where float32 arithmetic rounded to bf16
+// once is within 0.0016 to 0.0017.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -467,7 +475,7 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
       for (int e = 0; e < 4; ++e) {
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], c2, -m_run)) * count[u][e];
         l_run += p;
-        pb[4 * u + e] = (__bf16)p;
+        pb[4 * u + e] = (__bf16)p;  // for the product alone
       }
     // V through the wave's own LDS tile, to be read transposed (LDS operations
     // of a wave complete in order: no wait between).
@@ -867,7 +875,8 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
         // for the tile's maximum: a tile whose probabilities of half a row sum to
         // more than kSumSlack (or overflow: the first tile's do) has its scores
         // still in registers and forms them again with its maximum as reference.
-        // Probabilities above 1 are held by bf16 and float32 as well as those below.
+        // Probabilities above 1 are held by bf16 (see above) and float32 as well as
+        // those below.
         bf16x8 pb[2][2];
         float lt;
         auto probabilities = [&] {
@@ -1213,7 +1222,10 @@ __device__ inline void join_singles(const PagedArgs& a, int group) {
 
 // Tokens of tiles, and those of no sequence: D/8 lanes a row, head by head and
 // token by token, the loads of all patterns before their use.  kPats bounds the
-// patterns at compile time; kSubs such groups of lanes share a row, each with
+// patterns at compile time: 5, the length of the paper's list, or all 16, whose
+// records and rows in flight take 186 registers instead of 76 (lists of up to 5 with
+// the second form: 4096 tokens at 28672 79 us instead of 65, 512 at 31500 30 instead
+// of 26; of six patterns it takes 27 us of 90, of eight 26 of 71).  kSubs such groups of lanes share a row, each with
 // every kSubs-th split.
 template <int D, int kPats, int kSubs>
 __device__ inline void join_tiles(const PagedArgs& a, int group) {

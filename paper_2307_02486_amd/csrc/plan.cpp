@@ -280,7 +280,10 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
     // positions of one fill m / (128 r) tiles, rounded up.  (One sequence of 512
     // tokens, the paper's patterns: 14 tiles a head where 9 are there; with 27
     // the workgroups without work held up the others.)  Units are dealt to the
-    // XCDs: up to 16 tiles, fewer where there would not be eight units each.
+    // XCDs: up to 16 tiles, fewer where there would not be eight units each.  (At most
+    // 1, 4, 16, 64 tiles: 2048 tokens at 30000, dense, 253, 251, 248, 250 us, 4096 at
+    // 28672 64.5, 64.6, 65.6, 65.6, 8192 dense 141, 141, 147, 148.  Two units each, eight,
+    // 32: 270, 248, 256 us; 68.8, 65.6, 64.7; 146, 147, 140.)
     const int64_t some = std::min(B, T), segments = (T - some) / t.w + 2 * some, fill = int64_t{t.r} * kPagedRows;
     const int64_t tiles = std::min(T, segments + (T - segments) / fill);
     if (tiles >= kMost / H / ts) return DA_EINVAL;
@@ -296,8 +299,11 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   if (one_items >= kMost || one_items + items + 16 * H * p.tile_slots >= kMost || (T + 1) * H >= kMost) return DA_EINVAL;
   p.one_items = one_items;
   p.tile_items = items;
-  // Where the sizes allow many more items than they let expect, the launch is
-  // as large as the latter.
+  // Where the sizes allow more than one and a half times as many items as they let
+  // expect, the launch is as large as the latter.  (Every item that the sizes allow
+  // against that, at 1.5 times as many: two prompts of 8192 160 us, 167; 1.7: four
+  // chunks of 4096 162, 166; 2.3: two chunks of 300 30.4, 29.0, three of 2000 85.5, 86.7;
+  // 4.7: 16 sequences with 1000 new tokens of one 43.5, 33.1; 10: 64 with 2048 127, 87.)
   const int64_t likely = std::max<int64_t>(1024, expected);
   p.steps = !p.all_few && 2 * (one_items + items) > 3 * likely;
   p.grid = p.steps ? (likely + 7) / 8 * 8 : one_items + items;
