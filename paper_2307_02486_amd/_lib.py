@@ -1,5 +1,5 @@
-"""ctypes view of libdilated_attn.so (the C ABI of include/dilated_attn.h
-and include/dilated_attn_paged.h).
+"""ctypes view of libdilated_attn.so (the C ABI of include/dilated_attn.h,
+include/dilated_attn_paged.h and include/dilated_attn_compressed.h).
 
 Argument marshalling only.  torch is imported first so that the library binds
 to the HIP runtime torch already loaded (one runtime per process).
@@ -40,6 +40,10 @@ class PagedCacheArgs(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
                 ("seq_lens", ctypes.c_void_p), ("q_start", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
                 ("page_size", ctypes.c_int64), ("max_pages", ctypes.c_int64)]
+
+
+class PagedCacheF8Args(ctypes.Structure):
+    _fields_ = [("pages", PagedCacheArgs), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class DilatedAttnError(RuntimeError):
@@ -105,6 +109,21 @@ def load():
     lib.dilated_attn_paged_fwd.argtypes = [vp, cache, vp, vp] + [i64] * 7 + [ctypes.POINTER(Pattern), i64, i64, f32,
                                                                             vp, u64, vp]
     lib.dilated_attn_paged_fwd.restype = ctypes.c_int
+    cache8 = ctypes.POINTER(PagedCacheF8Args)
+    lib.dilated_attn_cache_append_f8.argtypes = ([vp] * 6 + [cache8] + [i64] * 8
+                                                 + [f32, i64, i64, f32, f32, f32, i64, vp])
+    lib.dilated_attn_cache_append_f8.restype = ctypes.c_int
+    lib.dilated_attn_paged_fwd_f8.argtypes = ([vp, cache8, vp, vp] + [i64] * 7
+                                              + [ctypes.POINTER(Pattern), i64, i64, f32, vp, u64, vp])
+    lib.dilated_attn_paged_fwd_f8.restype = ctypes.c_int
+    lib.dilated_attn_page_weights_workspace.argtypes = [i64] * 8 + [ctypes.POINTER(Pattern), i64, i64,
+                                                                    ctypes.POINTER(u64)]
+    lib.dilated_attn_page_weights_workspace.restype = ctypes.c_int
+    lib.dilated_attn_page_weights.argtypes = [vp, vp, cache8, vp] + [i64] * 6 + [ctypes.POINTER(Pattern), i64, i64, f32,
+                                                                               vp, u64, vp]
+    lib.dilated_attn_page_weights.restype = ctypes.c_int
+    lib.dilated_attn_evict_pages.argtypes = [vp] * 6 + [i64] * 7 + [vp]
+    lib.dilated_attn_evict_pages.restype = ctypes.c_int
     lib.dilated_attn_strerror.argtypes = [ctypes.c_int]
     lib.dilated_attn_strerror.restype = ctypes.c_char_p
     lib.dilated_attn_profile_begin.argtypes = [i64]

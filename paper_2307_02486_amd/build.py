@@ -19,7 +19,7 @@ LIB_NAME = "libdilated_attn.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 
 HIP_SOURCES = ["attn_fwd.hip", "combine.hip", "attn_bwd.hip", "xpos.hip", "wgrad.hip", "layernorm.hip", "heads.hip",
-               "paged_attn.hip", "noalloc.hip"]
+               "paged_attn.hip", "cache8.hip", "pages.hip", "noalloc.hip"]
 HOST_SOURCES = ["plan.cpp", "api.cpp"]
 
 ARCH = "gfx950"

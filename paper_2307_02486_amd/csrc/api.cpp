@@ -7,7 +7,7 @@
 #include <cstdint>
 #include <vector>
 
-#include "../../include/dilated_attn_paged.h"
+#include "../../include/dilated_attn_compressed.h"
 #include "kernels.h"
 #include "paged.h"
 #include "plan.h"
@@ -382,9 +382,9 @@ int dilated_attn_qk_norm_xpos_bwd(const void* dqo, const void* dko, const void* 
 
 namespace {
 
-// Cache sizes that both paged calls take; the rows fit 32-bit indices.
-bool cache_ok(int64_t B, int64_t Hkv, const da_paged_cache_t* c) {
-  if (!c || !c->k || !c->v || !c->block_table || !c->seq_lens || !c->q_start) return false;
+// Cache sizes that the paged calls take; the rows fit 32-bit indices.
+bool cache_ok(int64_t B, int64_t Hkv, const da_paged_cache_t* c, bool values = true) {
+  if (!c || !c->k || (values && !c->v) || !c->block_table || !c->seq_lens || !c->q_start) return false;
   constexpr int64_t kMost = int64_t{1} << 31;
   return B >= 1 && B < kMost && c->page_size >= 1 && c->page_size <= (int64_t{1} << 16) &&
          (c->page_size & (c->page_size - 1)) == 0 && c->max_pages >= 1 && c->max_pages < kMost / c->page_size &&
@@ -399,13 +399,21 @@ da::PagedCache paged_cache(const da_paged_cache_t* c) {
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-}  // namespace
+// The bytes of a cache's keys (or values), and of an 8-bit cache's scales of them.
+uint64_t pool_bytes(const da_paged_cache_t* c, int64_t Hkv, int64_t row_bytes) {
+  return static_cast<uint64_t>(c->num_pages * c->page_size * Hkv) * static_cast<uint64_t>(row_bytes);
+}
+uint64_t scale_bytes(const da_paged_cache_t* c, int64_t Hkv) {
+  return static_cast<uint64_t>(c->num_pages * Hkv) *
+         static_cast<uint64_t>(c->page_size / std::min<int64_t>(c->page_size, DA_CACHE_BLOCK));
+}
 
-int dilated_attn_cache_append(const void* q, const void* k, const void* v, const void* qw, const void* kw, void* qo,
-                              const da_paged_cache_t* cache, int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D,
-                              int64_t q_stride, int64_t k_stride, int64_t v_stride, float eps, int64_t rotate,
-                              int64_t center, float base, float gamma, float scale_base, int64_t dtype,
-                              void* stream) {
+// The append to a cache of the call's type, or (with scales) in 8 bits.
+int cache_append(const void* q, const void* k, const void* v, const void* qw, const void* kw, void* qo,
+                 const da_paged_cache_t* cache, const da_paged_cache_f8_t* f8, int64_t T, int64_t B, int64_t H,
+                 int64_t Hkv, int64_t D, int64_t q_stride, int64_t k_stride, int64_t v_stride, float eps,
+                 int64_t rotate, int64_t center, float base, float gamma, float scale_base, int64_t dtype,
+                 void* stream) {
   const int64_t strides[3] = {k_stride, v_stride, q_stride}, heads[3] = {Hkv, Hkv, H};
   if (const int rc = head_shapes(T, H, Hkv, D, dtype, strides, heads, q ? 3 : 2); rc != DA_OK) return rc;
   if (!cache_ok(B, Hkv, cache) || (T > 0 && (!k || !v)) || (q != nullptr) != (qo != nullptr)) return DA_EINVAL;
@@ -415,21 +423,88 @@ int dilated_attn_cache_append(const void* q, const void* k, const void* v, const
                         static_cast<const void*>(cache->v)})
     if (!aligned16(p)) return DA_EALIGN;
   if (!aligned4(cache->block_table) || !aligned4(cache->seq_lens) || !aligned4(cache->q_start)) return DA_EALIGN;
+  if (f8 && (!f8->k_scale || !f8->v_scale || T >= (int64_t{1} << 30))) return DA_EINVAL;
   const int64_t es = dtype == DA_BF16 ? 2 : 4;
-  const uint64_t wb = static_cast<uint64_t>(D * es),
-                 cb = static_cast<uint64_t>(cache->num_pages * cache->page_size * Hkv) * static_cast<uint64_t>(D * es);
+  const uint64_t wb = static_cast<uint64_t>(D * es), cb = pool_bytes(cache, Hkv, f8 ? D : D * es),
+                 sb = f8 ? scale_bytes(cache, Hkv) : 0;
   const Span ins[8] = {{q, q ? strided_bytes(T, H * D, q_stride, es) : 0}, {k, strided_bytes(T, Hkv * D, k_stride, es)},
                        {v, strided_bytes(T, Hkv * D, v_stride, es)}, {qw, qw ? wb : 0}, {kw, kw ? wb : 0},
                        {cache->block_table, static_cast<uint64_t>(B) * cache->max_pages * 4},
                        {cache->seq_lens, static_cast<uint64_t>(B) * 4}, {cache->q_start, static_cast<uint64_t>(B + 1) * 4}};
-  const Span outs[3] = {{qo, qo ? static_cast<uint64_t>(T * H * D * es) : 0}, {cache->k, cb}, {cache->v, cb}};
-  if (any_overlap(outs, 3, ins, 8)) return DA_EINVAL;
+  const Span outs[5] = {{qo, qo ? static_cast<uint64_t>(T * H * D * es) : 0}, {cache->k, cb}, {cache->v, cb},
+                        {f8 ? f8->k_scale : nullptr, sb}, {f8 ? f8->v_scale : nullptr, sb}};
+  if (any_overlap(outs, f8 ? 5 : 3, ins, 8)) return DA_EINVAL;
   if (T == 0) return DA_OK;
   const da::QkNormCall c{q, k, qw, kw, qo, nullptr, B, 0, H, Hkv, D, q_stride, k_stride, eps,
                          {rotate != 0, rotate ? center : 0, base, gamma, scale_base}, static_cast<int>(dtype)};
-  return da::launch_cache_append(c, v, v_stride, paged_cache(cache), T, static_cast<hipStream_t>(stream)) == hipSuccess
+  da::PagedCache pc = paged_cache(cache);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (f8) {
+    pc.k_scale = f8->k_scale;
+    pc.v_scale = f8->v_scale;
+    return da::launch_cache_append8(c, v, v_stride, pc, T, st) == hipSuccess ? DA_OK : DA_EHIP;
+  }
+  return da::launch_cache_append(c, v, v_stride, pc, T, st) == hipSuccess ? DA_OK : DA_EHIP;
+}
+
+// The attention over a cache of the call's type, or (with scales) in 8 bits.
+int paged_fwd(const void* q, const da_paged_cache_t* cache, const da_paged_cache_f8_t* f8, void* out, float* lse,
+              int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride, int64_t max_new,
+              const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype, float softmax_scale, void* workspace,
+              uint64_t workspace_bytes, void* stream) {
+  if (const int rc = head_shapes(T, H, Hkv, D, dtype, &q_stride, &H, 1); rc != DA_OK) return rc;
+  if (!cache_ok(B, Hkv, cache) || (f8 && (!f8->k_scale || !f8->v_scale))) return DA_EINVAL;
+  da::PagedPlan p;
+  if (const int rc = da::make_paged_plan(T, B, H, Hkv, D, cache->num_pages, cache->page_size, cache->max_pages,
+                                         max_new, patterns, num_patterns, dtype, softmax_scale, &p);
+      rc != DA_OK)
+    return rc;
+  if (T == 0) return DA_OK;
+  if (!q || !out || !lse || !workspace) return DA_EINVAL;
+  for (const void* x : {q, static_cast<const void*>(out), static_cast<const void*>(workspace),
+                        static_cast<const void*>(cache->k), static_cast<const void*>(cache->v)})
+    if (!aligned16(x)) return DA_EALIGN;
+  if (!aligned4(cache->block_table) || !aligned4(cache->seq_lens) || !aligned4(cache->q_start) || !aligned4(lse))
+    return DA_EALIGN;
+  if (workspace_bytes < p.workspace_bytes) return DA_EWORKSPACE;
+  const int64_t es = dtype == DA_BF16 ? 2 : 4;
+  const uint64_t cb = pool_bytes(cache, Hkv, f8 ? D : D * es), sb = f8 ? scale_bytes(cache, Hkv) : 0;
+  const Span ins[8] = {{q, strided_bytes(T, H * D, q_stride, es)}, {cache->k, cb}, {cache->v, cb},
+                       {cache->block_table, static_cast<uint64_t>(B) * cache->max_pages * 4},
+                       {cache->seq_lens, static_cast<uint64_t>(B) * 4}, {cache->q_start, static_cast<uint64_t>(B + 1) * 4},
+                       {f8 ? f8->k_scale : nullptr, sb}, {f8 ? f8->v_scale : nullptr, sb}};
+  const Span outs[3] = {{out, static_cast<uint64_t>(T * H * D * es)}, {lse, static_cast<uint64_t>(T * H) * 4},
+                        {workspace, p.workspace_bytes}};
+  if (any_overlap(outs, 3, ins, f8 ? 8 : 6)) return DA_EINVAL;
+  da::PagedCache pc = paged_cache(cache);
+  if (f8) {
+    pc.k_scale = f8->k_scale;
+    pc.v_scale = f8->v_scale;
+  }
+  return da::launch_paged(p, q, q_stride, pc, out, lse, workspace, static_cast<hipStream_t>(stream)) == hipSuccess
              ? DA_OK
              : DA_EHIP;
+}
+
+}  // namespace
+
+int dilated_attn_cache_append(const void* q, const void* k, const void* v, const void* qw, const void* kw, void* qo,
+                              const da_paged_cache_t* cache, int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D,
+                              int64_t q_stride, int64_t k_stride, int64_t v_stride, float eps, int64_t rotate,
+                              int64_t center, float base, float gamma, float scale_base, int64_t dtype,
+                              void* stream) {
+  return cache_append(q, k, v, qw, kw, qo, cache, nullptr, T, B, H, Hkv, D, q_stride, k_stride, v_stride, eps, rotate,
+                      center, base, gamma, scale_base, dtype, stream);
+}
+
+int dilated_attn_cache_append_f8(const void* q, const void* k, const void* v, const void* qw, const void* kw,
+                                 void* qo, const da_paged_cache_f8_t* cache, int64_t T, int64_t B, int64_t H,
+                                 int64_t Hkv, int64_t D, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                 float eps, int64_t rotate, int64_t center, float base, float gamma,
+                                 float scale_base, int64_t dtype, void* stream) {
+  if (!cache) return DA_EINVAL;
+  return cache_append(q, k, v, qw, kw, qo, &cache->pages, cache, T, B, H, Hkv, D, q_stride, k_stride, v_stride, eps,
+                      rotate, center, base, gamma, scale_base, dtype, stream);
 }
 
 int dilated_attn_paged_workspace(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages,
@@ -447,33 +522,87 @@ int dilated_attn_paged_fwd(const void* q, const da_paged_cache_t* cache, void* o
                            int64_t H, int64_t Hkv, int64_t D, int64_t q_stride, int64_t max_new,
                            const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype, float softmax_scale,
                            void* workspace, uint64_t workspace_bytes, void* stream) {
+  return paged_fwd(q, cache, nullptr, out, lse, T, B, H, Hkv, D, q_stride, max_new, patterns, num_patterns, dtype,
+                   softmax_scale, workspace, workspace_bytes, stream);
+}
+
+int dilated_attn_paged_fwd_f8(const void* q, const da_paged_cache_f8_t* cache, void* out, float* lse, int64_t T,
+                              int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride, int64_t max_new,
+                              const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                              float softmax_scale, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!cache) return DA_EINVAL;
+  return paged_fwd(q, &cache->pages, cache, out, lse, T, B, H, Hkv, D, q_stride, max_new, patterns, num_patterns,
+                   dtype, softmax_scale, workspace, workspace_bytes, stream);
+}
+
+int dilated_attn_page_weights_workspace(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages,
+                                        int64_t page_size, int64_t max_pages, const da_pattern_t* patterns,
+                                        int64_t num_patterns, int64_t dtype, uint64_t* bytes) {
+  if (!bytes) return DA_EINVAL;
+  da::WeightPlan p;
+  const int rc = da::make_weight_plan(T, B, H, Hkv, D, num_pages, page_size, max_pages, patterns, num_patterns, dtype,
+                                      0.0f, &p);
+  if (rc == DA_OK) *bytes = p.workspace_bytes;
+  return rc;
+}
+
+int dilated_attn_page_weights(const void* q, const float* lse, const da_paged_cache_f8_t* cache, float* weights,
+                              int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride,
+                              const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                              float softmax_scale, void* workspace, uint64_t workspace_bytes, void* stream) {
   if (const int rc = head_shapes(T, H, Hkv, D, dtype, &q_stride, &H, 1); rc != DA_OK) return rc;
-  if (!cache_ok(B, Hkv, cache)) return DA_EINVAL;
-  da::PagedPlan p;
-  if (const int rc = da::make_paged_plan(T, B, H, Hkv, D, cache->num_pages, cache->page_size, cache->max_pages,
-                                         max_new, patterns, num_patterns, dtype, softmax_scale, &p);
+  const da_paged_cache_t* c = cache ? &cache->pages : nullptr;
+  if (!cache_ok(B, Hkv, c, false) || !cache->k_scale) return DA_EINVAL;
+  da::WeightPlan p;
+  if (const int rc = da::make_weight_plan(T, B, H, Hkv, D, c->num_pages, c->page_size, c->max_pages, patterns,
+                                          num_patterns, dtype, softmax_scale, &p);
       rc != DA_OK)
     return rc;
   if (T == 0) return DA_OK;
-  if (!q || !out || !lse || !workspace) return DA_EINVAL;
-  for (const void* x : {q, static_cast<const void*>(out), static_cast<const void*>(workspace),
-                        static_cast<const void*>(cache->k), static_cast<const void*>(cache->v)})
+  if (!q || !lse || !weights || !workspace) return DA_EINVAL;
+  for (const void* x : {q, static_cast<const void*>(workspace), static_cast<const void*>(c->k)})
     if (!aligned16(x)) return DA_EALIGN;
-  if (!aligned4(cache->block_table) || !aligned4(cache->seq_lens) || !aligned4(cache->q_start) || !aligned4(lse))
+  if (!aligned4(c->block_table) || !aligned4(c->seq_lens) || !aligned4(c->q_start) || !aligned4(lse) ||
+      !aligned4(weights))
     return DA_EALIGN;
   if (workspace_bytes < p.workspace_bytes) return DA_EWORKSPACE;
   const int64_t es = dtype == DA_BF16 ? 2 : 4;
-  const uint64_t cb = static_cast<uint64_t>(cache->num_pages * cache->page_size * Hkv) * static_cast<uint64_t>(D * es);
-  const Span ins[6] = {{q, strided_bytes(T, H * D, q_stride, es)}, {cache->k, cb}, {cache->v, cb},
-                       {cache->block_table, static_cast<uint64_t>(B) * cache->max_pages * 4},
-                       {cache->seq_lens, static_cast<uint64_t>(B) * 4}, {cache->q_start, static_cast<uint64_t>(B + 1) * 4}};
-  const Span outs[3] = {{out, static_cast<uint64_t>(T * H * D * es)}, {lse, static_cast<uint64_t>(T * H) * 4},
-                        {workspace, p.workspace_bytes}};
-  if (any_overlap(outs, 3, ins, 6)) return DA_EINVAL;
-  return da::launch_paged(p, q, q_stride, paged_cache(cache), out, lse, workspace, static_cast<hipStream_t>(stream)) ==
+  const Span ins[7] = {{q, strided_bytes(T, H * D, q_stride, es)}, {lse, static_cast<uint64_t>(T * H) * 4},
+                       {c->k, pool_bytes(c, Hkv, D)}, {cache->k_scale, scale_bytes(c, Hkv)},
+                       {c->block_table, static_cast<uint64_t>(B) * c->max_pages * 4},
+                       {c->seq_lens, static_cast<uint64_t>(B) * 4}, {c->q_start, static_cast<uint64_t>(B + 1) * 4}};
+  const Span outs[2] = {{weights, static_cast<uint64_t>(c->num_pages) * 4}, {workspace, p.workspace_bytes}};
+  if (any_overlap(outs, 2, ins, 7)) return DA_EINVAL;
+  da::PagedCache pc = paged_cache(c);
+  pc.k_scale = cache->k_scale;
+  return da::launch_page_weights(p, q, q_stride, lse, pc, weights, workspace, static_cast<hipStream_t>(stream)) ==
                  hipSuccess
              ? DA_OK
              : DA_EHIP;
+}
+
+int dilated_attn_evict_pages(const float* weights, const int32_t* block_table, const int32_t* seq_lens,
+                             int32_t* table_out, int32_t* freed, int32_t* count, int64_t B, int64_t num_pages,
+                             int64_t page_size, int64_t max_pages, int64_t keep, int64_t first, int64_t last,
+                             void* stream) {
+  constexpr int64_t kMost = int64_t{1} << 31;
+  if (!weights || !block_table || !seq_lens || !table_out || !freed || !count) return DA_EINVAL;
+  if (B < 1 || B >= kMost || num_pages < 1 || num_pages >= kMost || page_size < 1 ||
+      page_size > (int64_t{1} << 16) || (page_size & (page_size - 1)) || max_pages < 1 ||
+      max_pages >= kMost / page_size || keep < 0 || first < 0 || last < 0 || last >= kMost)
+    return DA_EINVAL;
+  for (const void* x : {static_cast<const void*>(weights), static_cast<const void*>(block_table),
+                        static_cast<const void*>(seq_lens), static_cast<const void*>(table_out),
+                        static_cast<const void*>(freed), static_cast<const void*>(count)})
+    if (!aligned4(x)) return DA_EALIGN;
+  const uint64_t tb = static_cast<uint64_t>(B) * max_pages * 4;
+  const Span ins[3] = {{weights, static_cast<uint64_t>(num_pages) * 4}, {seq_lens, static_cast<uint64_t>(B) * 4},
+                       {block_table, table_out == block_table ? 0 : tb}};
+  const Span outs[3] = {{table_out, tb}, {freed, tb}, {count, static_cast<uint64_t>(B) * 4}};
+  if (any_overlap(outs, 3, ins, 3)) return DA_EINVAL;
+  const da::EvictCall c{weights, block_table, seq_lens, table_out, freed, count, B, num_pages, page_size, max_pages,
+                        keep, first, last};
+  return da::launch_evict(c, static_cast<hipStream_t>(stream)) == hipSuccess ? DA_OK : DA_EHIP;
 }
 
 int dilated_attn_profile_begin(int64_t capacity) {

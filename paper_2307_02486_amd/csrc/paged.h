@@ -41,7 +41,12 @@ struct PagedCache {
   const int32_t *table, *lens, *start;
   int64_t num_pages, max_pages;
   int page_log2;
+  // 8-bit caches (k and v hold e4m3 values; otherwise null): the scales' exponents,
+  // biased by 127, [num_pages][Hkv][page / block], block = 2^min(page_log2, kCacheBlockLog2)
+  // tokens.  Pages outside the pool hold no keys there.
+  uint8_t *k_scale = nullptr, *v_scale = nullptr;
 };
+constexpr int kCacheBlockLog2 = 4;
 
 hipError_t launch_cache_append(const QkNormCall& c, const void* v, int64_t v_stride, const PagedCache& cache,
                                int64_t T, hipStream_t stream);
@@ -49,5 +54,23 @@ hipError_t launch_cache_append(const QkNormCall& c, const void* v, int64_t v_str
 // Dilated attention of new tokens over a paged cache.
 hipError_t launch_paged(const PagedPlan& plan, const void* q, int64_t q_stride, const PagedCache& cache, void* out,
                         float* lse, void* workspace, hipStream_t stream);
+
+// New keys and values into an 8-bit cache, and the queries beside them.
+hipError_t launch_cache_append8(const QkNormCall& c, const void* v, int64_t v_stride, const PagedCache& cache,
+                                int64_t T, hipStream_t stream);
+
+// The attention weight that the pages of an 8-bit cache got from new tokens, added
+// to weights [num_pages].
+hipError_t launch_page_weights(const WeightPlan& plan, const void* q, int64_t q_stride, const float* lse,
+                               const PagedCache& cache, float* weights, void* workspace, hipStream_t stream);
+
+// The lightest pages out of each sequence's table.
+struct EvictCall {
+  const float* weights;
+  const int32_t *table, *lens;
+  int32_t *table_out, *freed, *count;
+  int64_t B, num_pages, page_size, max_pages, keep, first, last;
+};
+hipError_t launch_evict(const EvictCall& c, hipStream_t stream);
 
 }  // namespace da

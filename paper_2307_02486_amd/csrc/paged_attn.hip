@@ -39,14 +39,11 @@
 
 #include <algorithm>
 
-#include "device_common.h"
-#include "paged.h"
+#include "paged_device.h"
 
 namespace da {
 namespace {
 
-constexpr int kPgThreads = 256;
-constexpr int kPgWaves = kPgThreads / 64;
 constexpr float kLowest = -3.402823466e38f;  // a running maximum of no score: the lowest finite value
 constexpr float kSumSlack = 1024.0f;  // a half row's sum above it moves its reference (tiles)
 constexpr float kSlack = 8.0f;       // a score this far above its row's reference (log2) moves it
@@ -54,13 +51,14 @@ constexpr float kSlack = 8.0f;       // a score this far above its row's referen
 struct PagedArgs {
   const void* q;
   const char *kc, *vc;
+  const uint8_t *ks, *vs;  // 8-bit caches: the blocks' scales
   const int32_t *table, *lens, *start;
   char* ws;
   void* out;
   float* lse;
   int64_t qs;  // elements between tokens of q
   int64_t one_rec, one_row, tile_rec, tile_row;  // byte offsets in the workspace
-  int32_t T, B, H, Hkv, G, npat, num_pages, max_pages, page_log2;
+  int32_t T, B, H, Hkv, G, npat, num_pages, max_pages, page_log2, block_log2;
   int32_t few, singles, one_slots, one_items, tile_items, grid, join_groups;
   uint32_t reach;     // positions the table holds
   FastDiv fheads;     // division by H
@@ -86,24 +84,6 @@ __device__ inline void touch(const PagedArgs& a) {
   asm volatile("" ::"s"(x));
 }
 
-// The last pattern that begins at or before x.
-__device__ inline int pattern_at(const int32_t (&begin)[DA_MAX_PATTERNS], int x) {
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < DA_MAX_PATTERNS; ++i) n += begin[i] <= x;
-  return n - 1;
-}
-
-// The keys of pattern P that a query at position pos sees, if its head is kept:
-// positions first + t r, t < n; rho is the head offset that is kept.
-struct Lattice {
-  int rho, first, n;
-};
-__device__ inline Lattice lattice_of(const PagedPattern& P, int pos) {
-  const int seg = static_cast<int>(P.fw.div(pos)) * P.w, loc = pos - seg;
-  const int t = P.fr.div(loc), rho = loc - t * P.r;
-  return {rho, seg + rho, t + 1};
-}
 // How many of them a single token reads for P: where the list has a pattern
 // that holds every key of its segment, the others leave the keys of that
 // segment to it, which weights a key by the number of patterns that hold it.
@@ -114,90 +94,6 @@ __device__ inline int own_keys(const PagedArgs& a, const PagedPattern& P, bool i
   const int begin = static_cast<int>(a.full_fw.div(pos)) * a.full_w;
   return begin > x.first ? min(x.n, static_cast<int>(P.fr.div(begin - x.first - 1)) + 1) : 0;
 }
-__device__ inline int head_offset(const PagedPattern& P, int head) {
-  return head - static_cast<int>(P.fr.div(head)) * P.r;
-}
-
-// The loads of these values begin before this point.  (A load whose value is used
-// under a condition only would move there: another round to memory after those
-// that the condition waits for.)
-__device__ inline void here(int& v) { asm volatile("" : "+v"(v)); }
-
-// A sequence's new tokens: rows begin .. end - 1 of the call, the last of its
-// length len.
-struct Sequence {
-  int b;  // -1: the token has none
-  int begin, end, len;
-};
-// The sequences of kTokens tokens (the same in all lanes), by all lanes of a
-// wave: start [B + 1] ascends and the last entry that is not above a token is
-// its sequence's (empty ones before it share that value).  Whatever start
-// holds, the result is below B.  Up to 63 sequences all entries arrive in one
-// round of loads.
-template <int kTokens>
-__device__ inline void find_sequences(const PagedArgs& a, const int (&tok)[kTokens], int lane, Sequence (&sq)[kTokens]) {
-  int n[kTokens];
-#pragma unroll
-  for (int i = 0; i < kTokens; ++i) n[i] = 0;
-  int start = 0, len = 0;
-  for (int b0 = 0; b0 <= a.B; b0 += 64) {
-    const int b = b0 + lane;
-    start = a.start[min(b, a.B)];
-    len = a.lens[min(b, a.B - 1)];
-    here(len);
-#pragma unroll
-    for (int i = 0; i < kTokens; ++i) n[i] += __popcll(__ballot(b <= a.B && start <= tok[i]));
-  }
-#pragma unroll
-  for (int i = 0; i < kTokens; ++i) {
-    const int b = n[i] > a.B ? -1 : n[i] - 1;
-    sq[i] = Sequence{b, 0, 0, 0};
-    if (b < 0) continue;
-    if (a.B < 64) {
-      sq[i].begin = __builtin_amdgcn_readlane(start, b);
-      sq[i].end = __builtin_amdgcn_readlane(start, b + 1);
-      sq[i].len = __builtin_amdgcn_readlane(len, b);
-    } else {
-      sq[i].begin = a.start[b];
-      sq[i].end = a.start[b + 1];
-      sq[i].len = a.lens[b];
-    }
-  }
-}
-
-// Position of row tok of its sequence; -1 where it has none in the table.
-__device__ inline int position_of(const PagedArgs& a, const Sequence& sq, int tok) {
-  const int64_t p = static_cast<int64_t>(sq.len) - sq.end + tok;
-  return sq.b >= 0 && tok < sq.end && p >= 0 && p < a.reach ? static_cast<int>(p) : -1;
-}
-
-// Entry i of start, held to the call's tokens: what a tile reads and writes stays in bounds.
-__device__ inline int token_row(const PagedArgs& a, int i) { return max(0, min(a.start[i], a.T)); }
-
-// This thread's number, opaque to the compiler: in the loop over a workgroup's
-// items what follows from it would otherwise be formed before the loop and held
-// in registers over all of it (which then spill).
-__device__ inline int thread_id() {
-  int tid = __builtin_amdgcn_workitem_id_x();
-  asm volatile("" : "+v"(tid));
-  return tid;
-}
-
-// Running sum over the wave's lanes: within rows of 16 lanes by shifts on the
-// vector ALU, then the rows' last sums into the rows after them.
-template <int kCtrl, int kRows>
-__device__ inline int add_shifted(int v) {
-  return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, false);
-}
-__device__ inline int running_sum(int v) {
-  v = add_shifted<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
-  v = add_shifted<0x112, 0xf>(v);
-  v = add_shifted<0x114, 0xf>(v);
-  v = add_shifted<0x118, 0xf>(v);
-  v = add_shifted<0x142, 0xa>(v);  // row_bcast 15 into rows 1 and 3
-  return add_shifted<0x143, 0xc>(v);  // row_bcast 31 into rows 2 and 3
-}
-
 // A listed token: its row of q, its sequence and position.  kMixed: number e of
 // those in sequences of at most a.few new tokens; otherwise row e of the call.
 // False: not there, or not in the table.
@@ -232,48 +128,6 @@ __device__ inline bool single_token(const PagedArgs& a, int e, int lane, Token& 
   t.b = sq[0].b;
   t.pos = position_of(a, sq[0], t.tok);
   return t.pos >= 0;
-}
-
-// The heads of key head hk's group that pattern P keeps at segment-local
-// offset rho: first, first + r, ... below (hk + 1) G; none: count = 0.
-struct KeptHeads {
-  int first, count;
-};
-__device__ inline KeptHeads kept_heads(const PagedPattern& P, int hk, int G, int rho) {
-  const int h0 = hk * G;
-  int x = rho - (h0 - static_cast<int>(P.fr.div(h0)) * P.r);
-  if (x < 0) x += P.r;
-  if (x >= G) return {0, 0};
-  return {h0 + x, static_cast<int>(P.fr.div(G - 1 - x)) + 1};
-}
-
-// The table's entry for position pos of a sequence, and key head hk's row of the
-// cache there.  A page outside the pool reads the pool's last page: in bounds,
-// whatever the table holds.
-__device__ inline int table_entry(const PagedArgs& a, const int32_t* table, int pos) { return table[pos >> a.page_log2]; }
-__device__ inline uint32_t cache_row(const PagedArgs& a, int entry, int hk, int pos) {
-  const uint32_t page = min(static_cast<uint32_t>(entry), static_cast<uint32_t>(a.num_pages - 1));
-  return ((page * a.Hkv + hk) << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
-}
-// The cache rows of keys first .. first + n - 1 (positions base + t r) into row,
-// by a workgroup; keys past `last` are that one.  kAtOnce entries of a thread
-// are on their way together.
-template <int kAtOnce>
-__device__ inline void look_up_rows(const PagedArgs& a, const int32_t* table, int hk, int base, int r, int first,
-                                    int last, int n, int tid, uint32_t* row) {
-  for (int i0 = tid; i0 < n; i0 += kAtOnce * kPgThreads) {
-    int pos[kAtOnce], entry[kAtOnce];
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      pos[u] = base + min(first + i0 + u * kPgThreads, last) * r;
-      entry[u] = table_entry(a, table, pos[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) here(entry[u]);
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-      if (i0 + u * kPgThreads < n) row[i0 + u * kPgThreads] = cache_row(a, entry[u], hk, pos[u]);
-  }
 }
 
 // Keys of a split of n keys: whole 32-key tiles, and two of them for each wave
@@ -323,19 +177,23 @@ struct KeyFrag {
 
 constexpr int kOneTile = 32;    // keys of a wave's tile
 constexpr int kOneRows = 1024;  // keys whose rows are looked up at once
-template <int D>
+template <int D, bool kF8>
 struct SmemOne {
   __attribute__((aligned(16))) char v[kPgWaves][kOneTile * D * 2];  // each wave's V tile
   float ml[kPgWaves][2][16];
   u32x4 q[D / 32][64];     // Q^T operand, lane by lane
   uint32_t row[kOneRows];  // cache rows of the split's keys, a chunk at a time
+  uint64_t gone[kF8 ? kOneRows / 64 : 0];  // their keys of no page
 };
 
-template <int D, bool kMixed>
-__device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, SmemOne<D>& sm) {
+template <int D, bool kMixed, bool kF8>
+__device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, SmemOne<D, kF8>& sm) {
   constexpr int KC = D / 32, DB = D / 16, kTile = kOneTile;
   using TL = TileLayout<D>;
-  constexpr int kVLoads = kTile * TL::kSlots / 64;
+  // An 8-bit row of V is half as many 16-byte loads, each two slots of the tile.
+  constexpr int kVPieces = kF8 ? D / 16 : TL::kSlots;  // 16-byte pieces of a cached row
+  constexpr int kVLoads = kTile * kVPieces / 64;
+  using Keys = typename std::conditional<kF8, KeyFrag8<D>, KeyFrag<D>>::type;
   // Joined rows are D floats apart, 16-byte chunk c of row r at c ^ (r mod D/4).
   auto join_at = [](int r, int chunk) { return r * D + 4 * (chunk ^ (r & (D / 4 - 1))); };
   static_assert(16 * D * 4 <= kTile * D * 2, "the join fits a wave's V tile");
@@ -373,7 +231,8 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
   const int head = kh.first + (m0 + min(m, rows - 1)) * P.r;
   // Q^T operand (kept in LDS: in registers it would spill at D = 128).
   for (int c = wv; c < KC; c += kPgWaves) {
-    const u32x4 x = load16(static_cast<const u16*>(a.q) + tk.tok * a.qs + head * D + 32 * c + 8 * grp);
+    const int d0 = kF8 ? step_first<D>(c, grp) : 32 * c + 8 * grp;
+    const u32x4 x = load16(static_cast<const u16*>(a.q) + tk.tok * a.qs + head * D + d0);
     sm.q[c][lane] = m < rows ? x : u32x4{0u, 0u, 0u, 0u};
   }
 
@@ -392,24 +251,32 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
       if (m == r) mine = mask;
     }
   }
-  constexpr int kVStep = 64 / TL::kSlots;  // V rows of a load
-  const int vrow = lane / TL::kSlots;
+  constexpr int kVStep = 64 / kVPieces;  // V rows of a load
+  const int vrow = lane / kVPieces, vpiece = lane % kVPieces;
   char* my = sv[wv];
   // Requests the 32 keys from `key` on (counted within the chunk whose rows are in LDS).
-  auto request_k = [&](int key, KeyFrag<D>& kf) {
+  auto request_k = [&](int key, Keys& kf) {
+    if constexpr (kF8) {
+      request_keys8<D>(a, sm.row + key, m, grp, kf);
+    } else {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const char* p = a.kc + (static_cast<int64_t>(sm.row[key + 16 * u + m]) * TL::kRowBytes + 16 * grp);
+      for (int u = 0; u < 2; ++u) {
+        const char* p = a.kc + (static_cast<int64_t>(sm.row[key + 16 * u + m]) * TL::kRowBytes + 16 * grp);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) kf.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+        for (int c = 0; c < KC; ++c) kf.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+      }
     }
   };
   u32x4 vreg[kVLoads];
+  uint32_t vscale[kVLoads];
   auto request_v = [&](int key) {
 #pragma unroll
-    for (int i = 0; i < kVLoads; ++i)
+    for (int i = 0; i < kVLoads; ++i) {
+      const uint32_t row = sm.row[key + kVStep * i + vrow];
       vreg[i] = *reinterpret_cast<const u32x4*>(
-          a.vc + (static_cast<int64_t>(sm.row[key + kVStep * i + vrow]) * TL::kRowBytes + (lane % TL::kSlots) * 16));
+          a.vc + (static_cast<int64_t>(row) * (kVPieces * 16) + vpiece * 16));
+      if constexpr (kF8) vscale[i] = a.vs[row >> a.block_log2];
+    }
   };
   // V^T operand: lane's d = 16 db + (lane & 15), keys 4 grp + 0..3 and 16 more.
   // Block db's 16-byte slots are 2 db and 2 db + 1 before the swizzle, an
@@ -422,16 +289,34 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
   for (int db = 0; db < DB; ++db) acc[db] = f32x4{0, 0, 0, 0};
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
+  int chunk = k0;  // first key of the chunk whose rows are in LDS
 
   // first: the tile's first key (t); next: the next tile's, within the chunk, < 0: none
-  auto compute = [&](int first, const KeyFrag<D>& kf, int next) {
+  auto compute = [&](int first, const Keys& kf, int next) {
     f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       const bf16x8 qf = __builtin_bit_cast(bf16x8, sm.q[c][lane]);
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf.k[u][c]), qf, s[u], 0, 0, 0);
+      for (int u = 0; u < 2; ++u) {
+        u32x4 k;
+        if constexpr (kF8) k = widen8(kf.k[u][2 * c], kf.k[u][2 * c + 1], scale_of(kf.scale[u]));
+        else k = kf.k[u][c];
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), qf, s[u], 0, 0, 0);
+      }
+    }
+    uint32_t gone = 0;
+    if constexpr (kF8) {  // keys of no page (rows of the wave's tile: half a word)
+      const int local = first - chunk;
+      gone = uniform(static_cast<uint32_t>(sm.gone[local >> 6] >> (local & 32)));
+      if (gone) {
+        const uint32_t mine4 = gone >> (4 * grp);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (mine4 >> (16 * u + e) & 1) s[u][e] = -INFINITY;
+      }
     }
     const int left = ke - first - 4 * grp;  // keys from this lane's first on
 #pragma unroll
@@ -479,9 +364,27 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
       }
     // V through the wave's own LDS tile, to be read transposed (LDS operations
     // of a wave complete in order: no wait between).
+    if constexpr (kF8) {
+      if (gone) {  // zeros, as a weight of zero times whatever the pool holds there may be NaN
 #pragma unroll
-    for (int i = 0; i < kVLoads; ++i)
-      *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, lane % TL::kSlots)) = vreg[i];
+        for (int i = 0; i < kVLoads; ++i)
+          if (gone >> (kVStep * i + vrow) & 1) {
+            vreg[i] = u32x4{0u, 0u, 0u, 0u};
+            vscale[i] = 127;
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i) {
+      if constexpr (kF8) {
+        const float scale = scale_of(vscale[i]);
+        *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, 2 * vpiece)) = widen8(vreg[i][0], vreg[i][1], scale);
+        *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, 2 * vpiece + 1)) =
+            widen8(vreg[i][2], vreg[i][3], scale);
+      } else {
+        *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, vpiece)) = vreg[i];
+      }
+    }
     if (next >= 0) request_v(next);
     const uint32_t va = lds_addr(my);
     constexpr int kHalf = DB < 4 ? DB : 4;  // blocks whose V is read at once
@@ -507,15 +410,16 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
 
   for (int c0 = k0; c0 < ke; c0 += kOneRows) {
     const int keys = min(ke - c0, kOneRows), ntile = (keys + kTile - 1) / kTile;
+    chunk = c0;
     if (c0 > k0) __syncthreads();  // every wave is done with the rows before
-    look_up_rows<4>(a, table, hk, base, P.r, c0, ke - 1, ntile * kTile, tid, sm.row);
+    look_up_rows<4, kF8>(a, table, hk, base, P.r, c0, ke - 1, ntile * kTile, tid, sm.row, sm.gone);
     __syncthreads();
     if (wv >= ntile) continue;
     // While a tile is computed the next one's loads are under way, K's from its
     // start, V's from where its own V has left the registers.  A wave's last tile
     // is a branch of its own, so that at every use of K it is known which loads
     // are younger.
-    KeyFrag<D> ka, kb;
+    Keys ka, kb;
     request_k(wv * kTile, ka);
     request_v(wv * kTile);
     for (int tile = wv;;) {
@@ -568,10 +472,16 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
   }
 }
 
+// Four e4m3 values of a row times its scale, in float32.
+__device__ inline f32x4 widen4(uint32_t w, float scale) {
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+}
+
 // float32: a workgroup is one (token, query head, pattern, split).  D/4 lanes
 // hold a row, each group of them its own keys and running softmax; the groups
 // and waves meet in LDS.
-template <int D>
+template <int D, bool kF8>
 __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
   constexpr int kLanes = D / 4, kGroups = kPgThreads / kLanes, kUnroll = 4;
   __shared__ __attribute__((aligned(16))) float so[kGroups][D];
@@ -605,10 +515,22 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
   f32x4 acc = f32x4{0, 0, 0, 0};
   for (int t0 = k0; t0 < ke; t0 += kUnroll * kGroups) {
     f32x4 k[kUnroll], v[kUnroll];
+    bool gone[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int t = min(t0 + u * kGroups + grp, ke - 1);
       const int pos = base + t * P.r;
+      if constexpr (kF8) {
+        const int entry = table_entry(a, table, pos);
+        gone[u] = static_cast<uint32_t>(entry) >= static_cast<uint32_t>(a.num_pages);
+        const uint32_t row = cache_row(a, gone[u] ? 0 : entry, hk, pos);
+        const int64_t at = static_cast<int64_t>(row) * D + 4 * ch;
+        k[u] = widen4(*reinterpret_cast<const uint32_t*>(a.kc + at), scale_of(a.ks[row >> a.block_log2]));
+        const uint32_t word = *reinterpret_cast<const uint32_t*>(a.vc + at), byte = a.vs[row >> a.block_log2];
+        v[u] = widen4(gone[u] ? 0u : word, scale_of(gone[u] ? 127u : byte));  // (0 times what is there may be NaN)
+        continue;
+      }
+      gone[u] = false;
       const int64_t at = static_cast<int64_t>(cache_row(a, table_entry(a, table, pos), hk, pos)) * D + 4 * ch;
       k[u] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.kc) + at);
       v[u] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.vc) + at);
@@ -619,7 +541,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_one_f32(PagedArgs a) {
       float d = (q[0] * k[u][0] + q[1] * k[u][1]) + (q[2] * k[u][2] + q[3] * k[u][3]);
 #pragma unroll
       for (int x = 1; x < kLanes; x <<= 1) d += __shfl_xor(d, x, 64);
-      s[u] = t0 + u * kGroups + grp < ke ? d * a.scale_log2 : -INFINITY;
+      s[u] = t0 + u * kGroups + grp < ke && !gone[u] ? d * a.scale_log2 : -INFINITY;
       mx = fmaxf(mx, s[u]);
     }
     const float alpha = __builtin_amdgcn_exp2f(m_run - mx);
@@ -737,17 +659,20 @@ struct TileItem {
   int pi, tile, head, split;
 };
 
-constexpr int kTileRows = 4096;  // keys whose rows are looked up at once (three workgroups of D = 64 fit a CU)
+// Keys whose rows are looked up at once (three workgroups of D = 64 fit a CU, two of D = 128).
+template <bool kF8>
+constexpr int kTileRows = kF8 ? 2048 : 4096;
 
-template <int D>
+template <int D, bool kF8>
 struct SmemTile {
   __attribute__((aligned(16))) u16 k[2][kPagedKeyTile * D];
   __attribute__((aligned(16))) u16 v[2][kPagedKeyTile * D];
-  uint32_t row[kTileRows];  // cache rows of the keys, a chunk at a time
+  uint32_t row[kTileRows<kF8>];  // cache rows of the keys, a chunk at a time
+  uint64_t gone[kF8 ? kTileRows<kF8> / 64 : 0];  // their keys of no page
 };
 
-template <int D>
-__device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemTile<D>& sm) {
+template <int D, bool kF8>
+__device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemTile<D, kF8>& sm) {
   constexpr int BM = kPagedRows, BN = kPagedKeyTile;
   constexpr int KC = D / 16, DB = D / 32;
   using TL = TileLayout<D>;
@@ -798,6 +723,47 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
     lrow[i] = s / TL::kSlots;
     lslot[i] = (s % TL::kSlots) ^ TL::swz(lrow[i]);
   }
+  // 8-bit caches: a thread has a quarter of a row of K and of V, whose loads are
+  // under way while a tile is computed; they go to LDS as bf16, once for the four
+  // waves that read the tile.
+  constexpr int kPieces = D > 32 ? D / 64 : 1;  // 16-byte loads (D = 32: of 8 bytes) of a thread's quarter
+  const int brow = tid >> 2, bpart = tid & 3;
+  uint32_t kbytes[kPieces * 4], vbytes[kPieces * 4], kscale = 0, vscale = 0;
+  auto request_tile = [&](int jt) {
+    const uint32_t row = sm.row[jt * BN + brow];
+    const char* kp = a.kc + (static_cast<int64_t>(row) * D + (D > 32 ? 16 : 8) * bpart);
+    const char* vp = a.vc + (static_cast<int64_t>(row) * D + (D > 32 ? 16 : 8) * bpart);
+    if constexpr (D == 32) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(kp), y = *reinterpret_cast<const u32x2*>(vp);
+      kbytes[0] = x[0], kbytes[1] = x[1], vbytes[0] = y[0], vbytes[1] = y[1];
+    } else {
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(kp + 64 * p), y = *reinterpret_cast<const u32x4*>(vp + 64 * p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kbytes[4 * p + i] = x[i], vbytes[4 * p + i] = y[i];
+      }
+    }
+    kscale = a.ks[row >> a.block_log2];
+    vscale = a.vs[row >> a.block_log2];
+  };
+  auto store_tile = [&](int jt, int buf) {
+    if (sm.gone[jt] >> brow & 1) {  // zeros, as a weight of zero times whatever the pool holds there may be NaN
+#pragma unroll
+      for (int i = 0; i < kPieces * 4; ++i) vbytes[i] = 0;
+      vscale = 127;
+    }
+    char* kl = reinterpret_cast<char*>(&sm.k[buf][0]);
+    char* vl = reinterpret_cast<char*>(&sm.v[buf][0]);
+    const float ksc = scale_of(kscale), vsc = scale_of(vscale);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {  // eight elements each: slot bpart, or two of 4 p + bpart
+      const int slot = D == 32 ? bpart : 2 * (bpart + 4 * (i >> 1)) + (i & 1);
+      const int at = TL::offset(brow, slot);
+      *reinterpret_cast<u32x4*>(kl + at) = widen8(kbytes[2 * i], kbytes[2 * i + 1], ksc);
+      *reinterpret_cast<u32x4*>(vl + at) = widen8(vbytes[2 * i], vbytes[2 * i + 1], vsc);
+    }
+  };
   // Tile jt of the chunk whose rows are in LDS.
   auto load_tile = [&](int jt, int buf) {
     char* kl = reinterpret_cast<char*>(&sm.k[buf][0]);
@@ -829,16 +795,24 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
   for (int db = 0; db < DB; ++db) acc_o[db] = f32x16{};
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
-  for (int c0 = kb; c0 < ke; c0 += kTileRows) {
-    const int ntile = (min(ke - c0, kTileRows) + BN - 1) / BN;
-    look_up_rows<8>(a, table, hk, base, P.r, c0, ke - 1, ntile * BN, tid, sm.row);
+  for (int c0 = kb; c0 < ke; c0 += kTileRows<kF8>) {
+    const int ntile = (min(ke - c0, kTileRows<kF8>) + BN - 1) / BN;
+    look_up_rows<8, kF8>(a, table, hk, base, P.r, c0, ke - 1, ntile * BN, tid, sm.row, sm.gone);
     __syncthreads();
-    load_tile(0, 0);
-    wait_loads<0>();
+    if constexpr (kF8) {
+      request_tile(0);
+      store_tile(0, 0);
+    } else {
+      load_tile(0, 0);
+      wait_loads<0>();
+    }
     __syncthreads();
     for (int jt = 0; jt < ntile; ++jt) {
       const int cur = jt & 1, k0 = c0 + jt * BN;
-      if (jt + 1 < ntile) load_tile(jt + 1, cur ^ 1);
+      if (jt + 1 < ntile) {
+        if constexpr (kF8) request_tile(jt + 1);
+        else load_tile(jt + 1, cur ^ 1);
+      }
       const char* kl = reinterpret_cast<const char*>(&sm.k[cur][0]);
       const char* vl = reinterpret_cast<const char*>(&sm.v[cur][0]);
       if (k0 <= wq_lo + 31 && wq_lo < qend) {  // not all keys after this wave's queries
@@ -870,6 +844,19 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
 #pragma unroll
             for (int j = 0; j < 16; ++j)
               if (first + x * 32 + 8 * (j >> 2) + (j & 3) > 0) acc_s[x][j] = -INFINITY;
+        }
+        if constexpr (kF8) {  // keys of no page
+          const uint64_t word = sm.gone[jt];
+          const uint32_t gone[2] = {uniform(static_cast<uint32_t>(word)), uniform(static_cast<uint32_t>(word >> 32))};
+          if (gone[0] | gone[1]) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint32_t mine = gone[x] >> (4 * hi);
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (mine >> (8 * (j >> 2) + (j & 3)) & 1) acc_s[x][j] = -INFINITY;
+            }
+          }
         }
         // P = 2^(c S - m) for the reference m of the row so far, without looking
         // for the tile's maximum: a tile whose probabilities of half a row sum to
@@ -937,7 +924,11 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
           });
         });
       }
-      wait_loads<0>();
+      if constexpr (kF8) {
+        if (jt + 1 < ntile) store_tile(jt + 1, cur ^ 1);
+      } else {
+        wait_loads<0>();
+      }
       __syncthreads();
     }
   }
@@ -994,40 +985,40 @@ __device__ inline bool tile_item(const PagedArgs& a, int pi, int local, int tile
 }
 
 // Every token a single one.
-template <int D>
+template <int D, bool kF8>
 __global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_singles(PagedArgs a) {
-  __shared__ SmemOne<D> sm;
+  __shared__ SmemOne<D, kF8> sm;
   touch(a);
   const int idx = launch_index();
   if (idx >= a.one_items) return;
   const int pi = pattern_at(a.one_begin, idx);
   OneItem it;
-  if (one_item(a, pi, idx - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, false>(a, it, sm);
+  if (one_item(a, pi, idx - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, false, kF8>(a, it, sm);
 }
 
-template <int D>
+template <int D, bool kF8>
 union SmemMixed {
-  SmemTile<D> tile;
-  SmemOne<D> one;
+  SmemTile<D, kF8> tile;
+  SmemOne<D, kF8> one;
   int count[DA_MAX_PATTERNS + 1];
 };
 
 // Tiles and single tokens in one launch, the tiles first, as they take longer:
 // every item that the sizes allow.
-template <int D>
+template <int D, bool kF8>
 __global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_mixed(PagedArgs a) {
-  __shared__ SmemMixed<D> sm;
+  __shared__ SmemMixed<D, kF8> sm;
   touch(a);
   const int idx = launch_index();
   if (idx < a.tile_items) {
     const int pi = pattern_at(a.tile_begin, idx);
     const PagedPattern& P = a.pat[pi];
     TileItem it;
-    if (tile_item(a, pi, idx - P.tile_begin, P.tiles, P.run, P.tile_split.d, it)) query_tiles<D>(a, it, sm.tile);
+    if (tile_item(a, pi, idx - P.tile_begin, P.tiles, P.run, P.tile_split.d, it)) query_tiles<D, kF8>(a, it, sm.tile);
   } else if (idx - a.tile_items < a.one_items) {
     const int pi = pattern_at(a.one_begin, idx - a.tile_items);
     OneItem it;
-    if (one_item(a, pi, idx - a.tile_items - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, true>(a, it, sm.one);
+    if (one_item(a, pi, idx - a.tile_items - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, true, kF8>(a, it, sm.one);
   }
 }
 
@@ -1040,9 +1031,9 @@ __global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_mixed(Page
 // each item: held in registers over an item the counts would spill, and most
 // workgroups have one.  (No least number of workgroups a CU: asking for 1, 2 or 3
 // of them is within 1 % at heads of 32, 64 and 128.)
-template <int D>
+template <int D, bool kF8>
 __global__ __launch_bounds__(kPgThreads) void paged_mixed_steps(PagedArgs a) {
-  __shared__ SmemMixed<D> sm;
+  __shared__ SmemMixed<D, kF8> sm;
   touch(a);
   const uint32_t idx = launch_index();  // below 2^31, as the items and the launch are
   if (idx >= static_cast<uint32_t>(a.grid)) return;  // its items are another's
@@ -1084,12 +1075,12 @@ __global__ __launch_bounds__(kPgThreads) void paged_mixed_steps(PagedArgs a) {
       TileItem it;
       if (tile_item(a, pi, item - begin, __builtin_amdgcn_readlane(tiles, pi), __builtin_amdgcn_readlane(run, pi),
                     __builtin_amdgcn_readlane(splits, pi), it))
-        query_tiles<D>(a, it, sm.tile);
+        query_tiles<D, kF8>(a, it, sm.tile);
     } else if (item < all_items) {
       const int pi = __builtin_ctzll(__ballot(one_end > item - tile_items));
       const int begin = tile_items + __builtin_amdgcn_readlane(one_end, pi) - __builtin_amdgcn_readlane(ones, pi);
       OneItem it;
-      if (one_item(a, pi, item - begin, tokens, it)) single_tokens<D, true>(a, it, sm.one);
+      if (one_item(a, pi, item - begin, tokens, it)) single_tokens<D, true, kF8>(a, it, sm.one);
     }
     __syncthreads();  // the item is done with its LDS
   }
@@ -1320,19 +1311,19 @@ void launch_join(int64_t rows, const PagedArgs& a, hipStream_t stream) {
   else hipLaunchKernelGGL((paged_join<T, D, false>), grid_of((rows + kPgWaves - 1) / kPgWaves), threads, 0, stream, a);
 }
 
-template <int D>
+template <int D, bool kF8>
 void launch_all(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
   const dim3 threads(kPgThreads), grid = grid_of(p.grid);
   const int64_t singles = p.singles * p.H;
   if (p.dtype == DA_F32) {
-    hipLaunchKernelGGL(paged_one_f32<D>, grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((paged_one_f32<D, kF8>), grid, threads, 0, stream, a);
     launch_join<float, D>(singles, a, stream);
   } else if (p.all_few) {
-    hipLaunchKernelGGL(paged_singles<D>, grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((paged_singles<D, kF8>), grid, threads, 0, stream, a);
     launch_join<u16, D>(singles, a, stream);
   } else {
-    if (p.steps) hipLaunchKernelGGL(paged_mixed_steps<D>, grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL(paged_mixed<D>, grid, threads, 0, stream, a);
+    if (p.steps) hipLaunchKernelGGL((paged_mixed_steps<D, kF8>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((paged_mixed<D, kF8>), grid, threads, 0, stream, a);
     const bool share = p.T * p.H <= kJoinShared && p.tile_slots > p.npat;
     const int64_t rows = kPgThreads / (D / 8) / (share ? kJoinSubs : 1);
     a.join_groups = static_cast<int32_t>((p.T * p.H + rows - 1) / rows);
@@ -1345,6 +1336,13 @@ void launch_all(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
   }
 }
 
+template <bool kF8>
+void launch_cached(const PagedPlan& p, PagedArgs& a, hipStream_t stream) {
+  if (p.D == 32) launch_all<32, kF8>(p, a, stream);
+  else if (p.D == 64) launch_all<64, kF8>(p, a, stream);
+  else launch_all<128, kF8>(p, a, stream);
+}
+
 }  // namespace
 
 hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, const PagedCache& cache, void* out,
@@ -1353,6 +1351,9 @@ hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, con
   a.q = q;
   a.kc = static_cast<const char*>(cache.k);
   a.vc = static_cast<const char*>(cache.v);
+  a.ks = cache.k_scale;
+  a.vs = cache.v_scale;
+  a.block_log2 = std::min(cache.page_log2, kCacheBlockLog2);
   a.table = cache.table;
   a.lens = cache.lens;
   a.start = cache.start;
@@ -1392,9 +1393,8 @@ hipError_t launch_paged(const PagedPlan& p, const void* q, int64_t q_stride, con
     a.one_begin[i] = i < p.npat ? p.pat[i].one_begin : 0x7fffffff;
     a.tile_begin[i] = i < p.npat ? p.pat[i].tile_begin : 0x7fffffff;
   }
-  if (p.D == 32) launch_all<32>(p, a, stream);
-  else if (p.D == 64) launch_all<64>(p, a, stream);
-  else launch_all<128>(p, a, stream);
+  if (cache.k_scale) launch_cached<true>(p, a, stream);
+  else launch_cached<false>(p, a, stream);
   return hipGetLastError();
 }
 

@@ -324,4 +324,58 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
   return DA_OK;
 }
 
+int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages, int64_t page,
+                     int64_t max_pages, const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                     float softmax_scale, WeightPlan* out) {
+  constexpr int64_t kMost = int64_t{1} << 31;
+  if (!out) return DA_EINVAL;
+  PagedPlan base;  // the same sizes and patterns are valid
+  if (const int rc = make_paged_plan(T, B, H, Hkv, D, num_pages, page, max_pages, 1, patterns, num_patterns, dtype,
+                                     softmax_scale, &base);
+      rc != DA_OK)
+    return rc;
+  WeightPlan p;
+  std::memset(&p, 0, sizeof(p));
+  p.T = T; p.B = B; p.H = H; p.Hkv = Hkv; p.D = D;
+  p.num_pages = num_pages; p.page = page; p.max_pages = max_pages;
+  p.dtype = base.dtype;
+  p.page_log2 = base.page_log2;
+  p.npat = base.npat;
+  p.scale = base.scale;
+  p.lone = T <= B;
+  p.rows = p.lone ? T : B;
+  const int64_t G = H / Hkv, reach = max_pages * page;
+  auto units = [&](int64_t r) {
+    if (!p.lone) return Hkv * std::min(G, r);
+    return r >= G ? std::min(Hkv, (H + r - 1) / r) : Hkv;
+  };
+  double busy = 0.0;
+  for (int i = 0; i < p.npat; ++i) busy += static_cast<double>(p.rows) * units(base.pat[i].r);
+  for (int i = 0; i < p.npat; ++i) {
+    PagedPattern& t = p.pat[i];
+    t = base.pat[i];
+    const int64_t n = units(t.r);
+    // the positions that a row's keys can lie in, and their pages
+    const int64_t span = std::min(reach, p.lone ? int64_t{t.w} : t.w + T);
+    const int64_t pages = std::min(max_pages, span / page + 2);
+    const int64_t keys = (span + t.r - 1) / t.r;
+    const int64_t least = (pages + kWeightPages - 1) / kWeightPages;
+    const int64_t splits = std::max(
+        least, std::max<int64_t>(1, std::min({static_cast<int64_t>(2048.0 / std::max(1.0, busy) + 0.5), (keys + 255) / 256, pages})));
+    if (splits >= kMost || p.rows * n >= kMost - 8) return DA_EINVAL;
+    t.one_split = make_fastdiv(static_cast<uint32_t>(splits));
+    t.one_heads = make_fastdiv(static_cast<uint32_t>(n));
+    t.one_slot = static_cast<int32_t>(p.units);
+    t.one_begin = static_cast<int32_t>(p.items);
+    p.units += n;
+    const int64_t padded = (p.rows * n + 7) / 8 * 8;  // units XCD by XCD
+    if (padded > 0 && splits > (kMost - 1 - p.items) / padded) return DA_EINVAL;
+    p.items += padded * splits;
+  }
+  if (p.units >= kMost || (p.rows > 0 && p.units * max_pages > (int64_t{1} << 60) / p.rows)) return DA_EINVAL;
+  p.workspace_bytes = align_up(static_cast<uint64_t>(p.units) * p.rows * max_pages * 4);
+  *out = p;
+  return DA_OK;
+}
+
 }  // namespace da

@@ -155,4 +155,26 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
                     int64_t max_pages, int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns,
                     int64_t dtype, float softmax_scale, PagedPlan* out);
 
+// The attention weight that pages got from new tokens.  An item is one row (a
+// token if the call has no more of them than sequences, otherwise a sequence), one
+// unit of a pattern (a key head with those of its query heads that share a dilation
+// offset; of a single token those of its own offset) and one split of the pages that
+// its keys lie in; it writes a partial sum for each of its pages, and a second launch
+// adds a page's.  In a PagedPattern: one_split are the splits, one_heads the units,
+// one_slot the first unit's number among all, one_begin the first item.
+constexpr int64_t kWeightPages = 1024;  // pages of an item at most
+struct WeightPlan {
+  int64_t T, B, H, Hkv, D, num_pages, page, max_pages;
+  int dtype, page_log2, npat;
+  float scale;
+  bool lone;                 // rows are tokens
+  int64_t rows, units, items;
+  uint64_t workspace_bytes;  // float32 [units][rows][max_pages]
+  PagedPattern pat[DA_MAX_PATTERNS];
+};
+
+int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages, int64_t page,
+                     int64_t max_pages, const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                     float softmax_scale, WeightPlan* out);
+
 }  // namespace da

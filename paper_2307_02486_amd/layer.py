@@ -11,7 +11,7 @@ the standard attention replaced by dilated attention).
 With qk_norm the heads of q and k are RMS-normed before xPos, in the same pass
 (dilated_attn_qk_norm_xpos).  `step` is the layer for serving: new tokens of
 several sequences against a paged cache (dilated_attn_cache_append,
-dilated_attn_paged_fwd).
+dilated_attn_paged_fwd, and those of a cache in 8 bits).
 
 The residual connection belongs to the block around the layer.  The
 attention and xPos run in the library's HIP kernels (their backward passes
@@ -28,8 +28,8 @@ from typing import Sequence, Tuple
 import torch
 from torch.autograd import forward_ad
 
-from .ops import (cache_append, dilated_attn, dilated_attn_bwd, layer_norm, layer_norm_bwd, paged_attn, qk_norm_xpos,
-                  qk_norm_xpos_bwd, wgrad, xpos)
+from .ops import (cache_append, dilated_attn, dilated_attn_bwd, layer_norm, layer_norm_bwd, page_weights, paged_attn,
+                  qk_norm_xpos, qk_norm_xpos_bwd, wgrad, xpos)
 from .serving import check_xpos
 
 
@@ -264,9 +264,11 @@ class LongNetAttention(torch.nn.Module):
         keys and values go to `cache` (a PagedCache and one of its batches, for
         the cache's layer `layer`) and which attend to what is there of their
         own sequence: what forward gives on whole sequences, row by row (up to
-        rounding: xPos is centred on the cache's centre).  Rows of x past the
-        batch's tokens are of no sequence.  Causal layers only, without
-        gradients and not under torch.jit.trace."""
+        rounding: xPos is centred on the cache's centre; a cache in 8 bits rounds
+        its keys and values).  Rows of x past the batch's tokens are of no
+        sequence.  A cache that counts its pages' weights has this layer's
+        added.  Causal layers only, without gradients and not under
+        torch.jit.trace."""
         if torch.jit.is_tracing():
             raise RuntimeError("step cannot be traced: a trace sees nothing of the kernels that it calls")
         if not self.causal:
@@ -282,9 +284,12 @@ class LongNetAttention(torch.nn.Module):
         u = _layer_norm(self.ln_in, x)
         q, k, v = (_linear(m, u).view(T, H, D) for m in (self.q_proj, self.k_proj, self.v_proj))
         where = (cache.k[layer], cache.v[layer], batch.block_table, batch.seq_lens, batch.q_start)
+        scales = {} if cache.k_scale is None else dict(k_scale=cache.k_scale[layer], v_scale=cache.v_scale[layer])
         q = cache_append(q, k, v, *where, self.q_norm, self.k_norm, self.qk_eps, self.use_xpos, cache.center,
-                         *self.xpos_args)
-        a = paged_attn(q, *where, self.patterns, max_new=batch.max_new)[0]
+                         *self.xpos_args, **scales)
+        a, lse = paged_attn(q, *where, self.patterns, max_new=batch.max_new, **scales)
+        if cache.weights is not None:
+            page_weights(q, lse, cache.k[layer], scales["k_scale"], *where[2:], self.patterns, cache.weights)
         return _linear(self.out_proj, _layer_norm(self.ln_sub, a.view(T, H * D)))
 
     def float64_params(self) -> dict:

@@ -3,9 +3,9 @@
 `plan`/`dilated_attn`, `plan_bwd`/`dilated_attn_bwd` and `xpos` mirror the
 C ABI (dilated_attn_plan / dilated_attn_fwd, dilated_attn_bwd_plan /
 dilated_attn_bwd, dilated_attn_xpos), and so do `qk_norm_xpos` and its
-gradients, `cache_append` and `paged_attn`: torch supplies device memory and
-the stream, every step of the computation runs in the HIP kernels of
-libdilated_attn.so.
+gradients, `cache_append` and `paged_attn` (both also on a cache in 8 bits),
+`page_weights` and `evict_pages`: torch supplies device memory and the stream,
+every step of the computation runs in the HIP kernels of libdilated_attn.so.
 """
 from __future__ import annotations
 
@@ -426,6 +426,7 @@ def _contiguous_like(t: torch.Tensor) -> torch.Tensor:
 _HEADS: dict = {}
 _APPENDS: dict = {}
 _PAGED: dict = {}
+_WEIGHTS: dict = {}
 
 
 def _keep(known: dict, key, value):
@@ -520,6 +521,32 @@ def _cache_shape(k_cache: torch.Tensor, block_table: torch.Tensor, D: int):
     return B, Hkv, pages, page, max_pages
 
 
+CACHE_F8 = torch.float8_e4m3fn  # values of a cache in 8 bits
+CACHE_SCALE = torch.float8_e8m0fnu  # powers of two, one for each block of tokens and key head
+CACHE_BLOCK = 16  # tokens of a block (a page of fewer is one block)
+
+
+def cache_scale_shape(k_cache: torch.Tensor) -> tuple:
+    """[num_pages, Hkv, blocks of a page]: the shape of the scales of a cache in 8 bits."""
+    pages, Hkv, page, _ = k_cache.shape
+    return pages, Hkv, page // min(page, CACHE_BLOCK)
+
+
+def _check_scale(name: str, scale, cache: torch.Tensor):
+    """Refuse a cache in 8 bits without its scales, or with others than its own."""
+    if scale is None:
+        raise ValueError(f"a cache in 8 bits needs {name}")
+    if scale.dtype != CACHE_SCALE or scale.get_device() != cache.get_device() or not scale.is_contiguous() \
+            or scale.shape != cache_scale_shape(cache):
+        raise ValueError(f"{name} must be a contiguous {CACHE_SCALE} tensor of shape {list(cache_scale_shape(cache))} "
+                         f"on the cache's device")
+
+
+def _cache_args(k_cache, v_cache, block_table, seq_lens, q_start, pages, page, max_pages):
+    return _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                               q_start.data_ptr(), pages, page, max_pages)
+
+
 def _check_cache(dev: int, dtype, B: int, k_cache, v_cache, block_table, seq_lens, q_start):
     """Refuse cache tensors of another type, device, shape or layout than the call's."""
     i32 = torch.int32
@@ -540,7 +567,8 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
                  v_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, q_start: torch.Tensor,
                  q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
                  rotate: bool = True, center: int = 0, base: float = 10000.0, gamma: float = 0.4,
-                 scale_base: float = 512.0, stream: torch.cuda.Stream | None = None):
+                 scale_base: float = 512.0, stream: torch.cuda.Stream | None = None,
+                 k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
     """New keys and values into a paged cache, the keys normed (with k_weight)
     and rotated by xPos on the way; returns the queries normed (with q_weight)
     and rotated, [T, H, D], or None without q.
@@ -550,7 +578,13 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
     They are the last of its seq_lens[b] tokens (int32 [B]).  Token p lies in
     page block_table[b, p // page_size] (int32 [B, max_pages]) of k_cache and
     v_cache [num_pages, Hkv, page_size, D], page_size a power of two.  `center`
-    is the xPos centre, the same for the life of a cache.  Enqueued on `stream`."""
+    is the xPos centre, the same for the life of a cache.  Enqueued on `stream`.
+
+    A cache in 8 bits: k_cache and v_cache are float8_e4m3fn, k_scale and v_scale
+    float8_e8m0fnu [num_pages, Hkv, page_size / 16] (cache_scale_shape), a power of
+    two for each block of 16 tokens and key head.  An element is its e4m3 value
+    times its block's scale, the least that cuts no value off; a block keeps its
+    scale or takes a larger one as tokens come, its older values then rescaled."""
     lib = _lib.load()
     key = (None if q is None else (q.shape, q.stride()), k.shape, k.stride(), v.shape, v.stride(), k.dtype,
            k_cache.shape, block_table.shape)
@@ -575,7 +609,13 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
     dev, dt = k.get_device(), k.dtype
     if dev < 0:
         raise RuntimeError("cache_append runs on the GPU only; k must be a device tensor")
-    _check_cache(dev, dt, B, k_cache, v_cache, block_table, seq_lens, q_start)
+    f8 = k_cache.dtype == CACHE_F8
+    _check_cache(dev, CACHE_F8 if f8 else dt, B, k_cache, v_cache, block_table, seq_lens, q_start)
+    if f8:
+        _check_scale("k_scale", k_scale, k_cache)
+        _check_scale("v_scale", v_scale, v_cache)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError(f"k_scale and v_scale go with a cache of {CACHE_F8}")
     if v.dtype != dt or v.get_device() != dev:
         raise ValueError(f"v must be a {dt} tensor on {k.device}")
     qo = None
@@ -589,10 +629,13 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
         _check_like("q_weight", q_weight, (D,), dt, k.device)
     if k_weight is not None:
         _check_like("k_weight", k_weight, (D,), dt, k.device)
-    cache = _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-                                q_start.data_ptr(), pages, page, max_pages)
+    cache, append = _cache_args(k_cache, v_cache, block_table, seq_lens, q_start, pages, page, max_pages), \
+        lib.dilated_attn_cache_append
+    if f8:
+        cache, append = _lib.PagedCacheF8Args(cache, k_scale.data_ptr(), v_scale.data_ptr()), \
+            lib.dilated_attn_cache_append_f8
     raw = _raw_stream(k.device) if stream is None else stream.cuda_stream
-    rc = lib.dilated_attn_cache_append(
+    rc = append(
         None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
         None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
         None if qo is None else qo.data_ptr(), cache, T, B, H, Hkv, D, qs, ks, vs, float(eps),
@@ -619,7 +662,8 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
                seq_lens: torch.Tensor, q_start: torch.Tensor, patterns: Sequence[Tuple[int, int]],
                max_new: int | None = None, scale: float | None = None, out: torch.Tensor | None = None,
                lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-               stream: torch.cuda.Stream | None = None):
+               stream: torch.cuda.Stream | None = None, k_scale: torch.Tensor | None = None,
+               v_scale: torch.Tensor | None = None):
     """Causal dilated attention of new tokens q [T, H, D] over a paged cache that
     holds their keys and values already (see cache_append for the cache and
     the sequences' arrays): a token at position p gets what row p of
@@ -629,7 +673,11 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
     spares what only longer ones need where it is at most 4.  Returns (out
     [T, H, D], lse [H, T] float32); a token of no sequence has zeros and -inf.
     Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor of
-    at least paged_workspace_bytes."""
+    at least paged_workspace_bytes.
+
+    A cache in 8 bits comes with k_scale and v_scale, as for cache_append.  Its
+    table may name pages outside the pool (-1, say): they hold no keys, and a row
+    all of whose keys are gone has zeros and -inf."""
     lib = _lib.load()
     patterns = tuple(patterns)
     shapes = (q.shape, q.stride(), q.dtype, k_cache.shape, block_table.shape, max_new)
@@ -653,7 +701,13 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
     dev = q.get_device()
     if dev < 0:
         raise RuntimeError("paged_attn runs on the GPU only; q must be a device tensor")
-    _check_cache(dev, q.dtype, B, k_cache, v_cache, block_table, seq_lens, q_start)
+    f8 = k_cache.dtype == CACHE_F8
+    _check_cache(dev, CACHE_F8 if f8 else q.dtype, B, k_cache, v_cache, block_table, seq_lens, q_start)
+    if f8:
+        _check_scale("k_scale", k_scale, k_cache)
+        _check_scale("v_scale", v_scale, v_cache)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError(f"k_scale and v_scale go with a cache of {CACHE_F8}")
     owned = []
     if out is None:
         out = _contiguous_like(q)
@@ -672,11 +726,14 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
         if workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
         nbytes = workspace.numel()
-    cache = _lib.PagedCacheArgs(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-                                q_start.data_ptr(), pages, page, max_pages)
+    cache, attend = _cache_args(k_cache, v_cache, block_table, seq_lens, q_start, pages, page, max_pages), \
+        lib.dilated_attn_paged_fwd
+    if f8:
+        cache, attend = _lib.PagedCacheF8Args(cache, k_scale.data_ptr(), v_scale.data_ptr()), \
+            lib.dilated_attn_paged_fwd_f8
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
-    rc = lib.dilated_attn_paged_fwd(q.data_ptr(), cache, out.data_ptr(), lse.data_ptr(), T, B, H, Hkv, D, qs, new, arr,
-                                    n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
+    rc = attend(q.data_ptr(), cache, out.data_ptr(), lse.data_ptr(), T, B, H, Hkv, D, qs, new, arr, n, dcode,
+                float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, owned)
@@ -690,3 +747,115 @@ def paged_workspace_bytes(T: int, B: int, H: int, Hkv: int, D: int, num_pages: i
     shape = (int(T), int(B), int(H), int(Hkv), int(D), int(num_pages), int(page_size), int(max_pages),
              int(T if max_new is None else max_new))
     return _paged_workspace(shape, _pattern_key(patterns), _dtype_code(dtype))
+
+
+@functools.lru_cache(maxsize=256)
+def _weight_workspace(shape: tuple, pats: tuple, dtype_code: int) -> int:
+    lib = _lib.load()
+    arr, n = _pattern_array_cached(pats)
+    need = ctypes.c_uint64(0)
+    rc = lib.dilated_attn_page_weights_workspace(*shape, arr, n, dtype_code, ctypes.byref(need))
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    return need.value
+
+
+def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_scale: torch.Tensor,
+                 block_table: torch.Tensor, seq_lens: torch.Tensor, q_start: torch.Tensor,
+                 patterns: Sequence[Tuple[int, int]], weights: torch.Tensor, scale: float | None = None,
+                 workspace: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
+    """The attention that each page of a cache in 8 bits gets from the new tokens,
+    added to weights (float32 [num_pages], which is returned): over the page's
+    keys, the tokens q [T, H, D] of its sequence that see them, their heads and
+    the patterns that hold the pair, the sum of exp(scale q.k - lse).
+
+    q, the cache and the sequences' arrays are those of paged_attn, lse [H, T]
+    what it returned; a row without a finite lse adds nothing.  Each head of a
+    token that sees a key adds one in all.  A page belongs to one sequence of the
+    call.  Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor
+    of at least page_weights_workspace_bytes."""
+    lib = _lib.load()
+    patterns = tuple(patterns)
+    shapes = (q.shape, q.stride(), q.dtype, k_cache.shape, block_table.shape)
+    try:
+        call = _WEIGHTS.get((shapes, patterns))
+    except TypeError:  # patterns given as lists
+        call = None
+    if call is None:
+        if q.device.type != "cuda":
+            raise RuntimeError("page_weights runs on the GPU only; q must be a device tensor")
+        if q.dim() != 3:
+            raise ValueError("q must be [T, H, D]")
+        T, H, D = q.shape
+        B, Hkv, pages, page, max_pages = _cache_shape(k_cache, block_table, D)
+        dcode, pats = _dtype_code(q.dtype), _pattern_key(patterns)
+        need = _weight_workspace((T, B, H, Hkv, D, pages, page, max_pages), pats, dcode)
+        call = _keep(_WEIGHTS, (shapes, pats), (T, B, H, Hkv, D, _token_stride("q", q, 1, q.dtype, q.device), dcode, pages,
+                                                page, max_pages, max(need, 16), *_pattern_array_cached(pats)))
+    T, B, H, Hkv, D, qs, dcode, pages, page, max_pages, need, arr, n = call
+    dev = q.get_device()
+    if dev < 0:
+        raise RuntimeError("page_weights runs on the GPU only; q must be a device tensor")
+    if k_cache.dtype != CACHE_F8:
+        raise ValueError(f"k_cache must be a {CACHE_F8} tensor, a cache in 8 bits")
+    _check_cache(dev, CACHE_F8, B, k_cache, k_cache, block_table, seq_lens, q_start)
+    _check_scale("k_scale", k_scale, k_cache)
+    _check_like("lse", lse, (H, T), torch.float32, q.device)
+    _check_like("weights", weights, (pages,), torch.float32, q.device)
+    owned = []
+    if workspace is None:
+        workspace, nbytes = q.new_empty(need, dtype=torch.uint8), need
+        owned.append(workspace)
+    else:
+        if workspace.dtype != torch.uint8 or workspace.device != q.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous uint8 tensor on q's device")
+        nbytes = workspace.numel()
+    cache = _lib.PagedCacheF8Args(_cache_args(k_cache, k_cache, block_table, seq_lens, q_start, pages, page, max_pages),
+                                  k_scale.data_ptr(), None)
+    raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
+    rc = lib.dilated_attn_page_weights(q.data_ptr(), lse.data_ptr(), cache, weights.data_ptr(), T, B, H, Hkv, D, qs, arr,
+                                       n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    _stream_use(stream, owned)
+    return weights
+
+
+def page_weights_workspace_bytes(T: int, B: int, H: int, Hkv: int, D: int, num_pages: int, page_size: int,
+                                 max_pages: int, patterns: Sequence[Tuple[int, int]], dtype=torch.bfloat16) -> int:
+    """Validate a page_weights problem and return the workspace it needs (host only)."""
+    shape = (int(T), int(B), int(H), int(Hkv), int(D), int(num_pages), int(page_size), int(max_pages))
+    return _weight_workspace(shape, _pattern_key(patterns), _dtype_code(dtype))
+
+
+def evict_pages(weights: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, page_size: int, keep: int,
+                first: int = 1, last: int = 1, stream: torch.cuda.Stream | None = None):
+    """The pages of least weight out of each sequence's table, until it has `keep`.
+
+    weights float32 [num_pages], block_table int32 [B, max_pages], seq_lens int32
+    [B]; entries of a row outside [0, num_pages) are pages that are not there.  Of
+    equal weights the page that comes first goes.  The row's first `first` entries
+    and the last `last` of those that its length reaches into never go.  Returns
+    (table, freed, count): the table with -1 for what goes, the pages that go in
+    the row's order and -1 after them [B, max_pages], and how many they are [B].
+    Enqueued on `stream`."""
+    lib = _lib.load()
+    dev = weights.get_device()
+    if dev < 0:
+        raise RuntimeError("evict_pages runs on the GPU only; weights must be a device tensor")
+    if block_table.dim() != 2 or weights.dim() != 1:
+        raise ValueError("weights must be [num_pages] and block_table [B, max_pages]")
+    B, max_pages = block_table.shape
+    _check_like("weights", weights, weights.shape, torch.float32, weights.device)
+    _check_like("block_table", block_table, (B, max_pages), torch.int32, weights.device)
+    _check_like("seq_lens", seq_lens, (B,), torch.int32, weights.device)
+    table, freed = torch.empty_like(block_table), torch.empty_like(block_table)
+    count = torch.empty_like(seq_lens)
+    raw = _raw_stream(weights.device) if stream is None else stream.cuda_stream
+    rc = lib.dilated_attn_evict_pages(weights.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), table.data_ptr(),
+                                      freed.data_ptr(), count.data_ptr(), B, weights.numel(), int(page_size), max_pages,
+                                      int(keep), int(first), int(last), raw)
+    if rc != 0:
+        raise _lib.DilatedAttnError(rc, lib)
+    _stream_use(stream, [table, freed, count])
+    return table, freed, count

@@ -9,6 +9,8 @@ from typing import NamedTuple, Sequence
 
 import torch
 
+from .ops import CACHE_F8, CACHE_SCALE, cache_scale_shape, evict_pages
+
 
 def xpos_span(gamma: float, scale_base: float) -> int:
     """How far from the xPos centre a position may lie: its scale is at most 2^64
@@ -61,11 +63,17 @@ class PagedCache:
     positions (36261 with their defaults), and the whole table has to fit.  xpos,
     the layers' (gamma, scale_base), checks that here; otherwise their first step
     refuses.
+
+    dtype float8_e4m3fn makes a cache in 8 bits, whose scales are the lists k_scale
+    and v_scale.  With weigh=True it counts in `weights` (float32 [num_pages]) the
+    attention that its pages get in each step, all layers together, and `evict` gives
+    up the pages that got least.  Pages of a sequence that are gone are -1 in its
+    table; its tokens keep their positions.
     """
 
     def __init__(self, num_pages: int, page_size: int, max_pages: int, num_heads: int, head_dim: int,
                  layers: int = 1, center: int | None = None, device=None, dtype=torch.bfloat16,
-                 xpos: tuple | None = None):
+                 xpos: tuple | None = None, weigh: bool = False):
         if page_size < 1 or page_size & (page_size - 1):
             raise ValueError("page_size must be a power of two")
         if num_pages < 1 or max_pages < 1 or layers < 1:
@@ -76,6 +84,15 @@ class PagedCache:
         shape = (num_pages, num_heads, page_size, head_dim)
         self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
         self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
+        self.k_scale = self.v_scale = self.weights = None
+        if dtype == CACHE_F8:
+            scales = dict(size=cache_scale_shape(self.k[0]), device=device, dtype=CACHE_SCALE)
+            self.k_scale = [torch.empty(**scales) for _ in range(layers)]
+            self.v_scale = [torch.empty(**scales) for _ in range(layers)]
+        if weigh:
+            if dtype != CACHE_F8:
+                raise ValueError(f"weigh goes with a cache of {CACHE_F8}")
+            self.weights = torch.zeros(num_pages, device=device)
         self.page_size, self.max_pages = page_size, max_pages
         self.device = self.k[0].device
         self._free = list(range(num_pages - 1, -1, -1))
@@ -90,7 +107,7 @@ class PagedCache:
 
     def release(self, sequence):
         """Forget a sequence; its pages go back to the pool."""
-        self._free += self._pages.pop(sequence, [])
+        self._free += [p for p in self._pages.pop(sequence, []) if p >= 0]
         self._length.pop(sequence, None)
         self._last.pop(sequence, None)
 
@@ -103,10 +120,43 @@ class PagedCache:
         for s, n in zip(batch.sequences, batch.new):
             self._length[s] -= n
             pages, keep = self._pages[s], -(-self._length[s] // self.page_size)
-            self._free += reversed(pages[keep:])
+            self._free += [p for p in reversed(pages[keep:]) if p >= 0]
             del pages[keep:], self._last[s]
             if self._length[s] == 0:
                 self.release(s)
+
+    def evict(self, keep: int, sequences: Sequence | None = None, first: int = 1, last: int = 1) -> int:
+        """Give up the pages of least weight of each of these sequences (default:
+        all), until it has `keep`; never its first `first` pages nor its last `last`
+        (see evict_pages).  They go back to the pool.  Only between steps: a batch
+        made before names them still.  Waits for the GPU.  Returns how many went."""
+        if self.weights is None:
+            raise ValueError("evict needs a cache that counts its pages' weights (weigh=True)")
+        if keep < 0 or first < 0 or last < 0:
+            raise ValueError("keep, first and last must not be negative")
+        names = list(self._pages if sequences is None else sequences)
+        if len(set(names)) != len(names) or any(s not in self._pages for s in names):
+            raise ValueError("sequences must be different ones that the cache holds")
+        if not names:
+            return 0
+        lens = torch.tensor([self._length[s] for s in names], dtype=torch.int32).to(self.device)
+        _, freed, count = evict_pages(self.weights, self._table(names).to(self.device), lens, self.page_size, keep,
+                                      first, last)
+        freed, count = freed.cpu(), count.tolist()
+        for s, row, n in zip(names, freed, count):
+            if n:
+                gone = set(row[:n].tolist())
+                self._pages[s] = [-1 if p in gone else p for p in self._pages[s]]
+                self._free += reversed(sorted(gone))
+                self._last.pop(s, None)  # a batch made before cannot be taken back
+        return sum(count)
+
+    def _table(self, names: Sequence) -> torch.Tensor:
+        """The rows of these sequences in a table on the host."""
+        table = torch.full((len(names), self.max_pages), -1 if self.k_scale is not None else 0, dtype=torch.int32)
+        for i, s in enumerate(names):
+            table[i, : len(self._pages[s])] = torch.tensor(self._pages[s], dtype=torch.int32)
+        return table
 
     def extend(self, sequences: Sequence, new: Sequence[int]) -> Batch:
         """Room for `new` more tokens of each sequence (named for the first time,
@@ -126,12 +176,14 @@ class PagedCache:
         if sum(short) > len(self._free):
             raise RuntimeError(f"{sum(short)} pages are needed and {len(self._free)} are free")
         self._number += 1
-        table = torch.zeros((len(need), self.max_pages), dtype=torch.int32)
-        for i, (s, n, more) in enumerate(zip(sequences, lengths, short)):
-            pages = self._pages.setdefault(s, [])
-            pages += [self._free.pop() for _ in range(more)]
+        taken = []
+        for s, n, more in zip(sequences, lengths, short):
+            taken += (fresh := [self._free.pop() for _ in range(more)])
+            self._pages.setdefault(s, []).extend(fresh)
             self._length[s], self._last[s] = n, self._number
-            table[i, : len(pages)] = torch.tensor(pages, dtype=torch.int32)
+        table = self._table(sequences)
+        if self.weights is not None and taken:  # whoever had these pages before, they begin without weight
+            self.weights[torch.tensor(taken, device=self.device)] = 0.0
         start = torch.zeros(len(need) + 1, dtype=torch.int32)
         start[1:] = torch.tensor(new, dtype=torch.int32).cumsum(0)
         lens = torch.tensor(lengths, dtype=torch.int32)
