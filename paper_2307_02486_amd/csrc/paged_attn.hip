@@ -104,9 +104,13 @@ template <bool kMixed>
 __device__ inline bool single_token(const PagedArgs& a, int e, int lane, Token& t) {
   Sequence sq[1] = {Sequence{-1, 0, 0, 0}};
   if constexpr (!kMixed) {
+    // Most often row e is sequence e's only one: that much in one round of loads.
+    const int b = min(e, a.B - 1);
+    const Sequence guess{b, a.start[b], a.start[b + 1], a.lens[b]};
     const int tok[1] = {e};
     t.tok = e;
-    find_sequences(a, tok, lane, sq);
+    if (guess.begin == e && guess.end == e + 1) sq[0] = guess;
+    else find_sequences(a, tok, lane, sq);
   } else {
     t.tok = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -177,107 +181,135 @@ struct KeyFrag {
 
 constexpr int kOneTile = 32;    // keys of a wave's tile
 constexpr int kOneRows = 1024;  // keys whose rows are looked up at once
-template <int D, bool kF8>
+template <int D>
 struct SmemOne {
   __attribute__((aligned(16))) char v[kPgWaves][kOneTile * D * 2];  // each wave's V tile
   float ml[kPgWaves][2][16];
   u32x4 q[D / 32][64];     // Q^T operand, lane by lane
   uint32_t row[kOneRows];  // cache rows of the split's keys, a chunk at a time
-  uint64_t gone[kF8 ? kOneRows / 64 : 0];  // their keys of no page
 };
 
-template <int D, bool kMixed, bool kF8>
-__device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, SmemOne<D, kF8>& sm) {
-  constexpr int KC = D / 32, DB = D / 16, kTile = kOneTile;
-  using TL = TileLayout<D>;
-  // An 8-bit row of V is half as many 16-byte loads, each two slots of the tile.
-  constexpr int kVPieces = kF8 ? D / 16 : TL::kSlots;  // 16-byte pieces of a cached row
-  constexpr int kVLoads = kTile * kVPieces / 64;
-  using Keys = typename std::conditional<kF8, KeyFrag8<D>, KeyFrag<D>>::type;
-  // Joined rows are D floats apart, 16-byte chunk c of row r at c ^ (r mod D/4).
-  auto join_at = [](int r, int chunk) { return r * D + 4 * (chunk ^ (r & (D / 4 - 1))); };
-  static_assert(16 * D * 4 <= kTile * D * 2, "the join fits a wave's V tile");
-  auto& sv = sm.v;
-  auto& sml = sm.ml;
-
-  const int tid = thread_id(), lane = tid & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int pi = it.pi;
-  const PagedPattern& P = a.pat[pi];
+// What a single-token item has to do: a token, the query heads of a key head that
+// share its keys, and the split [k0, ke) of these.
+struct OneWork {
   Token tk;
-  if (!single_token<kMixed>(a, it.e, lane, tk)) return;
-  const Lattice lat = lattice_of(P, tk.pos);
+  Lattice lat;
+  KeptHeads kh;
+  int hk, m0, rows, k0, ke;  // key head; first of its kept query heads here and how many
+};
+template <bool kMixed>
+__device__ inline bool one_work(const PagedArgs& a, const OneItem& it, int lane, OneWork& w) {
+  const PagedPattern& P = a.pat[it.pi];
+  if (!single_token<kMixed>(a, it.e, lane, w.tk)) return false;
+  w.lat = lattice_of(P, w.tk.pos);
   // Dilations of a group's size and above keep one head of a group at most: the
   // head-th kept one; below, every group has some, in blocks.
-  int hk = it.head, block = 0;
+  int block = 0;
+  w.hk = it.head;
   if (P.r >= a.G) {
-    const int64_t h = lat.rho + static_cast<int64_t>(it.head) * P.r;
-    if (h >= a.H) return;
-    hk = static_cast<int>(h) / a.G;
+    const int64_t h = w.lat.rho + static_cast<int64_t>(it.head) * P.r;
+    if (h >= a.H) return false;
+    w.hk = static_cast<int>(h) / a.G;
   } else if (a.G > static_cast<int>(kPagedGroupRows)) {
     block = it.head / a.Hkv;
-    hk = it.head - block * a.Hkv;
+    w.hk = it.head - block * a.Hkv;
   }
-  const KeptHeads kh = kept_heads(P, hk, a.G, lat.rho);
-  const int m0 = block * static_cast<int>(kPagedGroupRows);
-  if (m0 >= kh.count) return;
-  const int rows = min(static_cast<int>(kPagedGroupRows), kh.count - m0);
-  const int n = own_keys(a, P, pi == a.full, tk.pos, lat), per = split_keys_of(P, n);
-  const int k0 = it.split * per;
-  if (k0 >= n) return;
-  const int ke = min(k0 + per, n);
+  w.kh = kept_heads(P, w.hk, a.G, w.lat.rho);
+  w.m0 = block * static_cast<int>(kPagedGroupRows);
+  if (w.m0 >= w.kh.count) return false;
+  w.rows = min(static_cast<int>(kPagedGroupRows), w.kh.count - w.m0);
+  const int n = own_keys(a, P, it.pi == a.full, w.tk.pos, w.lat), per = split_keys_of(P, n);
+  w.k0 = it.split * per;
+  w.ke = min(w.k0 + per, n);
+  return w.k0 < n;
+}
+// Patterns whose keys this item reads too, for any head of it and for the lane's.
+struct Shared {
+  unsigned with, mine;
+};
+__device__ inline Shared shared_patterns(const PagedArgs& a, const OneItem& it, const OneWork& w, int lane) {
+  Shared x{0, 0};
+  if (it.pi != a.full || a.npat == 1) return x;
+  const PagedPattern Q = a.pat[lane & 15];  // a pattern per lane
+  const bool there = lane < a.npat && lane != it.pi;
+  const int rho = there ? lattice_of(Q, w.tk.pos).rho : 0;
+  for (int r = 0; r < w.rows; ++r) {
+    const bool kept = there && head_offset(Q, w.kh.first + (w.m0 + r) * a.pat[it.pi].r) == rho;
+    const unsigned mask = static_cast<unsigned>(__ballot(kept));
+    x.with |= mask;
+    if ((lane & 15) == r) x.mine = mask;
+  }
+  return x;
+}
+
+// The waves' partial rows (acc, reference m_run and sum l_run) meet in LDS, each in
+// its wave's own V tile, and go to the workspace.
+template <int D>
+__device__ inline void store_one(const PagedArgs& a, const OneItem& it, const OneWork& work, const f32x4 (&acc)[D / 16],
+                                 float m_run, float l_run, char (&sv)[kPgWaves][kOneTile * D * 2],
+                                 float (&sml)[kPgWaves][2][16], int tid, int wv) {
+  constexpr int DB = D / 16;
+  // Joined rows are D floats apart, 16-byte chunk c of row r at c ^ (r mod D/4).
+  auto join_at = [](int r, int chunk) { return r * D + 4 * (chunk ^ (r & (D / 4 - 1))); };
+  static_assert(16 * D * 4 <= kOneTile * D * 2, "the join fits a wave's V tile");
+  const PagedPattern& P = a.pat[it.pi];
+  const int lane = tid & 63, m = lane & 15, grp = lane >> 4;
+  l_run = sum_over_groups(l_run);
+  float* jo = reinterpret_cast<float*>(sv[wv]);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(jo + join_at(m, 4 * db + grp)) = acc[db];
+  if (grp == 0) {
+    sml[wv][0][m] = m_run;
+    sml[wv][1][m] = l_run;
+  }
+  __syncthreads();
+  const int64_t row0 = static_cast<int64_t>(it.e) * a.H;
+  for (int x = tid; x < work.rows * (D / 4); x += kPgThreads) {
+    const int r = x / (D / 4), d = (x % (D / 4)) * 4;
+    float mt = sml[0][0][r];
+#pragma unroll
+    for (int w = 1; w < kPgWaves; ++w) mt = fmaxf(mt, sml[w][0][r]);
+    float l = 0.0f;
+    f32x4 o = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kPgWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sml[w][0][r] - mt);
+      l += f * sml[w][1][r];
+      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(sv[w]) + join_at(r, d / 4));
+    }
+    const int64_t at = (row0 + work.kh.first + (work.m0 + r) * P.r) * a.one_slots + P.one_slot + it.split;
+    o *= l > 0.0f ? 1.0f / l : 0.0f;
+    *reinterpret_cast<f32x4*>(a.ws + a.one_row + (at * D + d) * 4) = o;
+    if (d == 0) reinterpret_cast<float*>(a.ws + a.one_rec)[at] = mt + __builtin_amdgcn_logf(l);
+  }
+}
+
+template <int D, bool kMixed>
+__device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, SmemOne<D>& sm) {
+  constexpr int KC = D / 32, DB = D / 16, kTile = kOneTile;
+  using TL = TileLayout<D>;
+  constexpr int kVLoads = kTile * TL::kSlots / 64;
+  const int tid = thread_id(), lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  OneWork w;
+  if (!one_work<kMixed>(a, it, lane, w)) return;
+  const PagedPattern& P = a.pat[it.pi];
+  const Token& tk = w.tk;
+  const int hk = w.hk, rows = w.rows, k0 = w.k0, ke = w.ke;
 
   const int m = lane & 15, grp = lane >> 4;
-  const int head = kh.first + (m0 + min(m, rows - 1)) * P.r;
+  const int head = w.kh.first + (w.m0 + min(m, rows - 1)) * P.r;
   // Q^T operand (kept in LDS: in registers it would spill at D = 128).
   for (int c = wv; c < KC; c += kPgWaves) {
-    const int d0 = kF8 ? step_first<D>(c, grp) : 32 * c + 8 * grp;
-    const u32x4 x = load16(static_cast<const u16*>(a.q) + tk.tok * a.qs + head * D + d0);
+    const u32x4 x = load16(static_cast<const u16*>(a.q) + tk.tok * a.qs + head * D + 32 * c + 8 * grp);
     sm.q[c][lane] = m < rows ? x : u32x4{0u, 0u, 0u, 0u};
   }
 
   const int32_t* table = a.table + static_cast<int64_t>(tk.b) * a.max_pages;
-  const int base = lat.first;
-  // Patterns whose keys this one reads too, for any head here and for the lane's.
-  unsigned with = 0, mine = 0;
-  if (pi == a.full && a.npat > 1) {
-    const PagedPattern Q = a.pat[lane & 15];  // a pattern per lane
-    const bool there = lane < a.npat && lane != pi;
-    const int rho = there ? lattice_of(Q, tk.pos).rho : 0;
-    for (int r = 0; r < rows; ++r) {
-      const bool kept = there && head_offset(Q, kh.first + (m0 + r) * P.r) == rho;
-      const unsigned mask = static_cast<unsigned>(__ballot(kept));
-      with |= mask;
-      if (m == r) mine = mask;
-    }
-  }
-  constexpr int kVStep = 64 / kVPieces;  // V rows of a load
-  const int vrow = lane / kVPieces, vpiece = lane % kVPieces;
-  char* my = sv[wv];
-  // Requests the 32 keys from `key` on (counted within the chunk whose rows are in LDS).
-  auto request_k = [&](int key, Keys& kf) {
-    if constexpr (kF8) {
-      request_keys8<D>(a, sm.row + key, m, grp, kf);
-    } else {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const char* p = a.kc + (static_cast<int64_t>(sm.row[key + 16 * u + m]) * TL::kRowBytes + 16 * grp);
-#pragma unroll
-        for (int c = 0; c < KC; ++c) kf.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
-      }
-    }
-  };
-  u32x4 vreg[kVLoads];
-  uint32_t vscale[kVLoads];
-  auto request_v = [&](int key) {
-#pragma unroll
-    for (int i = 0; i < kVLoads; ++i) {
-      const uint32_t row = sm.row[key + kVStep * i + vrow];
-      vreg[i] = *reinterpret_cast<const u32x4*>(
-          a.vc + (static_cast<int64_t>(row) * (kVPieces * 16) + vpiece * 16));
-      if constexpr (kF8) vscale[i] = a.vs[row >> a.block_log2];
-    }
-  };
+  const int base = w.lat.first;
+  const Shared shared = shared_patterns(a, it, w, lane);
+  const unsigned with = shared.with, mine = shared.mine;
+  char* my = sm.v[wv];
   // V^T operand: lane's d = 16 db + (lane & 15), keys 4 grp + 0..3 and 16 more.
   // Block db's 16-byte slots are 2 db and 2 db + 1 before the swizzle, an
   // exclusive or: its address is block 0's with bits of db flipped.
@@ -289,34 +321,34 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
   for (int db = 0; db < DB; ++db) acc[db] = f32x4{0, 0, 0, 0};
   float m_run = kLowest, l_run = 0.0f;
   const float c2 = a.scale_log2;
-  int chunk = k0;  // first key of the chunk whose rows are in LDS
 
+  constexpr int kVStep = 64 / TL::kSlots;  // V rows of a load
+  const int vrow = lane / TL::kSlots;
+  // Requests the 32 keys from `key` on (counted within the chunk whose rows are in LDS).
+  auto request_k = [&](int key, KeyFrag<D>& kf) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const char* p = a.kc + (static_cast<int64_t>(sm.row[key + 16 * u + m]) * TL::kRowBytes + 16 * grp);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) kf.k[u][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+    }
+  };
+  u32x4 vreg[kVLoads];
+  auto request_v = [&](int key) {
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i)
+      vreg[i] = *reinterpret_cast<const u32x4*>(
+          a.vc + (static_cast<int64_t>(sm.row[key + kVStep * i + vrow]) * TL::kRowBytes + (lane % TL::kSlots) * 16));
+  };
   // first: the tile's first key (t); next: the next tile's, within the chunk, < 0: none
-  auto compute = [&](int first, const Keys& kf, int next) {
+  auto compute = [&](int first, const KeyFrag<D>& kf, int next) {
     f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       const bf16x8 qf = __builtin_bit_cast(bf16x8, sm.q[c][lane]);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        u32x4 k;
-        if constexpr (kF8) k = widen8(kf.k[u][2 * c], kf.k[u][2 * c + 1], scale_of(kf.scale[u]));
-        else k = kf.k[u][c];
-        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), qf, s[u], 0, 0, 0);
-      }
-    }
-    uint32_t gone = 0;
-    if constexpr (kF8) {  // keys of no page (rows of the wave's tile: half a word)
-      const int local = first - chunk;
-      gone = uniform(static_cast<uint32_t>(sm.gone[local >> 6] >> (local & 32)));
-      if (gone) {
-        const uint32_t mine4 = gone >> (4 * grp);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (mine4 >> (16 * u + e) & 1) s[u][e] = -INFINITY;
-      }
+      for (int u = 0; u < 2; ++u)
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf.k[u][c]), qf, s[u], 0, 0, 0);
     }
     const int left = ke - first - 4 * grp;  // keys from this lane's first on
 #pragma unroll
@@ -364,27 +396,9 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
       }
     // V through the wave's own LDS tile, to be read transposed (LDS operations
     // of a wave complete in order: no wait between).
-    if constexpr (kF8) {
-      if (gone) {  // zeros, as a weight of zero times whatever the pool holds there may be NaN
 #pragma unroll
-        for (int i = 0; i < kVLoads; ++i)
-          if (gone >> (kVStep * i + vrow) & 1) {
-            vreg[i] = u32x4{0u, 0u, 0u, 0u};
-            vscale[i] = 127;
-          }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kVLoads; ++i) {
-      if constexpr (kF8) {
-        const float scale = scale_of(vscale[i]);
-        *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, 2 * vpiece)) = widen8(vreg[i][0], vreg[i][1], scale);
-        *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, 2 * vpiece + 1)) =
-            widen8(vreg[i][2], vreg[i][3], scale);
-      } else {
-        *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, vpiece)) = vreg[i];
-      }
-    }
+    for (int i = 0; i < kVLoads; ++i)
+      *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, lane % TL::kSlots)) = vreg[i];
     if (next >= 0) request_v(next);
     const uint32_t va = lds_addr(my);
     constexpr int kHalf = DB < 4 ? DB : 4;  // blocks whose V is read at once
@@ -410,16 +424,15 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
 
   for (int c0 = k0; c0 < ke; c0 += kOneRows) {
     const int keys = min(ke - c0, kOneRows), ntile = (keys + kTile - 1) / kTile;
-    chunk = c0;
     if (c0 > k0) __syncthreads();  // every wave is done with the rows before
-    look_up_rows<4, kF8>(a, table, hk, base, P.r, c0, ke - 1, ntile * kTile, tid, sm.row, sm.gone);
+    look_up_rows<4, false>(a, table, hk, base, P.r, c0, ke - 1, ntile * kTile, tid, sm.row, nullptr);
     __syncthreads();
     if (wv >= ntile) continue;
     // While a tile is computed the next one's loads are under way, K's from its
     // start, V's from where its own V has left the registers.  A wave's last tile
     // is a branch of its own, so that at every use of K it is known which loads
     // are younger.
-    Keys ka, kb;
+    KeyFrag<D> ka, kb;
     request_k(wv * kTile, ka);
     request_v(wv * kTile);
     for (int tile = wv;;) {
@@ -441,35 +454,239 @@ __device__ inline void single_tokens(const PagedArgs& a, const OneItem& it, Smem
     }
   }
 
-  // The waves' partial rows meet in LDS, each in its wave's own V tile.
-  l_run = sum_over_groups(l_run);
-  float* jo = reinterpret_cast<float*>(my);
+  store_one<D>(a, it, w, acc, m_run, l_run, sm.v, sm.ml, tid, wv);
+}
+
+// 8-bit caches.  A wave takes 64 keys at a time, as many bytes under way as with 32
+// wide ones, and finds its own keys' rows, so that the waves meet at the end only.
+// Tiles without a page are passed over.  64 tokens at 1K to 32K cached, five patterns,
+// 139 MB: 47 us (32 keys at a time, rows by the workgroup: 61); with every key in one page,
+// from the L2, 28; loads and nothing else 41.  So it is the start of an item (4 us: lengths,
+// table, keys, one after the other) and the tail of the launch more than HBM.  Not
+// faster: an item a wave (46 to 60 us at 256 to 1024 keys each), one query head's products
+// on the vector ALU (45), the patterns' items mixed, twice or half the splits.
+constexpr int kOneKeys = 64;   // keys of a wave's tile
+constexpr int kOneAhead = 4;   // its tiles whose rows are looked up at once
+template <int D>
+struct SmemOne8 {
+  __attribute__((aligned(16))) char v[kPgWaves][kOneTile * D * 2];  // each wave's V tile, 32 keys at a time
+  float ml[kPgWaves][2][16];
+  u32x4 q[kPgWaves][D / 32][64];                 // Q^T operand, lane by lane
+  uint32_t row[kPgWaves][kOneAhead][kOneKeys];  // cache rows of the wave's keys
+};
+
+template <int D, bool kMixed>
+__device__ inline void single_tokens8(const PagedArgs& a, const OneItem& it, SmemOne8<D>& sm) {
+  constexpr int KC = D / 32, DB = D / 16, KU = kOneKeys / 16;
+  constexpr int kPieces = D / 16;             // 16-byte pieces of a row
+  constexpr int kHalfV = 32 * kPieces / 64;   // loads of 32 rows of V
+  constexpr int kVStep = 64 / kPieces;        // rows of a load
+  using TL = TileLayout<D>;
+  const int tid = thread_id(), lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  OneWork w;
+  if (!one_work<kMixed>(a, it, lane, w)) return;
+  const PagedPattern& P = a.pat[it.pi];
+  const int ke = w.ke, base = w.lat.first;
+  const int m = lane & 15, grp = lane >> 4;
+  const int32_t* table = a.table + static_cast<int64_t>(w.tk.b) * a.max_pages;
+  char* my = sm.v[wv];
+  u32x4(&q)[KC][64] = sm.q[wv];
+
+  f32x4 acc[DB];
 #pragma unroll
-  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(jo + join_at(m, 4 * db + grp)) = acc[db];
-  if (grp == 0) {
-    sml[wv][0][m] = m_run;
-    sml[wv][1][m] = l_run;
-  }
-  __syncthreads();
-  const int64_t row0 = static_cast<int64_t>(it.e) * a.H;
-  for (int x = tid; x < rows * (D / 4); x += kPgThreads) {
-    const int r = x / (D / 4), d = (x % (D / 4)) * 4;
-    float mt = sml[0][0][r];
+  for (int db = 0; db < DB; ++db) acc[db] = f32x4{0, 0, 0, 0};
+  float m_run = kLowest, l_run = 0.0f;
+  const float c2 = a.scale_log2;
+  Shared shared{0, 0};
+  for (int c0 = w.k0; c0 < ke; c0 += kPgWaves * kOneAhead * kOneKeys) {
+    // The rows of the wave's tiles, a key a lane; which keys have no page.
+    int pos[kOneAhead], entry[kOneAhead];
 #pragma unroll
-    for (int w = 1; w < kPgWaves; ++w) mt = fmaxf(mt, sml[w][0][r]);
-    float l = 0.0f;
-    f32x4 o = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < kPgWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sml[w][0][r] - mt);
-      l += f * sml[w][1][r];
-      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(sv[w]) + join_at(r, d / 4));
+    for (int t = 0; t < kOneAhead; ++t) {
+      pos[t] = base + min(c0 + (t * kPgWaves + wv) * kOneKeys + lane, ke - 1) * P.r;
+      entry[t] = table_entry(a, table, pos[t]);
     }
-    const int64_t at = (row0 + kh.first + (m0 + r) * P.r) * a.one_slots + P.one_slot + it.split;
-    o *= l > 0.0f ? 1.0f / l : 0.0f;
-    *reinterpret_cast<f32x4*>(a.ws + a.one_row + (at * D + d) * 4) = o;
-    if (d == 0) reinterpret_cast<float*>(a.ws + a.one_rec)[at] = mt + __builtin_amdgcn_logf(l);
+    if (c0 == w.k0) {  // meanwhile
+      const int head = w.kh.first + (w.m0 + min(m, w.rows - 1)) * P.r;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const u32x4 x = load16(static_cast<const u16*>(a.q) + w.tk.tok * a.qs + head * D + step_first<D>(c, grp));
+        q[c][lane] = m < w.rows ? x : u32x4{0u, 0u, 0u, 0u};
+      }
+      shared = shared_patterns(a, it, w, lane);
+    }
+    uint32_t left = 0, gone_lo = 0, gone_hi = 0;  // tiles with keys; lane t: tile t's keys without a page
+#pragma unroll
+    for (int t = 0; t < kOneAhead; ++t) {
+      const uint32_t row = cache_row(a, entry[t], w.hk, pos[t]);
+      const uint64_t word = __ballot(static_cast<uint32_t>(entry[t]) >= static_cast<uint32_t>(a.num_pages));
+      if (c0 + (t * kPgWaves + wv) * kOneKeys < ke && ~word != 0) left |= 1u << t;
+      // A key without a page has the row of one that is there: what it holds is the
+      // sequence's own, and a weight of zero times it is zero.
+      const uint32_t some = read_lane(row, ~word != 0 ? __builtin_ctzll(~word) : 0);
+      sm.row[wv][t][lane] = word >> lane & 1 ? some : row;
+      if (lane == t) {
+        gone_lo = static_cast<uint32_t>(word);
+        gone_hi = static_cast<uint32_t>(word >> 32);
+      }
+    }
+    if (!left) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the rows are in LDS (a wave's operations complete in order)
+    __builtin_amdgcn_wave_barrier();
+    // V^T operand: lane's d = 16 db + (lane & 15), keys 4 grp + 0..3 and 16 more.
+    const int tr_r = 4 * grp + ((lane & 15) >> 2), tr_d = (lane & 3) * 4;
+    const uint32_t voff = TL::offset(tr_r, tr_d >> 3) + (tr_d & 7) * 2;
+    const int vrow = lane / kPieces, vpiece = lane % kPieces;
+    // A tile's K leaves its registers with its scores and the next tile's K is then
+    // requested into them, V when its second half is in LDS.
+    KeyFrag8<D> kf[KU / 2];
+    u32x4 vreg[2 * kHalfV];
+    uint32_t vscale[2 * kHalfV];
+    auto request_k = [&](int t) {
+#pragma unroll
+      for (int h = 0; h < KU / 2; ++h) request_keys8<D>(a, sm.row[wv][t] + 32 * h, m, grp, kf[h]);
+    };
+    auto request_v = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < 2 * kHalfV; ++i) {
+        const uint32_t row = sm.row[wv][t][kVStep * i + vrow];
+        vreg[i] = *reinterpret_cast<const u32x4*>(a.vc + (static_cast<int64_t>(row) * D + vpiece * 16));
+        vscale[i] = a.vs[row >> a.block_log2];
+      }
+    };
+    // The wave's tile t, and if `more`, requests for its tile `next`.
+    auto compute = [&](auto more, int t, int next) {
+      constexpr bool kMore = decltype(more)::value;
+      const int first = c0 + (t * kPgWaves + wv) * kOneKeys;
+      f32x4 s[KU];
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const KeyFrag8<D>& k = kf[u >> 1];
+        s[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k.wide(u & 1, c)),
+                                                         __builtin_bit_cast(bf16x8, q[c][lane]), s[u], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // K is widened 16 keys at a time
+      }
+      __builtin_amdgcn_sched_barrier(0);  // K's registers are free from here on
+      if constexpr (kMore) request_k(next);
+      __builtin_amdgcn_sched_barrier(0);
+      // Keys past the split and those of no page.
+      const uint32_t gone[2] = {static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(gone_lo), t)),
+                                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(gone_hi), t))};
+      if (first + kOneKeys > ke || (gone[0] | gone[1])) {
+        const int left = ke - first - 4 * grp;
+#pragma unroll
+        for (int u = 0; u < KU; ++u) {
+          const uint32_t out = gone[u >> 1] >> (16 * (u & 1) + 4 * grp);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (16 * u + e >= left || (out >> e & 1)) s[u][e] = -INFINITY;
+        }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int u = 0; u < KU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[u][e]);
+      mx *= c2;
+      if (__any(mx > m_run + kSlack)) {
+        const float m_new = fmaxf(m_run, max_over_groups(mx));
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+      }
+#pragma unroll
+      for (int u = 0; u < KU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], c2, -m_run));
+      if (shared.with) {  // times the patterns that hold a key, a byte for each of four keys
+        uint32_t count[KU];
+#pragma unroll
+        for (int u = 0; u < KU; ++u) count[u] = 0x01010101u;
+        for (unsigned rest = shared.with; rest; rest &= rest - 1) {
+          const int i = __builtin_ctz(rest);
+          const PagedPattern& Q = a.pat[i];
+          const int d0 = base + first - lattice_of(Q, w.tk.pos).first;
+          const uint32_t row_keeps = shared.mine >> i & 1 ? 0x01010101u : 0u;
+          // of four keys from a multiple of r on, those that are multiples
+          const uint32_t comb = Q.r == 1 ? 0xf : Q.r == 2 ? 0x5 : Q.r == 3 ? 0x9 : 0x1;
+#pragma unroll
+          for (int u = 0; u < KU; ++u) {
+            const int x = d0 + 4 * grp + 16 * u;
+            const int over = max(x, 0) - static_cast<int>(Q.fr.div(max(x, 0))) * Q.r;
+            int ahead = over > 0 ? Q.r - over : 0;  // to the next multiple
+            if (x < 0) ahead = -x;                  // to the pattern's first key
+            const uint32_t hits = ahead < 4 ? comb << ahead & 0xf : 0u;
+            count[u] += hits * 0x00204081u & row_keeps;  // bit e to the lowest of byte e
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < KU; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[u][e] *= static_cast<float>(count[u] >> (8 * e) & 0xff);
+      }
+      bf16x8 pb[2];
+#pragma unroll
+      for (int u = 0; u < KU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          l_run += s[u][e];
+          pb[u >> 1][4 * (u & 1) + e] = (__bf16)s[u][e];  // for the product alone
+        }
+      // V through the wave's own LDS tile, 32 keys at a time, to be read transposed
+      // (LDS operations of a wave complete in order: no wait between).
+      const uint32_t va = lds_addr(my);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        __builtin_amdgcn_sched_barrier(0);  // V is widened here, not before
+#pragma unroll
+        for (int i = 0; i < kHalfV; ++i) {
+          const u32x4 x = vreg[h * kHalfV + i];
+          const float scale = scale_of(vscale[h * kHalfV + i]);
+          *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, 2 * vpiece)) = widen8(x[0], x[1], scale);
+          *reinterpret_cast<u32x4*>(my + TL::offset(kVStep * i + vrow, 2 * vpiece + 1)) = widen8(x[2], x[3], scale);
+        }
+        if constexpr (kMore) {
+          if (h == 1) request_v(next);
+        }
+        constexpr int kAtOnce = DB < 4 ? DB : 4;  // blocks whose V is read at once
+#pragma unroll
+        for (int d0 = 0; d0 < DB; d0 += kAtOnce) {
+          u32x2 vf[kAtOnce][2];
+#pragma unroll
+          for (int x = 0; x < kAtOnce; ++x) {
+            const uint32_t at = va + (voff ^ ((d0 + x) << 5));
+            vf[x][0] = lds_read_tr16<0>(at);
+            vf[x][1] = lds_read_tr16<16 * TL::kRowBytes>(at);
+          }
+          lds_wait<0>();
+#pragma unroll
+          for (int x = 0; x < kAtOnce; ++x) {
+            lds_bind(vf[x][0]);
+            lds_bind(vf[x][1]);
+            const u32x4 v4 = {vf[x][0][0], vf[x][0][1], vf[x][1][0], vf[x][1][1]};
+            acc[d0 + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v4), pb[h], acc[d0 + x], 0, 0, 0);
+          }
+        }
+      }
+    };
+    int tile = __builtin_ctz(left);
+    request_k(tile);
+    request_v(tile);
+    for (left &= left - 1; left; left &= left - 1) {
+      const int next = __builtin_ctz(left);
+      compute(std::true_type{}, tile, next);
+      tile = next;
+    }
+    compute(std::false_type{}, tile, 0);  // at every wait it is known which loads are younger
   }
+  store_one<D>(a, it, w, acc, m_run, l_run, sm.v, sm.ml, tid, wv);
 }
 
 // Four e4m3 values of a row times its scale, in float32.
@@ -815,7 +1032,14 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
       }
       const char* kl = reinterpret_cast<const char*>(&sm.k[cur][0]);
       const char* vl = reinterpret_cast<const char*>(&sm.v[cur][0]);
-      if (k0 <= wq_lo + 31 && wq_lo < qend) {  // not all keys after this wave's queries
+      uint32_t gone[2] = {0, 0};
+      if constexpr (kF8) {
+        const uint64_t word = sm.gone[jt];
+        gone[0] = uniform(static_cast<uint32_t>(word));
+        gone[1] = uniform(static_cast<uint32_t>(word >> 32));
+      }
+      // not all keys after this wave's queries, nor without a page
+      if (k0 <= wq_lo + 31 && wq_lo < qend && (gone[0] & gone[1]) != 0xffffffffu) {
         constexpr int QG = D <= 64 ? 2 : 1;
         f32x16 acc_s[2];
 #pragma unroll
@@ -846,8 +1070,6 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
               if (first + x * 32 + 8 * (j >> 2) + (j & 3) > 0) acc_s[x][j] = -INFINITY;
         }
         if constexpr (kF8) {  // keys of no page
-          const uint64_t word = sm.gone[jt];
-          const uint32_t gone[2] = {uniform(static_cast<uint32_t>(word)), uniform(static_cast<uint32_t>(word >> 32))};
           if (gone[0] | gone[1]) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -984,22 +1206,30 @@ __device__ inline bool tile_item(const PagedArgs& a, int pi, int local, int tile
   return it.tile >= 0;
 }
 
+template <int D, bool kF8>
+using SmemSingle = typename std::conditional<kF8, SmemOne8<D>, SmemOne<D>>::type;
+template <int D, bool kMixed, bool kF8>
+__device__ inline void one_tokens(const PagedArgs& a, const OneItem& it, SmemSingle<D, kF8>& sm) {
+  if constexpr (kF8) single_tokens8<D, kMixed>(a, it, sm);
+  else single_tokens<D, kMixed>(a, it, sm);
+}
+
 // Every token a single one.
 template <int D, bool kF8>
-__global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_singles(PagedArgs a) {
-  __shared__ SmemOne<D, kF8> sm;
+__global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : kF8 ? 4 : 3) void paged_singles(PagedArgs a) {
+  __shared__ SmemSingle<D, kF8> sm;
   touch(a);
   const int idx = launch_index();
   if (idx >= a.one_items) return;
   const int pi = pattern_at(a.one_begin, idx);
   OneItem it;
-  if (one_item(a, pi, idx - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, false, kF8>(a, it, sm);
+  if (one_item(a, pi, idx - a.pat[pi].one_begin, a.singles, it)) one_tokens<D, false, kF8>(a, it, sm);
 }
 
 template <int D, bool kF8>
 union SmemMixed {
   SmemTile<D, kF8> tile;
-  SmemOne<D, kF8> one;
+  SmemSingle<D, kF8> one;
   int count[DA_MAX_PATTERNS + 1];
 };
 
@@ -1018,7 +1248,7 @@ __global__ __launch_bounds__(kPgThreads, D == 128 ? 2 : 3) void paged_mixed(Page
   } else if (idx - a.tile_items < a.one_items) {
     const int pi = pattern_at(a.one_begin, idx - a.tile_items);
     OneItem it;
-    if (one_item(a, pi, idx - a.tile_items - a.pat[pi].one_begin, a.singles, it)) single_tokens<D, true, kF8>(a, it, sm.one);
+    if (one_item(a, pi, idx - a.tile_items - a.pat[pi].one_begin, a.singles, it)) one_tokens<D, true, kF8>(a, it, sm.one);
   }
 }
 
@@ -1080,7 +1310,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_mixed_steps(PagedArgs a) {
       const int pi = __builtin_ctzll(__ballot(one_end > item - tile_items));
       const int begin = tile_items + __builtin_amdgcn_readlane(one_end, pi) - __builtin_amdgcn_readlane(ones, pi);
       OneItem it;
-      if (one_item(a, pi, item - begin, tokens, it)) single_tokens<D, true, kF8>(a, it, sm.one);
+      if (one_item(a, pi, item - begin, tokens, it)) one_tokens<D, true, kF8>(a, it, sm.one);
     }
     __syncthreads();  // the item is done with its LDS
   }

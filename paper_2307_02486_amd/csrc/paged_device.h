@@ -204,15 +204,26 @@ __device__ inline u32x4 widen8(uint32_t lo, uint32_t hi, float scale) {
 __device__ inline uint32_t uniform(uint32_t x) {
   return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(x)));
 }
+// Lane l's x, the same in all lanes.
+__device__ inline uint32_t read_lane(uint32_t x, int l) {
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), l));
+}
 // A scale's byte is the exponent of the power of two that it stands for.
 __device__ inline float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // A wave's 32 keys of an 8-bit cache on their way: two blocks of 16, words of the
 // rows and the rows' scale bytes.
+// (Whole vectors: word by word, a loop that has the next tile's on their way would
+// copy them, and wait for them to.)
 template <int D>
 struct KeyFrag8 {
-  uint32_t k[2][D / 16];
+  typedef typename std::conditional<D == 32, u32x2, u32x4>::type Piece;
+  static constexpr int kPer = D == 32 ? 2 : 4;  // words of a piece
+  Piece k[2][D / 16 / kPer];
   uint32_t scale[2];
+  __device__ uint32_t word(int u, int i) const { return k[u][i / kPer][i % kPer]; }
+  // Step c of block u as bf16.
+  __device__ u32x4 wide(int u, int c) const { return widen8(word(u, 2 * c), word(u, 2 * c + 1), scale_of(scale[u])); }
 };
 // Requests the 32 keys whose cache rows are row[key .. key + 31]: block u's key m =
 // lane mod 16 in lanes m, m + 16, ..., 16 bytes of every 64 each (D = 32: 8 of 32).
@@ -224,18 +235,9 @@ __device__ inline void request_keys8(const Args& a, const uint32_t* rows, int m,
   for (int u = 0; u < 2; ++u) {
     const uint32_t row = rows[16 * u + m];
     const char* p = a.kc + (static_cast<int64_t>(row) * D + (D > 32 ? 16 : 8) * grp);
-    if constexpr (D == 32) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-      kf.k[u][0] = x[0];
-      kf.k[u][1] = x[1];
-    } else {
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(p + 64 * c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kf.k[u][4 * c + i] = x[i];
-      }
-    }
+    for (int c = 0; c < D / 16 / KeyFrag8<D>::kPer; ++c)
+      kf.k[u][c] = *reinterpret_cast<const typename KeyFrag8<D>::Piece*>(p + 64 * c);
     kf.scale[u] = a.ks[row >> a.block_log2];
   }
 }

@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kPgThreads) void weight_parts(WeightArgs a) {
 #pragma unroll
           for (int u2 = 0; u2 < 2; ++u2)
 #pragma unroll
-            for (int s = 0; s < KC; ++s) kf[u2][s] = widen8(next.k[u2][2 * s], next.k[u2][2 * s + 1], scale_of(next.scale[u2]));
+            for (int s = 0; s < KC; ++s) kf[u2][s] = next.wide(u2, s);
           if (tile + kPgWaves < ntile) request_keys8<D>(a, row + (tile + kPgWaves) * kWtTile, m, grp, next);
           const uint32_t no_page = uniform(static_cast<uint32_t>(gone[tile >> 1] >> ((tile & 1) * 32)));
           const uint32_t live = ~no_page >> (4 * grp);
