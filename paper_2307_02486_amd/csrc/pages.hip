@@ -5,13 +5,11 @@
 // row's softmax, exp(scale q.k - lse) with the row's log-sum-exp from the attention.
 // A workgroup is one unit of a pattern (a key head with the query heads that share
 // a dilation offset: their keys are the same lattice g w + rho + t r) and one split
-// of the pages that the keys lie in.  Its waves take 32-key tiles in turn, which
-// stay in registers as operands of v_mfma_f32_16x16x32_bf16 while columns of 16
-// (token, head) pairs pass by in LDS; a key's sum over them stays in LDS.  Then a
-// thread adds the keys of a page, in order, and a second launch adds the
-// partial sums of a page in the order of the units: no atomics, the same bits
-// every time.  float32 queries are three bf16 terms each, whose products with an
-// e4m3 key are exact.  All sums are float32.
+// of the pages that the keys lie in.  64 keys stay in registers as operands of
+// v_mfma_f32_16x16x32_bf16 while columns of 16 (token, head) pairs pass by.  Then the
+// keys of a page are added, and a second launch adds a page's partial sums: no
+// atomics, the same bits every time.  float32 queries are three bf16 terms each, whose
+// products with an e4m3 key are exact.  All sums are float32.
 //
 // evict_pages: a workgroup per sequence finds the weight up to which pages go by
 // counting digits of eight bits, then lists them in the order of the table.
@@ -103,196 +101,360 @@ __device__ inline void split_terms(const float* p, u32x4 (&t)[3]) {
   }
 }
 
-constexpr int kWtTile = 32;    // keys of a wave's tile
-constexpr int kWtRows = 1024;  // keys whose rows are looked up at once
+constexpr int kWtKeys = 64;  // keys of a tile
 
-template <typename T, int D, bool kLone>
-__global__ __launch_bounds__(kPgThreads) void weight_parts(WeightArgs a) {
-  constexpr int KC = D / 32, kTerms = sizeof(T) == 2 ? 1 : 3;
-  constexpr int kGroups = kTerms == 1 ? 4 : 2, kCols = 16 * kGroups;  // columns in LDS at a time
-  __shared__ u32x4 sq[kGroups][KC][kTerms][64];
-  __shared__ float slse[kCols];  // a column's lse in log2 units
-  __shared__ int slast[kCols];   // its last key, -1: none
-  __shared__ uint32_t row[kWtRows];
-  __shared__ uint64_t gone[kWtRows / 64];
-  __shared__ __attribute__((aligned(16))) float sums[kWtRows];
-  __shared__ float psum[kWeightPages];
+// What an item has to do: its row's new tokens, its unit, its share of the unit's
+// columns, its pages [p0, p1).
+struct WeightItem {
+  NewTokens c;
+  Unit un;
+  int b, row, u, share, seg0, p0, p1;
+};
+template <bool kLone>
+__device__ inline bool weight_item(const WeightArgs& a, int idx, int pi, int lane, WeightItem& it) {
+  const PagedPattern& P = a.pat[pi];
+  // Unit number n runs with all its splits on XCD n mod 8.
+  const int j = (idx - P.one_begin) >> 3, block8 = P.one_split.div(j);
+  const int split = j - block8 * P.one_split.d, n = block8 * 8 + ((idx - P.one_begin) & 7);
+  it.row = P.one_heads.div(n);
+  it.u = n - it.row * P.one_heads.d;
+  if (it.row >= a.rows) return false;
+  it.c = row_tokens<kLone>(a, it.row, lane, it.b);
+  const int u = P.tile_split.div(it.u);
+  it.share = it.u - u * P.tile_split.d;
+  if (it.c.c1 <= it.c.c0 || !unit_of<kLone>(a, P, it.c.c0, u, it.un)) return false;
+  // this split's pages, of those from the first token's segment on
+  it.seg0 = static_cast<int>(P.fw.div(it.c.c0)) * P.w;
+  const int pg0 = it.seg0 >> a.page_log2, pages = ((it.c.c1 - 1) >> a.page_log2) + 1 - pg0;
+  const int per = min(static_cast<int>(P.one_split.div(pages + P.one_split.d - 1)), static_cast<int>(kWeightPages));
+  it.p0 = pg0 + split * per;
+  it.p1 = min(it.p0 + per, pg0 + pages);
+  return it.p0 < it.p1;
+}
+// The first t at or after segment-local position x, of those rho + t r.
+__device__ inline int first_at(const PagedPattern& P, int rho, int x) {
+  return x > rho ? static_cast<int>(P.fr.div(x - rho - 1)) + 1 : 0;
+}
+
+struct SmemWeights {
+  uint32_t row[kPgWaves][kWtKeys];  // cache rows of a wave's tile
+  float sums[kPgWaves][kWtKeys];    // what its keys got
+  float psum[kWeightPages];         // what the item's pages got
+};
+// The rows of keys first .. first + 63 (positions base + t r), those past `last` as that
+// one, into a wave's LDS; returns the keys whose page is there, a bit each.
+__device__ inline uint64_t tile_rows(const WeightArgs& a, const int32_t* table, int hk, int base, int r, int first,
+                                     int last, int lane, uint32_t (&rows)[kWtKeys]) {
+  const int pos = base + min(first + lane, last) * r, entry = table_entry(a, table, pos);
+  const uint32_t row = cache_row(a, entry, hk, pos);  // in the pool, whatever the entry
+  const uint64_t live = __ballot(static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.num_pages) && first + lane <= last);
+  rows[lane] = row;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's LDS operations complete in order)
+  __builtin_amdgcn_wave_barrier();
+  return live;
+}
+// Sum over the wave's lanes, in all of them.
+__device__ inline float wave_sum(float v) {
+  v = row_sum<16>(v);
+  auto lane = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
+  return (lane(0) + lane(16)) + (lane(32) + lane(48));
+}
+// A key's sum over its 16 columns, for the 64 keys of a tile, into the wave's LDS.
+__device__ inline void put_sums(f32x4 (&sum)[4], int m, int grp, float (&out)[kWtKeys]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[u][e] = row_sum<16>(sum[u][e]);
+    if (m == 0) *reinterpret_cast<f32x4*>(&out[16 * u + 4 * grp]) = sum[u];
+  }
+}
+// A row's lse in log2 units; false where it is not finite: a row that sees nothing, or NaN.
+__device__ inline bool lse_of(const WeightArgs& a, int head, int tok, float& l) {
+  const float x = a.lse[static_cast<int64_t>(head) * a.T + tok];
+  uint32_t bits = __builtin_bit_cast(uint32_t, x);
+  asm("" : "+v"(bits));
+  l = x * kLog2e;
+  return (bits & 0x7fffffffu) < 0x7f800000u;
+}
+
+template <typename T, int D>
+struct QueryFrag {
+  static constexpr int kTerms = sizeof(T) == 2 ? 1 : 3;
+  u32x4 q[D / 32][kTerms];
+};
+template <typename T, int D>
+__device__ inline void load_queries(const WeightArgs& a, int tok, int head, int grp, bool there, QueryFrag<T, D>& f) {
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    split_terms(static_cast<const T*>(a.q) + tok * a.qs + head * D + step_first<D>(c, grp), f.q[c]);
+    if (!there)
+#pragma unroll
+      for (int i = 0; i < QueryFrag<T, D>::kTerms; ++i) f.q[c][i] = u32x4{0u, 0u, 0u, 0u};
+  }
+}
+// Scores of 64 keys by 16 columns.
+template <typename T, int D>
+__device__ inline void scores(const u32x4 (&k)[4][D / 32], const QueryFrag<T, D>& f, f32x4 (&s)[4]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) s[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = QueryFrag<T, D>::kTerms - 1; i >= 0; --i)
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[u][c]),
+                                                       __builtin_bit_cast(bf16x8, f.q[c][i]), s[u], 0, 0, 0);
+}
+
+// What the keys first .. first + 63 of a tile got, v (0 past `last`), a lane each, to their
+// pages' sums.  Keys of a page are neighbours: a sum over each run of them, and its
+// last lane adds it.
+__device__ inline void add_pages(const WeightArgs& a, const PagedPattern& P, int base, int first, int last, int lane, float v,
+                                 float* psum) {
+  const int pg = (base + min(first + lane, last) * P.r) >> a.page_log2;
+  const int before = __shfl_up(pg, 1);
+  const uint64_t starts = __ballot(lane == 0 || before != pg);
+  if (starts == 1) {
+    v = wave_sum(v);
+  } else {
+    const int behind = lane - (63 - __builtin_clzll(starts & (~uint64_t{0} >> (63 - lane))));
+    const int most = min(64, ((1 << a.page_log2) - 1) / P.r + 1);
+    for (int step = 1; step < most; step <<= 1) {
+      const float w = __shfl_up(v, step);
+      v += behind >= step ? w : 0.0f;
+    }
+  }
+  const int end = min(63, last - first);
+  if (lane == end || (lane < end && (starts >> (lane + 1) & 1))) psum[pg] += v;
+}
+
+// Rows that are tokens: a wave has a share of the item's pages and meets no other.
+template <typename T, int D>
+__global__ __launch_bounds__(kPgThreads) void weight_tokens(WeightArgs a) {
+  constexpr int KC = D / 32;
+  __shared__ __attribute__((aligned(16))) SmemWeights sm;
   const int tid = thread_id(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int idx = launch_index();
   if (idx >= a.items) return;
   const int pi = pattern_at(a.begin, idx);
   const PagedPattern& P = a.pat[pi];
-  // Unit number n runs with all its splits on XCD n mod 8.
-  const int j = (idx - P.one_begin) >> 3, block8 = P.one_split.div(j);
-  const int split = j - block8 * P.one_split.d, n = block8 * 8 + ((idx - P.one_begin) & 7);
-  const int r0 = P.one_heads.div(n), u = n - r0 * P.one_heads.d;
-  if (r0 >= a.rows) return;
-  int b;
-  const NewTokens c = row_tokens<kLone>(a, r0, lane, b);
-  Unit un;
-  if (c.c1 <= c.c0 || !unit_of<kLone>(a, P, c.c0, u, un)) return;
-  const int rho = un.rho, nh = un.heads.count;
-  // this split's pages, of those from the first token's segment on
-  const int seg0 = static_cast<int>(P.fw.div(c.c0)) * P.w;
-  const int pg0 = seg0 >> a.page_log2, pages = ((c.c1 - 1) >> a.page_log2) + 1 - pg0;
-  const int per = P.one_split.div(pages + P.one_split.d - 1);
-  const int p0 = pg0 + split * per, p1 = min(p0 + min(per, static_cast<int>(kWeightPages)), pg0 + pages);
+  WeightItem it;
+  if (!weight_item<true>(a, idx, pi, lane, it)) return;
+  const int rho = it.un.rho, nh = it.un.heads.count, pos = it.c.c0, tok = it.c.tok0 + pos;
+  const int per = (it.p1 - it.p0 + kPgWaves - 1) / kPgWaves;
+  const int p0 = it.p0 + wv * per, p1 = min(p0 + per, it.p1);
   if (p0 >= p1) return;
-  for (int i = tid; i < p1 - p0; i += kPgThreads) psum[i] = 0.0f;
+  for (int i = p0 + lane; i < p1; i += 64) sm.psum[i - it.p0] = 0.0f;
+
+  const int m = lane & 15, grp = lane >> 4, base = it.seg0 + rho;
+  const int32_t* table = a.table + static_cast<int64_t>(it.b) * a.max_pages;
+  const float c2 = a.scale_log2;
+  const int64_t end = static_cast<int64_t>(p1) << a.page_log2;
+  const int t0 = first_at(P, rho, max((p0 << a.page_log2) - it.seg0, 0));
+  const int t1 = first_at(P, rho, static_cast<int>(min(end, static_cast<int64_t>(pos) + 1)) - it.seg0);
+  for (int h0 = 0; h0 < nh; h0 += 16) {
+    QueryFrag<T, D> f;
+    const bool there = h0 + m < nh;
+    const int head = it.un.heads.first + (there ? h0 + m : 0) * P.r;
+    load_queries<T, D>(a, tok, head, grp, there, f);
+    float l;
+    const bool counts = lse_of(a, head, tok, l) && there;
+    // The next tile's keys are under way while one is computed.
+    KeyFrag8<D> next[2];
+    uint64_t live = 0;
+    auto request = [&](int first) {
+      live = tile_rows(a, table, it.un.hk, base, P.r, first, t1 - 1, lane, sm.row[wv]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) request_keys8<D>(a, sm.row[wv] + 32 * h, m, grp, next[h]);
+    };
+    if (t0 < t1) request(t0);
+    for (int first = t0; first < t1; first += kWtKeys) {
+      u32x4 k[4][KC];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int s = 0; s < KC; ++s) k[u][s] = next[u >> 1].wide(u & 1, s);
+      const uint64_t now = live;
+      if (first + kWtKeys < t1) request(first + kWtKeys);
+      if (!now) continue;
+      f32x4 s[4];
+      scores<T, D>(k, f, s);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t mine = static_cast<uint32_t>(now >> (16 * u + 4 * grp));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], c2, -l));
+          s[u][e] = counts && (mine >> e & 1) ? p : 0.0f;
+        }
+      }
+      put_sums(s, m, grp, sm.sums[wv]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      add_pages(a, P, base, first, min(first + kWtKeys, t1) - 1, lane, sm.sums[wv][lane], sm.psum - it.p0);
+    }
+  }
+  float* part = a.part + (static_cast<int64_t>(P.one_slot + it.u) * a.rows + it.row) * a.max_pages;
+  for (int i = p0 + lane; i < p1; i += 64) part[i] = sm.psum[i - it.p0];
+}
+
+// Rows that are sequences: the waves share a tile's keys and take 16 columns in turn (a
+// long chunk has hundreds of them).
+template <typename T, int D>
+__global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
+  constexpr int KC = D / 32;
+  __shared__ __attribute__((aligned(16))) SmemWeights sm;
+  const int tid = thread_id(), lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int idx = launch_index();
+  if (idx >= a.items) return;
+  const int pi = pattern_at(a.begin, idx);
+  const PagedPattern& P = a.pat[pi];
+  WeightItem it;
+  if (!weight_item<false>(a, idx, pi, lane, it)) return;
+  const NewTokens c = it.c;
+  const int rho = it.un.rho, nh = it.un.heads.count;
+  for (int i = tid; i < it.p1 - it.p0; i += kPgThreads) sm.psum[i] = 0.0f;
 
   const int m = lane & 15, grp = lane >> 4;
-  const int32_t* table = a.table + static_cast<int64_t>(b) * a.max_pages;
+  const int32_t* table = a.table + static_cast<int64_t>(it.b) * a.max_pages;
   const float c2 = a.scale_log2;
-  const int x0 = max(p0 << a.page_log2, seg0);
-  const int x1 = static_cast<int>(min(static_cast<int64_t>(p1) << a.page_log2, static_cast<int64_t>(c.c1)));
+  const int x0 = max(it.p0 << a.page_log2, it.seg0);
+  const int x1 = static_cast<int>(min(static_cast<int64_t>(it.p1) << a.page_log2, static_cast<int64_t>(c.c1)));
   for (int g = P.fw.div(x0); g <= static_cast<int>(P.fw.div(x1 - 1)); ++g) {
-    const int gs = g * P.w;
-    auto first_at = [&](int x) { return x > rho ? static_cast<int>(P.fr.div(x - rho - 1)) + 1 : 0; };
-    const int t0 = first_at(x0 - gs), t1 = first_at(min(x1 - gs, P.w));  // keys
-    const int q0 = max(first_at(c.c0 - gs), t0), q1 = first_at(min(c.c1 - gs, P.w));  // queries that see some
-    if (t0 >= t1 || q0 >= q1) continue;
-    for (int k0 = t0; k0 < t1; k0 += kWtRows) {
-      const int ke = min(t1, k0 + kWtRows), ntile = (ke - k0 + kWtTile - 1) / kWtTile;
-      const int qa = max(q0, k0), cols = (q1 - qa) * nh;  // the chunk's columns, token by token
-      if (cols <= 0) break;
-      __syncthreads();  // the chunk before is done with LDS
-      look_up_rows<4, true>(a, table, un.hk, gs + rho, P.r, k0, ke - 1, ntile * kWtTile, tid, row, gone);
-      for (int i = tid; i < ntile * kWtTile; i += kPgThreads) sums[i] = 0.0f;
-      for (int col0 = 0; col0 < cols; col0 += kCols) {
-        if (col0 > 0) __syncthreads();  // the columns before are done with
-        for (int x = wv; x < kGroups * KC; x += kPgWaves) {
-          const int gq = x / KC, step = x - gq * KC, col = col0 + 16 * gq + m;
-          u32x4 t[kTerms];
+    const int gs = g * P.w, base = gs + rho;
+    const int t0 = first_at(P, rho, x0 - gs), t1 = first_at(P, rho, min(x1 - gs, P.w));  // keys
+    const int q0 = max(first_at(P, rho, c.c0 - gs), t0), q1 = first_at(P, rho, min(c.c1 - gs, P.w));  // queries that see some
+    if (q0 >= q1) continue;
+    for (int k0 = t0; k0 < t1 && k0 < q1; k0 += kWtKeys) {
+      // Columns: tokens qa .. q1 - 1 of the nh heads, head by head (in blocks of 16
+      // tokens if there are that many, so that a block's last key is near its first);
+      // this item's share of them.
+      const int qa = max(q0, k0), ntok = q1 - qa, per = ntok < 16 ? ntok : (ntok + 15) & ~15, cols = per * nh;
+      const int share = (static_cast<int>(P.tile_split.div(((cols + 15) >> 4) + P.tile_split.d - 1))) << 4;
+      const int cend = min(cols, (it.share + 1) * share), cbegin = it.share * share + 16 * wv;
+      f32x4 sum[4];
 #pragma unroll
-          for (int i = 0; i < kTerms; ++i) t[i] = u32x4{0u, 0u, 0u, 0u};
-          if (col < cols) {
-            const int token = col / nh, pos = gs + rho + (qa + token) * P.r;
-            const int head = un.heads.first + (col - token * nh) * P.r;
-            split_terms(static_cast<const T*>(a.q) + (c.tok0 + pos) * a.qs + head * D + step_first<D>(step, grp), t);
-          }
+      for (int u = 0; u < 4; ++u) sum[u] = f32x4{0, 0, 0, 0};
+      uint64_t live = 0;
+      if (cbegin < cend) live = tile_rows(a, table, it.un.hk, base, P.r, k0, t1 - 1, lane, sm.row[wv]);
+      if (live) {
+        KeyFrag8<D> kf[2];
 #pragma unroll
-          for (int i = 0; i < kTerms; ++i) sq[gq][step][i][lane] = t[i];
-        }
-        if (tid < kCols) {
-          const int col = col0 + tid;
-          float x = 0.0f;
-          int last = -1;
-          if (col < cols) {
-            const int token = col / nh, head = un.heads.first + (col - token * nh) * P.r;
-            last = qa + token;
-            x = a.lse[static_cast<int64_t>(head) * a.T + c.tok0 + gs + rho + last * P.r];
-            uint32_t bits = __builtin_bit_cast(uint32_t, x);
-            asm("" : "+v"(bits));
-            if ((bits & 0x7fffffffu) >= 0x7f800000u) last = -1;  // a row that sees nothing, or NaN: adds nothing
-          }
-          slse[tid] = x * kLog2e;
-          slast[tid] = last;
-        }
-        __syncthreads();
-        const int groups = min(kGroups, (cols - col0 + 15) >> 4);
-        const int tmax = qa + (min(cols, col0 + kCols) - 1) / nh;  // the last key that a column here sees
-        KeyFrag8<D> next;
-        if (wv < ntile) request_keys8<D>(a, row + wv * kWtTile, m, grp, next);
-        for (int tile = wv; tile < ntile; tile += kPgWaves) {
-          const int first = k0 + tile * kWtTile;
-          if (first > tmax) break;
-          u32x4 kf[2][KC];
+        for (int h = 0; h < 2; ++h) request_keys8<D>(a, sm.row[wv] + 32 * h, m, grp, kf[h]);
+        struct Column {
+          int last;  // its last key, -1: none
+          float l;
+        };
+        auto column = [&](int col, QueryFrag<T, D>& f, Column& x) {
+          const int h = col / per, t = col - h * per;
+          const bool there = col < cols && t < ntok;
+          const int token = there ? qa + t : qa, head = it.un.heads.first + (there ? h : 0) * P.r;
+          const int tok = c.tok0 + base + token * P.r;
+          load_queries<T, D>(a, tok, head, grp, there, f);
+          x.last = lse_of(a, head, tok, x.l) && there ? token : -1;
+        };
+        constexpr int kStep = 16 * kPgWaves;
+        QueryFrag<T, D> f;
+        Column x;
+        column(cbegin + m, f, x);
+        u32x4 k[4][KC];
 #pragma unroll
-          for (int u2 = 0; u2 < 2; ++u2)
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int s = 0; s < KC; ++s) kf[u2][s] = next.wide(u2, s);
-          if (tile + kPgWaves < ntile) request_keys8<D>(a, row + (tile + kPgWaves) * kWtTile, m, grp, next);
-          const uint32_t no_page = uniform(static_cast<uint32_t>(gone[tile >> 1] >> ((tile & 1) * 32)));
-          const uint32_t live = ~no_page >> (4 * grp);
-          f32x4 sum[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
-          for (int gq = 0; gq < groups; ++gq) {
-            f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+          for (int s = 0; s < KC; ++s) k[u][s] = kf[u >> 1].wide(u & 1, s);
+        const bool some = ~live != 0;
+        for (int b0 = cbegin; b0 < cend; b0 += kStep) {
+          const QueryFrag<T, D> now = f;
+          const Column at = x;
+          if (b0 + kStep < cend) column(b0 + kStep + m, f, x);  // the next one's on their way
+          f32x4 s[4];
+          scores<T, D>(k, now, s);
+          const int left = at.last - k0 - 4 * grp;  // the last key that counts, from the lane's first
+          if (some || !__all(left >= kWtKeys)) {
 #pragma unroll
-            for (int i = kTerms - 1; i >= 0; --i)
+            for (int u = 0; u < 4; ++u) {
+              const uint32_t mine = static_cast<uint32_t>(live >> (16 * u + 4 * grp));
 #pragma unroll
-              for (int x = 0; x < KC; ++x)
-#pragma unroll
-                for (int u2 = 0; u2 < 2; ++u2)
-                  s[u2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[u2][x]),
-                                                                  __builtin_bit_cast(bf16x8, sq[gq][x][i][lane]), s[u2], 0, 0, 0);
-            const float neg = -slse[16 * gq + m];
-            const int left = min(slast[16 * gq + m], ke - 1) - first - 4 * grp;  // the last key that counts, from the lane's first
-#pragma unroll
-            for (int u2 = 0; u2 < 2; ++u2)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u2][e], c2, neg));
-                sum[u2][e] += 16 * u2 + e <= left && (live >> (16 * u2 + e) & 1) ? p : 0.0f;
-              }
-          }
-#pragma unroll
-          for (int u2 = 0; u2 < 2; ++u2) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[u2][e] = row_sum<16>(sum[u2][e]);
-            if (m == 0) {
-              f32x4* at = reinterpret_cast<f32x4*>(&sums[tile * kWtTile + 16 * u2 + 4 * grp]);
-              *at += sum[u2];
+              for (int e = 0; e < 4; ++e)
+                if (16 * u + e > left || !(mine >> e & 1)) s[u][e] = -INFINITY;
             }
           }
+          const float l = at.last < 0 ? 0.0f : at.l;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[u][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], c2, -l));
         }
       }
+      put_sums(sum, m, grp, sm.sums[wv]);
       __syncthreads();
-      // the chunk's pages, a thread each
-      const int pa = (gs + rho + k0 * P.r) >> a.page_log2, pe = (gs + rho + (ke - 1) * P.r) >> a.page_log2;
-      for (int pg = pa + tid; pg <= pe; pg += kPgThreads) {
-        const int from = max(first_at((pg << a.page_log2) - gs), k0);
-        const int to = min(first_at(static_cast<int>(min((static_cast<int64_t>(pg) + 1) << a.page_log2, int64_t{0x7fffffff})) - gs), ke);
-        float s = 0.0f;
-        for (int t = from; t < to; ++t) s += sums[t - k0];
-        psum[pg - p0] += s;
-      }
+      if (wv == 0)
+        add_pages(a, P, base, k0, min(k0 + kWtKeys, t1) - 1, lane,
+                  (sm.sums[0][lane] + sm.sums[1][lane]) + (sm.sums[2][lane] + sm.sums[3][lane]), sm.psum - it.p0);
+      __syncthreads();
     }
   }
   __syncthreads();
-  float* part = a.part + (static_cast<int64_t>(P.one_slot + u) * a.rows + r0) * a.max_pages;
-  for (int i = tid; i < p1 - p0; i += kPgThreads) part[p0 + i] = psum[i];
+  float* part = a.part + (static_cast<int64_t>(P.one_slot + it.u) * a.rows + it.row) * a.max_pages;
+  for (int i = tid; i < it.p1 - it.p0; i += kPgThreads) part[it.p0 + i] = sm.psum[i];
 }
 
-// The partial sums of a page into its weight, a thread a page of a sequence.
+// The partial sums of a page into its weight: a lane a page, the waves share the
+// units (u, u + 4, ...) and meet in LDS, all in a fixed order.
 template <bool kLone>
 __global__ __launch_bounds__(kPgThreads) void weight_join(WeightArgs a) {
-  const int per = (a.max_pages + kPgThreads - 1) / kPgThreads;
+  __shared__ float sums[kPgWaves][64];
+  const int per = (a.max_pages + 63) >> 6;
   const int idx = launch_index(), b = idx / per;
-  const int pg = (idx - b * per) * kPgThreads + static_cast<int>(__builtin_amdgcn_workitem_id_x());
-  if (b >= a.B || pg >= a.max_pages) return;
+  const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int pg = (idx - b * per) * 64 + lane;
+  if (b >= a.B) return;
   const NewTokens c = new_tokens(a, b);
-  if (c.c1 <= c.c0 || pg > (c.c1 - 1) >> a.page_log2) return;
-  const int entry = a.table[static_cast<int64_t>(b) * a.max_pages + pg];
-  if (static_cast<uint32_t>(entry) >= static_cast<uint32_t>(a.num_pages)) return;
+  if (c.c1 <= c.c0 || pg - lane > (c.c1 - 1) >> a.page_log2) return;
+  const int at = min(pg, a.max_pages - 1), entry = a.table[static_cast<int64_t>(b) * a.max_pages + at];
   float s = 0.0f;
   const int rows = kLone ? c.c1 - c.c0 : 1;
+  const int64_t step = static_cast<int64_t>(a.rows) * a.max_pages;
   for (int i = 0; i < rows; ++i) {
     const int c0 = c.c0 + i, last = kLone ? c0 : c.c1 - 1;
-    const int64_t r0 = kLone ? c.tok0 + c0 : b;
+    const int64_t row = kLone ? c.tok0 + c0 : b;
     for (int pi = 0; pi < a.npat; ++pi) {
       const PagedPattern& P = a.pat[pi];
-      if (pg < (static_cast<int>(P.fw.div(c0)) * P.w) >> a.page_log2 || pg > last >> a.page_log2) continue;
-      const float* part = a.part + (static_cast<int64_t>(P.one_slot) * a.rows + r0) * a.max_pages + pg;
-      const int units = P.one_heads.d;
-      for (int u = 0; u < units; ++u) {
-        Unit un;
-        if (unit_of<kLone>(a, P, c0, u, un)) s += part[static_cast<int64_t>(u) * a.rows * a.max_pages];
+      const int from = (static_cast<int>(P.fw.div(c0)) * P.w) >> a.page_log2, to = last >> a.page_log2;
+      if (pg - lane > to || pg - lane + 63 < from) continue;
+      const bool in = pg >= from && pg <= to;
+      const float* part = a.part + P.one_slot * step + row * a.max_pages + min(max(pg, from), to);
+      int units = P.one_heads.d;  // those that the row has
+      if constexpr (kLone) {
+        const int rho = lattice_of(P, c0).rho;
+        if (P.r >= a.G) units = min(units, rho < a.H ? static_cast<int>(P.fr.div(a.H - 1 - rho)) + 1 : 0);
       }
+      float v = 0.0f;
+#pragma unroll 4
+      for (int u = wv; u < units; u += kPgWaves) v += part[u * step];
+      s += in ? v : 0.0f;
     }
   }
-  a.weights[entry] += s;
+  sums[wv][lane] = s;
+  __syncthreads();
+  if (wv != 0 || pg > (c.c1 - 1) >> a.page_log2) return;
+  if (static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.num_pages))
+    a.weights[entry] += (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
 }
 
 template <typename T, int D>
 void launch_weights_d(const WeightPlan& p, const WeightArgs& a, hipStream_t stream) {
   const dim3 threads(kPgThreads), grid = grid_of(p.items);
-  const dim3 join = grid_of(p.B * ((p.max_pages + kPgThreads - 1) / kPgThreads));
+  const dim3 join = grid_of(p.B * ((p.max_pages + 63) / 64));
   if (p.lone) {
-    hipLaunchKernelGGL((weight_parts<T, D, true>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((weight_tokens<T, D>), grid, threads, 0, stream, a);
     hipLaunchKernelGGL(weight_join<true>, join, threads, 0, stream, a);
   } else {
-    hipLaunchKernelGGL((weight_parts<T, D, false>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((weight_sequences<T, D>), grid, threads, 0, stream, a);
     hipLaunchKernelGGL(weight_join<false>, join, threads, 0, stream, a);
   }
 }

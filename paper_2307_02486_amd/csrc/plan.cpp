@@ -349,19 +349,28 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
     if (!p.lone) return Hkv * std::min(G, r);
     return r >= G ? std::min(Hkv, (H + r - 1) / r) : Hkv;
   };
+  // A sequence's columns are dealt out until a wave has about eight times sixteen.
+  auto shares = [&](int64_t r) {
+    const int64_t cols = T / r * ((G + std::min(G, r) - 1) / std::min(G, r));
+    return p.lone ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, cols / 512));
+  };
   double busy = 0.0;
-  for (int i = 0; i < p.npat; ++i) busy += static_cast<double>(p.rows) * units(base.pat[i].r);
+  for (int i = 0; i < p.npat; ++i)
+    busy += static_cast<double>(p.rows) * units(base.pat[i].r) * shares(base.pat[i].r);
   for (int i = 0; i < p.npat; ++i) {
     PagedPattern& t = p.pat[i];
     t = base.pat[i];
-    const int64_t n = units(t.r);
+    t.tile_split = make_fastdiv(static_cast<uint32_t>(shares(t.r)));
+    const int64_t n = units(t.r) * shares(t.r);
     // the positions that a row's keys can lie in, and their pages
     const int64_t span = std::min(reach, p.lone ? int64_t{t.w} : t.w + T);
     const int64_t pages = std::min(max_pages, span / page + 2);
     const int64_t keys = (span + t.r - 1) / t.r;
     const int64_t least = (pages + kWeightPages - 1) / kWeightPages;
-    const int64_t splits = std::max(
-        least, std::max<int64_t>(1, std::min({static_cast<int64_t>(2048.0 / std::max(1.0, busy) + 0.5), (keys + 255) / 256, pages})));
+    // A round of keys an item: 256 of a token, 64 of a sequence.
+    const int64_t round = p.lone ? 256 : 64;
+    const int64_t some = static_cast<int64_t>((p.lone ? 2048.0 : 4096.0) / std::max(1.0, busy) + 0.5);
+    const int64_t splits = std::max({least, int64_t{1}, std::min({some, (keys + round - 1) / round, pages})});
     if (splits >= kMost || p.rows * n >= kMost - 8) return DA_EINVAL;
     t.one_split = make_fastdiv(static_cast<uint32_t>(splits));
     t.one_heads = make_fastdiv(static_cast<uint32_t>(n));

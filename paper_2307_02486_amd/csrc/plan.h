@@ -160,8 +160,10 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
 // unit of a pattern (a key head with those of its query heads that share a dilation
 // offset; of a single token those of its own offset) and one split of the pages that
 // its keys lie in; it writes a partial sum for each of its pages, and a second launch
-// adds a page's.  In a PagedPattern: one_split are the splits, one_heads the units,
-// one_slot the first unit's number among all, one_begin the first item.
+// adds a page's.  A sequence's tokens and heads of a unit are dealt out to several
+// units where they are many.  In a PagedPattern: one_split are the splits, one_heads
+// the units, tile_split how many of them share a key head and offset, one_slot the
+// first unit's number among all, one_begin the first item.
 constexpr int64_t kWeightPages = 1024;  // pages of an item at most
 struct WeightPlan {
   int64_t T, B, H, Hkv, D, num_pages, page, max_pages;
