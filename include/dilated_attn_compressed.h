@@ -77,8 +77,8 @@ int dilated_attn_paged_fwd_f8(const void* q, const da_paged_cache_f8_t* cache, v
  * lse         device pointer, [H, T] float32: that call's.  Rows whose lse is not
  *             finite add nothing.
  * cache       the keys (pages.v and v_scale are not looked at and may be NULL).
- * weights     device pointer, [num_pages] float32, updated.  A page belongs to one
- *             sequence of the call.
+ * weights     device pointer, [num_pages] float32, updated.  The tables name a page
+ *             once: of one that they name twice either sum may be lost.
  * workspace   device scratch of at least the bytes that
  *             dilated_attn_page_weights_workspace reports for the same sizes.
  *

@@ -946,8 +946,7 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
   constexpr int kPieces = D > 32 ? D / 64 : 1;  // 16-byte loads (D = 32: of 8 bytes) of a thread's quarter
   const int brow = tid >> 2, bpart = tid & 3;
   uint32_t kbytes[kPieces * 4], vbytes[kPieces * 4], kscale = 0, vscale = 0;
-  auto request_tile = [&](int jt) {
-    const uint32_t row = sm.row[jt * BN + brow];
+  auto request_tile = [&](uint32_t row) {
     const char* kp = a.kc + (static_cast<int64_t>(row) * D + (D > 32 ? 16 : 8) * bpart);
     const char* vp = a.vc + (static_cast<int64_t>(row) * D + (D > 32 ? 16 : 8) * bpart);
     if constexpr (D == 32) {
@@ -964,8 +963,8 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
     kscale = a.ks[row >> a.block_log2];
     vscale = a.vs[row >> a.block_log2];
   };
-  auto store_tile = [&](int jt, int buf) {
-    if (sm.gone[jt] >> brow & 1) {  // zeros, as a weight of zero times whatever the pool holds there may be NaN
+  auto store_tile = [&](const uint32_t (&gone)[2], int buf) {
+    if ((brow < 32 ? gone[0] : gone[1]) >> (brow & 31) & 1) {  // zeros, as a weight of zero times whatever the pool holds there may be NaN
 #pragma unroll
       for (int i = 0; i < kPieces * 4; ++i) vbytes[i] = 0;
       vscale = 127;
@@ -1016,9 +1015,19 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
     const int ntile = (min(ke - c0, kTileRows<kF8>) + BN - 1) / BN;
     look_up_rows<8, kF8>(a, table, hk, base, P.r, c0, ke - 1, ntile * BN, tid, sm.row, sm.gone);
     __syncthreads();
+    // 8 bits, read a tile ahead: the thread's row, and the keys without a page.
+    uint32_t row_next = 0, gone[2] = {0, 0};
+    uint64_t gone_next = 0;
+    auto keep_gone = [&] {
+      gone[0] = uniform(static_cast<uint32_t>(gone_next));
+      gone[1] = uniform(static_cast<uint32_t>(gone_next >> 32));
+    };
     if constexpr (kF8) {
-      request_tile(0);
-      store_tile(0, 0);
+      request_tile(sm.row[brow]);
+      gone_next = sm.gone[0];
+      row_next = sm.row[(ntile > 1 ? BN : 0) + brow];
+      keep_gone();
+      store_tile(gone, 0);
     } else {
       load_tile(0, 0);
       wait_loads<0>();
@@ -1027,17 +1036,16 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
     for (int jt = 0; jt < ntile; ++jt) {
       const int cur = jt & 1, k0 = c0 + jt * BN;
       if (jt + 1 < ntile) {
-        if constexpr (kF8) request_tile(jt + 1);
-        else load_tile(jt + 1, cur ^ 1);
+        if constexpr (kF8) {
+          request_tile(row_next);
+          gone_next = sm.gone[jt + 1];
+          row_next = sm.row[min(jt + 2, ntile - 1) * BN + brow];
+        } else {
+          load_tile(jt + 1, cur ^ 1);
+        }
       }
       const char* kl = reinterpret_cast<const char*>(&sm.k[cur][0]);
       const char* vl = reinterpret_cast<const char*>(&sm.v[cur][0]);
-      uint32_t gone[2] = {0, 0};
-      if constexpr (kF8) {
-        const uint64_t word = sm.gone[jt];
-        gone[0] = uniform(static_cast<uint32_t>(word));
-        gone[1] = uniform(static_cast<uint32_t>(word >> 32));
-      }
       // not all keys after this wave's queries, nor without a page
       if (k0 <= wq_lo + 31 && wq_lo < qend && (gone[0] & gone[1]) != 0xffffffffu) {
         constexpr int QG = D <= 64 ? 2 : 1;
@@ -1147,7 +1155,8 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
         });
       }
       if constexpr (kF8) {
-        if (jt + 1 < ntile) store_tile(jt + 1, cur ^ 1);
+        keep_gone();
+        if (jt + 1 < ntile) store_tile(gone, cur ^ 1);
       } else {
         wait_loads<0>();
       }

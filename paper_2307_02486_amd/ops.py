@@ -90,6 +90,15 @@ def _raw_stream(device: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _call_on(dev: int, function, *args) -> int:
+    """function(*args) with `dev` as the current device, whose null stream is meant
+    where the stream is 0."""
+    if torch._C._cuda_getDevice() == dev:
+        return function(*args)
+    with torch.cuda.device(dev):
+        return function(*args)
+
+
 def plan(B: int, N: int, H: int, D: int, patterns: Sequence[Tuple[int, int]], causal: bool = True,
          dtype=torch.bfloat16, scale: float | None = None) -> dict:
     """Validate a problem and return its workspace size and work counts (host only)."""
@@ -635,8 +644,8 @@ def cache_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cac
         cache, append = _lib.PagedCacheF8Args(cache, k_scale.data_ptr(), v_scale.data_ptr()), \
             lib.dilated_attn_cache_append_f8
     raw = _raw_stream(k.device) if stream is None else stream.cuda_stream
-    rc = append(
-        None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    rc = _call_on(
+        dev, append, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
         None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
         None if qo is None else qo.data_ptr(), cache, T, B, H, Hkv, D, qs, ks, vs, float(eps),
         1 if rotate else 0, int(center), float(base), float(gamma), float(scale_base), dcode, raw)
@@ -732,8 +741,8 @@ def paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, bl
         cache, attend = _lib.PagedCacheF8Args(cache, k_scale.data_ptr(), v_scale.data_ptr()), \
             lib.dilated_attn_paged_fwd_f8
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
-    rc = attend(q.data_ptr(), cache, out.data_ptr(), lse.data_ptr(), T, B, H, Hkv, D, qs, new, arr, n, dcode,
-                float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
+    rc = _call_on(dev, attend, q.data_ptr(), cache, out.data_ptr(), lse.data_ptr(), T, B, H, Hkv, D, qs, new, arr, n,
+                  dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, owned)
@@ -771,8 +780,7 @@ def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_sc
 
     q, the cache and the sequences' arrays are those of paged_attn, lse [H, T]
     what it returned; a row without a finite lse adds nothing.  Each head of a
-    token that sees a key adds one in all.  A page belongs to one sequence of the
-    call.  Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor
+    token that sees a key adds one in all.  The tables name a page once.  Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor
     of at least page_weights_workspace_bytes."""
     lib = _lib.load()
     patterns = tuple(patterns)
@@ -813,8 +821,8 @@ def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_sc
     cache = _lib.PagedCacheF8Args(_cache_args(k_cache, k_cache, block_table, seq_lens, q_start, pages, page, max_pages),
                                   k_scale.data_ptr(), None)
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
-    rc = lib.dilated_attn_page_weights(q.data_ptr(), lse.data_ptr(), cache, weights.data_ptr(), T, B, H, Hkv, D, qs, arr,
-                                       n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
+    rc = _call_on(dev, lib.dilated_attn_page_weights, q.data_ptr(), lse.data_ptr(), cache, weights.data_ptr(), T, B, H,
+                  Hkv, D, qs, arr, n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, owned)
@@ -852,9 +860,10 @@ def evict_pages(weights: torch.Tensor, block_table: torch.Tensor, seq_lens: torc
     table, freed = torch.empty_like(block_table), torch.empty_like(block_table)
     count = torch.empty_like(seq_lens)
     raw = _raw_stream(weights.device) if stream is None else stream.cuda_stream
-    rc = lib.dilated_attn_evict_pages(weights.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), table.data_ptr(),
-                                      freed.data_ptr(), count.data_ptr(), B, weights.numel(), int(page_size), max_pages,
-                                      int(keep), int(first), int(last), raw)
+    keep, first, last = (min(int(n), 2 ** 31 - 1) for n in (keep, first, last))  # more than a table has
+    rc = _call_on(dev, lib.dilated_attn_evict_pages, weights.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                  table.data_ptr(), freed.data_ptr(), count.data_ptr(), B, weights.numel(), int(page_size), max_pages,
+                  keep, first, last, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, [table, freed, count])

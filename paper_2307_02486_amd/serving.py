@@ -114,7 +114,8 @@ class PagedCache:
     def retract(self, batch: Batch):
         """Take back the extend that gave this batch: its sequences have their
         earlier lengths again, and pages taken for it go back to the pool.  Only
-        while no other extend of one of them, nor a release, came since."""
+        while no other extend of one of them, nor a release or an evict, came since.
+        What its layers added to the weights of other pages stays."""
         if not batch.sequences or any(self._last.get(s) != batch.number for s in batch.sequences):
             raise ValueError("not the last batch of all its sequences")
         for s, n in zip(batch.sequences, batch.new):
@@ -128,12 +129,13 @@ class PagedCache:
     def evict(self, keep: int, sequences: Sequence | None = None, first: int = 1, last: int = 1) -> int:
         """Give up the pages of least weight of each of these sequences (default:
         all), until it has `keep`; never its first `first` pages nor its last `last`
-        (see evict_pages).  They go back to the pool.  Only between steps: a batch
-        made before names them still.  Waits for the GPU.  Returns how many went."""
+        (see evict_pages), of which the last takes the next tokens.  They go back to
+        the pool.  Only between steps: a batch made before names them still.  Waits
+        for the GPU.  Returns how many went."""
         if self.weights is None:
             raise ValueError("evict needs a cache that counts its pages' weights (weigh=True)")
-        if keep < 0 or first < 0 or last < 0:
-            raise ValueError("keep, first and last must not be negative")
+        if keep < 0 or first < 0 or last < 1:
+            raise ValueError("keep and first must not be negative, and last at least 1")
         names = list(self._pages if sequences is None else sequences)
         if len(set(names)) != len(names) or any(s not in self._pages for s in names):
             raise ValueError("sequences must be different ones that the cache holds")

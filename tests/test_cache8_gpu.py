@@ -237,3 +237,25 @@ def test_other_stream_and_graph_replays():
         load(i)
         want = all_bytes(call())
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_pool_beyond_4_gib():
+    """Rows whose byte offsets pass 32 bits: what the same call leaves in a small pool."""
+    from paper_2307_02486_amd import cache_append
+    note("[append8] large pool")
+    pages, page, H, D = 37000, 64, 16, 128   # 4.85 GB each of k and v
+    large = [torch.zeros((pages, H, page, D), dtype=torch.uint8, device="cuda").view(F8) for _ in range(2)]
+    scales = [torch.zeros((pages, H, 4), dtype=torch.uint8, device="cuda").view(E8) for _ in range(2)]
+    ids = torch.tensor([36999, 35001, 36000], dtype=torch.int32, device="cuda")
+    small = [torch.zeros((3, H, page, D), dtype=torch.uint8, device="cuda").view(F8) for _ in range(2)]
+    small_scales = [torch.zeros((3, H, 4), dtype=torch.uint8, device="cuda").view(E8) for _ in range(2)]
+    for n0, n1 in ((0, 150), (150, 151)):
+        x = workloads.make_random((n1 - n0, 2 * H, D), BF, 1.0, 9, "cuda", n0)
+        lens, start = (torch.tensor(i, dtype=torch.int32, device="cuda") for i in ([n1], [0, n1 - n0]))
+        for pools, sc, table in ((large, scales, ids), (small, small_scales, torch.arange(3, dtype=torch.int32, device="cuda"))):
+            cache_append(None, x[:, :H], x[:, H:], *pools, table[None].contiguous(), lens, start,
+                         k_scale=sc[0], v_scale=sc[1])
+    for a, b in zip(large + scales, small + small_scales):
+        a, b = a.view(torch.uint8), b.view(torch.uint8)
+        assert bool((b != 0).any()) and torch.equal(a[ids.long()], b)
+        assert int(torch.count_nonzero(a)) == int(torch.count_nonzero(b))

@@ -188,6 +188,28 @@ def test_binding_refuses_host_tensors():
         evict_pages(z(4, d=torch.float32), i(1, 4), i(1), 16, 2)
 
 
+def test_calls_run_on_the_tensors_device(monkeypatch):
+    """Stream 0 is the current device's: a call for another device makes that current."""
+    from paper_2307_02486_amd import ops
+    now, seen = [0], []
+
+    class On:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.dev
+
+        def __exit__(self, *_):
+            now[0] = self.was
+
+    monkeypatch.setattr(ops.torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(ops.torch.cuda, "device", On)
+    for dev in (0, 1):
+        assert ops._call_on(dev, lambda *x: seen.append((now[0], x)) or 7, "a", 2) == 7
+    assert seen == [(0, ("a", 2)), (1, ("a", 2))] and now == [0]
+
+
 def test_scales_are_checked():
     from paper_2307_02486_amd.ops import _check_scale
     c = torch.zeros((4, 2, 32, 64), dtype=torch.uint8).view(F8)
@@ -229,6 +251,8 @@ def test_pages_that_are_gone_stay_gone(monkeypatch):
     monkeypatch.setattr(serving, "evict_pages", evict)
     with pytest.raises(ValueError):
         cache.evict(-1)
+    with pytest.raises(ValueError, match="last"):
+        cache.evict(2, last=0)  # the next tokens need it
     with pytest.raises(ValueError):
         cache.evict(2, ["a", "x"])
     with pytest.raises(ValueError):

@@ -106,3 +106,22 @@ def test_other_stream_and_graph_replays():
         want = evict_pages(w, table, lens, 16, 20)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_in_place_and_more_to_keep_than_there_can_be():
+    from paper_2307_02486_amd import _lib, evict_pages
+    note("[evict] in place")
+    lib = _lib.load()
+    for B, most in ((5, 70), (1, 20000)):
+        w, table, lens = case(B, most, 16, 5, "few")
+        want = evict_ref(w, table, lens, 16, most // 3, 1, 2)
+        w, table, lens = (torch.from_numpy(x).cuda() for x in (w, table, lens))
+        freed, count = torch.empty_like(table), torch.empty_like(lens)
+        given = table.clone()
+        rc = lib.dilated_attn_evict_pages(*(t.data_ptr() for t in (w, table, lens, table, freed, count)), B, w.numel(), 16,
+                                          most, most // 3, 1, 2, None)
+        torch.cuda.synchronize()
+        assert rc == 0 and all(np.array_equal(g.cpu().numpy(), x) for g, x in zip((table, freed, count), want))
+        for more in (dict(keep=2 ** 64), dict(keep=0, first=2 ** 70), dict(keep=0, last=2 ** 64)):
+            held, _, none = evict_pages(w, given, lens, 16, **more)
+            assert torch.equal(held, given) and not bool(none.any())

@@ -225,3 +225,39 @@ def test_other_stream_and_graph_replays():
             want = [*call(), weights]
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_columns_dealt_out():
+    """So many tokens and heads of a key head that several workgroups share them."""
+    from paper_2307_02486_amd import page_weights
+    note("[weights] columns dealt out")
+    for new, before, H, Hkv, D, pats in (([700, 3], [100, 900], 8, 1, 64, [(1024, 1), (2048, 3)]),
+                                         ([1500], [40], 4, 4, 32, DENSE)):
+        q, kc, vc, ks, vs, dev, table, lens, start = setup(new, before, H, Hkv, D, 16, BF)
+        lse64, want = reference(q, held_values(kc, vc, ks, vs), table, lens, start, 16, pats)
+        lse = torch.from_numpy(lse64.T.astype(np.float32)).contiguous().cuda()
+        weights = torch.zeros(kc.shape[0], device="cuda")
+        page_weights(q, lse, kc, ks, *dev, pats, weights)
+        assert (np.abs(to64(weights) - want) <= 2e-5 * want + 1e-6).all()
+
+
+def test_pool_beyond_4_gib():
+    """Rows whose byte offsets pass 32 bits: the weights that the same call gives in a small pool."""
+    from paper_2307_02486_amd import page_weights
+    note("[weights] large pool")
+    pages, page, H, D = 37000, 64, 16, 128   # 4.85 GB
+    large = torch.zeros((pages, H, page, D), dtype=torch.uint8, device="cuda").view(F8)
+    scales = torch.full((pages, H, 4), 127, dtype=torch.uint8, device="cuda").view(E8)
+    ids = torch.tensor([36999, 35001, 36000, 34000, 33001], dtype=torch.int32, device="cuda")
+    small, small_scales = normal_pool(5, H, page, D, 5)
+    large.view(torch.uint8)[ids.long()] = small.view(torch.uint8)
+    scales.view(torch.uint8)[ids.long()] = small_scales.view(torch.uint8)
+    for new in (1, 90):
+        q = workloads.make_random((new, H, D), BF, 1.0, 5, "cuda", 0)
+        lse = torch.full((H, new), 6.0, device="cuda")
+        lens, start = (torch.tensor(i, dtype=torch.int32, device="cuda") for i in ([300], [0, new]))
+        got, want = torch.zeros(pages, device="cuda"), torch.zeros(5, device="cuda")
+        page_weights(q, lse, large, scales, ids[None].contiguous(), lens, start, [(128, 1), (512, 3)], got)
+        page_weights(q, lse, small, small_scales, torch.arange(5, dtype=torch.int32, device="cuda")[None], lens, start,
+                     [(128, 1), (512, 3)], want)
+        assert bool((want > 0).any()) and torch.equal(got[ids.long()], want) and int((got != 0).sum()) == int((want != 0).sum())
