@@ -19,7 +19,7 @@ extern "C" {
  * page_size, D] bytes, and each block of DA_CACHE_BLOCK tokens (a whole page, if
  * that is fewer) of one key head has a scale: a byte x stands for 2^(x - 127), and
  * an element is its e4m3 value times its block's scale.  The append writes
- * 1 <= x <= 253; other bytes are taken for what the formula says.
+ * 1 <= x <= 253; 0 and 255 are not to be there.
  *
  * A table entry outside [0, num_pages) is a page that is not there: it holds no
  * keys.  Tokens keep their positions when pages before them go.

@@ -17,9 +17,9 @@
 // 45 us and 256 keys a round of the workgroup 67.  What is left is the chain of an
 // item's start (lengths, table, queries, keys) and the tail, as in the attention.
 // Chunks (512 tokens at 31500, 16 heads of 128 over four key heads, five patterns, 6.1
-// GFLOP): 45 us and 6.4; with every key operand read from LDS again for each 16
-// columns 159.  Bound by the exponentials and the columns' loads beside them: each
-// wave has 64 keys and 16 columns a step, at two to three waves a SIMD.
+// GFLOP): 33 us and 6.4; with a tile of keys a workgroup in every pattern 45, and with
+// every key operand read from LDS again for each 16 columns 159.  Bound by latency: an
+// item's start and its few steps of 16 columns, at two to three waves a SIMD.
 //
 // evict_pages: a workgroup per sequence finds the weight up to which pages go by
 // counting digits of eight bits, then lists them in the order of the table.  Bound by
@@ -313,8 +313,8 @@ __global__ __launch_bounds__(kPgThreads) void weight_tokens(WeightArgs a) {
   for (int i = p0 + lane; i < p1; i += 64) part[i] = sm.psum[i - it.p0];
 }
 
-// Rows that are sequences: the waves share a tile's keys and take 16 columns in turn (a
-// long chunk has hundreds of them).
+// Rows that are sequences.  Of many columns (a long chunk has hundreds) the waves share a
+// tile's keys and take 16 in turn; of few each wave has a tile of its own and all columns.
 template <typename T, int D>
 __global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
   constexpr int KC = D / 32;
@@ -341,13 +341,16 @@ __global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
     const int t0 = first_at(P, rho, x0 - gs), t1 = first_at(P, rho, min(x1 - gs, P.w));  // keys
     const int q0 = max(first_at(P, rho, c.c0 - gs), t0), q1 = first_at(P, rho, min(c.c1 - gs, P.w));  // queries that see some
     if (q0 >= q1) continue;
-    for (int k0 = t0; k0 < t1 && k0 < q1; k0 += kWtKeys) {
+    const bool apart = (q1 - q0) * nh <= kWeightApart;
+    for (int k00 = t0; k00 < t1 && k00 < q1; k00 += apart ? kPgWaves * kWtKeys : kWtKeys) {
+      const int k0 = apart ? k00 + wv * kWtKeys : k00;  // the wave's keys
       // Columns: tokens qa .. q1 - 1 of the nh heads, head by head (in blocks of 16
       // tokens if there are that many, so that a block's last key is near its first);
       // this item's share of them.
-      const int qa = max(q0, k0), ntok = q1 - qa, per = ntok < 16 ? ntok : (ntok + 15) & ~15, cols = per * nh;
+      const int qa = max(q0, k0), ntok = k0 < t1 ? max(q1 - qa, 0) : 0, per = ntok < 16 ? ntok : (ntok + 15) & ~15,
+                cols = per * nh;
       const int share = (static_cast<int>(P.tile_split.div(((cols + 15) >> 4) + P.tile_split.d - 1))) << 4;
-      const int cend = min(cols, (it.share + 1) * share), cbegin = it.share * share + 16 * wv;
+      const int cend = min(cols, (it.share + 1) * share), cbegin = it.share * share + (apart ? 0 : 16 * wv);
       f32x4 sum[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) sum[u] = f32x4{0, 0, 0, 0};
@@ -369,7 +372,7 @@ __global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
           load_queries<T, D>(a, tok, head, grp, there, f);
           x.last = lse_of(a, head, tok, x.l) && there ? token : -1;
         };
-        constexpr int kStep = 16 * kPgWaves;
+        const int step = apart ? 16 : 16 * kPgWaves;
         QueryFrag<T, D> f;
         Column x;
         column(cbegin + m, f, x);
@@ -379,10 +382,10 @@ __global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
 #pragma unroll
           for (int s = 0; s < KC; ++s) k[u][s] = kf[u >> 1].wide(u & 1, s);
         const bool some = ~live != 0;
-        for (int b0 = cbegin; b0 < cend; b0 += kStep) {
+        for (int b0 = cbegin; b0 < cend; b0 += step) {
           const QueryFrag<T, D> now = f;
           const Column at = x;
-          if (b0 + kStep < cend) column(b0 + kStep + m, f, x);  // the next one's on their way
+          if (b0 + step < cend) column(b0 + step + m, f, x);  // the next one's on their way
           f32x4 s[4];
           scores<T, D>(k, now, s);
           const int left = at.last - k0 - 4 * grp;  // the last key that counts, from the lane's first
@@ -404,9 +407,18 @@ __global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
       }
       put_sums(sum, m, grp, sm.sums[wv]);
       __syncthreads();
-      if (wv == 0)
-        add_pages(a, P, base, k0, min(k0 + kWtKeys, t1) - 1, lane,
-                  (sm.sums[0][lane] + sm.sums[1][lane]) + (sm.sums[2][lane] + sm.sums[3][lane]), sm.psum - it.p0);
+      if (wv == 0) {
+        const float got[kPgWaves] = {sm.sums[0][lane], sm.sums[1][lane], sm.sums[2][lane], sm.sums[3][lane]};
+        if (apart) {
+#pragma unroll
+          for (int w = 0; w < kPgWaves; ++w) {
+            const int first = k00 + w * kWtKeys;
+            if (first < min(t1, q1)) add_pages(a, P, base, first, min(first + kWtKeys, t1) - 1, lane, got[w], sm.psum - it.p0);
+          }
+        } else {
+          add_pages(a, P, base, k00, min(k00 + kWtKeys, t1) - 1, lane, (got[0] + got[1]) + (got[2] + got[3]), sm.psum - it.p0);
+        }
+      }
       __syncthreads();
     }
   }

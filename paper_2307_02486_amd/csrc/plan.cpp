@@ -350,11 +350,11 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
     return r >= G ? std::min(Hkv, (H + r - 1) / r) : Hkv;
   };
   // A sequence's columns are dealt out until a wave has about eight times sixteen.
-  // (512 tokens at 31500, 16 heads over four: 45 us; four times sixteen 48, sixteen
-  // times 46.6.)
+  // (512 tokens at 31500, 16 heads over four: 33 us; four times sixteen 39, sixteen
+  // times 35.)
+  auto columns = [&](int64_t r) { return T / r * ((G + std::min(G, r) - 1) / std::min(G, r)); };
   auto shares = [&](int64_t r) {
-    const int64_t cols = T / r * ((G + std::min(G, r) - 1) / std::min(G, r));
-    return p.lone ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, cols / 512));
+    return p.lone ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, columns(r) / 512));
   };
   double busy = 0.0;
   for (int i = 0; i < p.npat; ++i)
@@ -369,10 +369,11 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
     const int64_t pages = std::min(max_pages, span / page + 2);
     const int64_t keys = (span + t.r - 1) / t.r;
     const int64_t least = (pages + kWeightPages - 1) / kWeightPages;
-    // A round of keys an item: 256 of a token, 64 of a sequence.  (64 tokens at 1K to
-    // 32K: 33.0 us with 2048 workgroups or 1024, 34.3 with 4096 of 128 keys; the
-    // 512 tokens 45.0 with 4096 or 8192, 47.5 with 2048.)
-    const int64_t round = p.lone ? 256 : 64;
+    // A round of keys an item: 64 a wave, or 64 that the waves share.  (64 tokens at 1K
+    // to 32K: 33.0 us with 2048 workgroups or 1024, 34.3 with 4096 of 128 keys; the 512
+    // tokens 33 with 4096 or 2048, and with keys of their own for up to 128, 256, 512
+    // columns 33.2, 32.5, 41.7.)
+    const int64_t round = p.lone || columns(t.r) <= kWeightApart ? 256 : 64;
     const int64_t some = static_cast<int64_t>((p.lone ? 2048.0 : 4096.0) / std::max(1.0, busy) + 0.5);
     const int64_t splits = std::max({least, int64_t{1}, std::min({some, (keys + round - 1) / round, pages})});
     if (splits >= kMost || p.rows * n >= kMost - 8) return DA_EINVAL;

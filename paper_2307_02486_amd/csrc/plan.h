@@ -165,6 +165,7 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
 // the units, tile_split how many of them share a key head and offset, one_slot the
 // first unit's number among all, one_begin the first item.
 constexpr int64_t kWeightPages = 1024;  // pages of an item at most
+constexpr int64_t kWeightApart = 256;   // (token, head) pairs of a unit up to which each wave has keys of its own
 struct WeightPlan {
   int64_t T, B, H, Hkv, D, num_pages, page, max_pages;
   int dtype, page_log2, npat;
