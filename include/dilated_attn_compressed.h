@@ -79,19 +79,23 @@ int dilated_attn_paged_fwd_f8(const void* q, const da_paged_cache_f8_t* cache, v
  * cache       the keys (pages.v and v_scale are not looked at and may be NULL).
  * weights     device pointer, [num_pages] float32, updated.  The tables name a page
  *             once: of one that they name twice either sum may be lost.
+ * max_new     the most new tokens of any sequence, 0 if the caller does not know: it
+ *             chooses how the work is cut, and results differ by rounding only.
  * workspace   device scratch of at least the bytes that
- *             dilated_attn_page_weights_workspace reports for the same sizes.
+ *             dilated_attn_page_weights_workspace reports for the same sizes, one
+ *             call's at a time.
  *
  * Other arguments as for dilated_attn_paged_fwd_f8.  Scores are sums of exact
  * products in float32 (float32 queries as three bf16 terms), sums are float32 in an
  * order that the sizes fix: the same call gives the same bits every time.
  */
 int dilated_attn_page_weights_workspace(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages,
-                                        int64_t page_size, int64_t max_pages, const da_pattern_t* patterns,
-                                        int64_t num_patterns, int64_t dtype, uint64_t* bytes);
+                                        int64_t page_size, int64_t max_pages, int64_t max_new,
+                                        const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                                        uint64_t* bytes);
 int dilated_attn_page_weights(const void* q, const float* lse, const da_paged_cache_f8_t* cache, float* weights,
                               int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride,
-                              const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                              int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
                               float softmax_scale, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /*

@@ -116,10 +116,10 @@ def load():
     lib.dilated_attn_paged_fwd_f8.argtypes = ([vp, cache8, vp, vp] + [i64] * 7
                                               + [ctypes.POINTER(Pattern), i64, i64, f32, vp, u64, vp])
     lib.dilated_attn_paged_fwd_f8.restype = ctypes.c_int
-    lib.dilated_attn_page_weights_workspace.argtypes = [i64] * 8 + [ctypes.POINTER(Pattern), i64, i64,
+    lib.dilated_attn_page_weights_workspace.argtypes = [i64] * 9 + [ctypes.POINTER(Pattern), i64, i64,
                                                                     ctypes.POINTER(u64)]
     lib.dilated_attn_page_weights_workspace.restype = ctypes.c_int
-    lib.dilated_attn_page_weights.argtypes = [vp, vp, cache8, vp] + [i64] * 6 + [ctypes.POINTER(Pattern), i64, i64, f32,
+    lib.dilated_attn_page_weights.argtypes = [vp, vp, cache8, vp] + [i64] * 7 + [ctypes.POINTER(Pattern), i64, i64, f32,
                                                                                vp, u64, vp]
     lib.dilated_attn_page_weights.restype = ctypes.c_int
     lib.dilated_attn_evict_pages.argtypes = [vp] * 6 + [i64] * 7 + [vp]

@@ -536,26 +536,27 @@ int dilated_attn_paged_fwd_f8(const void* q, const da_paged_cache_f8_t* cache, v
 }
 
 int dilated_attn_page_weights_workspace(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages,
-                                        int64_t page_size, int64_t max_pages, const da_pattern_t* patterns,
-                                        int64_t num_patterns, int64_t dtype, uint64_t* bytes) {
+                                        int64_t page_size, int64_t max_pages, int64_t max_new,
+                                        const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                                        uint64_t* bytes) {
   if (!bytes) return DA_EINVAL;
   da::WeightPlan p;
-  const int rc = da::make_weight_plan(T, B, H, Hkv, D, num_pages, page_size, max_pages, patterns, num_patterns, dtype,
-                                      0.0f, &p);
+  const int rc = da::make_weight_plan(T, B, H, Hkv, D, num_pages, page_size, max_pages, max_new, patterns, num_patterns,
+                                      dtype, 0.0f, &p);
   if (rc == DA_OK) *bytes = p.workspace_bytes;
   return rc;
 }
 
 int dilated_attn_page_weights(const void* q, const float* lse, const da_paged_cache_f8_t* cache, float* weights,
                               int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride,
-                              const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
+                              int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
                               float softmax_scale, void* workspace, uint64_t workspace_bytes, void* stream) {
   if (const int rc = head_shapes(T, H, Hkv, D, dtype, &q_stride, &H, 1); rc != DA_OK) return rc;
   const da_paged_cache_t* c = cache ? &cache->pages : nullptr;
   if (!cache_ok(B, Hkv, c, false) || !cache->k_scale) return DA_EINVAL;
   da::WeightPlan p;
-  if (const int rc = da::make_weight_plan(T, B, H, Hkv, D, c->num_pages, c->page_size, c->max_pages, patterns,
-                                          num_patterns, dtype, softmax_scale, &p);
+  if (const int rc = da::make_weight_plan(T, B, H, Hkv, D, c->num_pages, c->page_size, c->max_pages, max_new,
+                                          patterns, num_patterns, dtype, softmax_scale, &p);
       rc != DA_OK)
     return rc;
   if (T == 0) return DA_OK;

@@ -325,10 +325,10 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
 }
 
 int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages, int64_t page,
-                     int64_t max_pages, const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
-                     float softmax_scale, WeightPlan* out) {
+                     int64_t max_pages, int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns,
+                     int64_t dtype, float softmax_scale, WeightPlan* out) {
   constexpr int64_t kMost = int64_t{1} << 31;
-  if (!out) return DA_EINVAL;
+  if (!out || max_new < 0) return DA_EINVAL;
   PagedPlan base;  // the same sizes and patterns are valid
   if (const int rc = make_paged_plan(T, B, H, Hkv, D, num_pages, page, max_pages, 1, patterns, num_patterns, dtype,
                                      softmax_scale, &base);
@@ -342,7 +342,11 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
   p.page_log2 = base.page_log2;
   p.npat = base.npat;
   p.scale = base.scale;
-  p.lone = T <= B;
+  // A token by itself reads its keys again: fine where most sequences have one, which is
+  // taken for granted of as many tokens as sequences, unless the caller knows of more.
+  // (64 new tokens of one sequence of 20000 among 63 without: 48 us as a sequence's,
+  // 225 as tokens; four 44 and 23.)
+  p.lone = T <= B && max_new <= kPagedFew;
   p.rows = p.lone ? T : B;
   const int64_t G = H / Hkv, reach = max_pages * page;
   auto units = [&](int64_t r) {

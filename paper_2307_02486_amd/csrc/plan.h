@@ -177,7 +177,7 @@ struct WeightPlan {
 };
 
 int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t num_pages, int64_t page,
-                     int64_t max_pages, const da_pattern_t* patterns, int64_t num_patterns, int64_t dtype,
-                     float softmax_scale, WeightPlan* out);
+                     int64_t max_pages, int64_t max_new, const da_pattern_t* patterns, int64_t num_patterns,
+                     int64_t dtype, float softmax_scale, WeightPlan* out);
 
 }  // namespace da

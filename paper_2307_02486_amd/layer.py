@@ -289,7 +289,8 @@ class LongNetAttention(torch.nn.Module):
                          *self.xpos_args, **scales)
         a, lse = paged_attn(q, *where, self.patterns, max_new=batch.max_new, **scales)
         if cache.weights is not None:
-            page_weights(q, lse, cache.k[layer], scales["k_scale"], *where[2:], self.patterns, cache.weights)
+            page_weights(q, lse, cache.k[layer], scales["k_scale"], *where[2:], self.patterns, cache.weights,
+                         max_new=batch.max_new)
         return _linear(self.out_proj, _layer_norm(self.ln_sub, a.view(T, H * D)))
 
     def float64_params(self) -> dict:

@@ -772,7 +772,8 @@ def _weight_workspace(shape: tuple, pats: tuple, dtype_code: int) -> int:
 def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_scale: torch.Tensor,
                  block_table: torch.Tensor, seq_lens: torch.Tensor, q_start: torch.Tensor,
                  patterns: Sequence[Tuple[int, int]], weights: torch.Tensor, scale: float | None = None,
-                 workspace: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
+                 workspace: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None,
+                 max_new: int | None = None) -> torch.Tensor:
     """The attention that each page of a cache in 8 bits gets from the new tokens,
     added to weights (float32 [num_pages], which is returned): over the page's
     keys, the tokens q [T, H, D] of its sequence that see them, their heads and
@@ -780,11 +781,13 @@ def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_sc
 
     q, the cache and the sequences' arrays are those of paged_attn, lse [H, T]
     what it returned; a row without a finite lse adds nothing.  Each head of a
-    token that sees a key adds one in all.  The tables name a page once.  Enqueued on `stream`.  A given workspace is a contiguous uint8 tensor
-    of at least page_weights_workspace_bytes."""
+    token that sees a key adds one in all.  The tables name a page once.
+    max_new, the most new tokens of any sequence if the caller knows it, chooses how
+    the work is cut.  Enqueued on `stream`.  A given workspace is a contiguous uint8
+    tensor of at least page_weights_workspace_bytes, one call's at a time."""
     lib = _lib.load()
     patterns = tuple(patterns)
-    shapes = (q.shape, q.stride(), q.dtype, k_cache.shape, block_table.shape)
+    shapes = (q.shape, q.stride(), q.dtype, k_cache.shape, block_table.shape, max_new)
     try:
         call = _WEIGHTS.get((shapes, patterns))
     except TypeError:  # patterns given as lists
@@ -797,10 +800,11 @@ def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_sc
         T, H, D = q.shape
         B, Hkv, pages, page, max_pages = _cache_shape(k_cache, block_table, D)
         dcode, pats = _dtype_code(q.dtype), _pattern_key(patterns)
-        need = _weight_workspace((T, B, H, Hkv, D, pages, page, max_pages), pats, dcode)
+        new = int(max_new or 0)
+        need = _weight_workspace((T, B, H, Hkv, D, pages, page, max_pages, new), pats, dcode)
         call = _keep(_WEIGHTS, (shapes, pats), (T, B, H, Hkv, D, _token_stride("q", q, 1, q.dtype, q.device), dcode, pages,
-                                                page, max_pages, max(need, 16), *_pattern_array_cached(pats)))
-    T, B, H, Hkv, D, qs, dcode, pages, page, max_pages, need, arr, n = call
+                                                page, max_pages, new, max(need, 16), *_pattern_array_cached(pats)))
+    T, B, H, Hkv, D, qs, dcode, pages, page, max_pages, new, need, arr, n = call
     dev = q.get_device()
     if dev < 0:
         raise RuntimeError("page_weights runs on the GPU only; q must be a device tensor")
@@ -822,7 +826,7 @@ def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_sc
                                   k_scale.data_ptr(), None)
     raw = _raw_stream(q.device) if stream is None else stream.cuda_stream
     rc = _call_on(dev, lib.dilated_attn_page_weights, q.data_ptr(), lse.data_ptr(), cache, weights.data_ptr(), T, B, H,
-                  Hkv, D, qs, arr, n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
+                  Hkv, D, qs, new, arr, n, dcode, float(scale or 0.0), workspace.data_ptr(), nbytes, raw)
     if rc != 0:
         raise _lib.DilatedAttnError(rc, lib)
     _stream_use(stream, owned)
@@ -830,9 +834,11 @@ def page_weights(q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, k_sc
 
 
 def page_weights_workspace_bytes(T: int, B: int, H: int, Hkv: int, D: int, num_pages: int, page_size: int,
-                                 max_pages: int, patterns: Sequence[Tuple[int, int]], dtype=torch.bfloat16) -> int:
+                                 max_pages: int, patterns: Sequence[Tuple[int, int]], dtype=torch.bfloat16,
+                                 max_new: int | None = None) -> int:
     """Validate a page_weights problem and return the workspace it needs (host only)."""
-    shape = (int(T), int(B), int(H), int(Hkv), int(D), int(num_pages), int(page_size), int(max_pages))
+    shape = (int(T), int(B), int(H), int(Hkv), int(D), int(num_pages), int(page_size), int(max_pages),
+             int(max_new or 0))
     return _weight_workspace(shape, _pattern_key(patterns), _dtype_code(dtype))
 
 

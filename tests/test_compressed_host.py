@@ -71,6 +71,10 @@ def test_workspace_holds_a_sum_of_each_unit_and_page():
     assert need(patterns=((64, 2),)) >= 2 * 4 * 4 * 4  # both offsets of a key head
     assert need(T=2, patterns=((64, 2),), max_pages=64) < need(patterns=((64, 2),), max_pages=64)
     assert need(T=0) >= 0
+    from paper_2307_02486_amd import page_weights_workspace_bytes
+    sizes = (70, 80, 4, 2, 64, 100, 16, 64, ((64, 2),))  # a token's sums by themselves, or a sequence's
+    assert len({page_weights_workspace_bytes(*sizes, max_new=n) for n in (None, 0, 1, 4)}) == 1
+    assert page_weights_workspace_bytes(*sizes, max_new=70) != page_weights_workspace_bytes(*sizes)
 
 
 @pytest.mark.parametrize("change", [
@@ -135,11 +139,11 @@ def test_paged_fwd_refuses(lib, change, code):
 
 
 def weigh(lib, q=0x100000, lse=0x300000, weights=0x310000, T=3, B=2, H=4, Hkv=2, D=64, qs=256, dtype=1, scale=0.0,
-          ws=0x8000000, ws_bytes=1 << 24, patterns=((64, 1),), **cache):
+          ws=0x8000000, ws_bytes=1 << 24, patterns=((64, 1),), max_new=0, **cache):
     from paper_2307_02486_amd import _lib
     arr, n = _lib.pattern_array(patterns)
-    return name(lib.dilated_attn_page_weights(q, lse, f8_args(**cache), weights, T, B, H, Hkv, D, qs, arr, n, dtype, scale,
-                                              ws, ws_bytes, None))
+    return name(lib.dilated_attn_page_weights(q, lse, f8_args(**cache), weights, T, B, H, Hkv, D, qs, max_new, arr, n, dtype,
+                                              scale, ws, ws_bytes, None))
 
 
 @pytest.mark.parametrize("change, code", [
@@ -148,7 +152,7 @@ def weigh(lib, q=0x100000, lse=0x300000, weights=0x310000, T=3, B=2, H=4, Hkv=2,
     (dict(lse=0x300002), "DA_EALIGN"), (dict(weights=0x310001), "DA_EALIGN"), (dict(ws=0x8000008), "DA_EALIGN"),
     (dict(ws_bytes=16), "DA_EWORKSPACE"), (dict(weights=0x5000000), "DA_EINVAL"), (dict(ws=0x1000000), "DA_EINVAL"),
     (dict(weights=0x300004), "DA_EINVAL"), (dict(weights=0x8000010), "DA_EINVAL"), (dict(D=96), "DA_EUNSUPPORTED"),
-    (dict(scale=-1.0), "DA_EINVAL"), (dict(k=None), "DA_EINVAL"),
+    (dict(scale=-1.0), "DA_EINVAL"), (dict(k=None), "DA_EINVAL"), (dict(max_new=-1), "DA_EINVAL"),
 ], ids=str)
 def test_page_weights_refuses(lib, change, code):
     assert weigh(lib, **change) == code

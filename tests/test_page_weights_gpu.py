@@ -261,3 +261,19 @@ def test_pool_beyond_4_gib():
         page_weights(q, lse, small, small_scales, torch.arange(5, dtype=torch.int32, device="cuda")[None], lens, start,
                      [(128, 1), (512, 3)], want)
         assert bool((want > 0).any()) and torch.equal(got[ids.long()], want) and int((got != 0).sum()) == int((want != 0).sum())
+
+
+def test_any_hint_of_the_most_new_tokens():
+    """As many tokens as sequences or fewer, in one of them, some or all."""
+    from paper_2307_02486_amd import page_weights
+    note("[weights] hints")
+    for new in ([40] + [0] * 59, [1, 3, 0, 0, 1], [1, 1, 1]):
+        before = [500 + 7 * i for i in range(len(new))]
+        for H, Hkv, pats in ((4, 4, [(128, 1), (512, 4)]), (8, 2, [(64, 1), (4096, 2)])):
+            q, kc, vc, ks, vs, dev, table, lens, start = setup(new, before, H, Hkv, 64, 16, BF)
+            lse64, want = reference(q, held_values(kc, vc, ks, vs), table, lens, start, 16, pats)
+            lse = torch.from_numpy(lse64.T.astype(np.float32)).contiguous().cuda()
+            for hint in (None, 1, 3, max(new), 1000):
+                weights = torch.zeros(kc.shape[0], device="cuda")
+                page_weights(q, lse, kc, ks, *dev, pats, weights, max_new=hint)
+                assert (np.abs(to64(weights) - want) <= 2e-5 * want + 1e-6).all(), hint
