@@ -493,7 +493,7 @@ struct EvictArgs {
   const float* weights;
   const int32_t *table, *lens;
   int32_t *table_out, *freed, *count;
-  int32_t num_pages, max_pages, page_log2;
+  int32_t B, num_pages, max_pages, page_log2;
   int64_t keep, first, last;
 };
 
@@ -521,6 +521,7 @@ __global__ __launch_bounds__(kWaves * 64) void evict(EvictArgs a) {
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t b = launch_index();
+  if (b >= a.B) return;
   const int32_t* table = a.table + b * a.max_pages;
   int32_t* out = a.table_out + b * a.max_pages;
   int32_t* freed = a.freed + b * a.max_pages;
@@ -689,8 +690,8 @@ hipError_t launch_page_weights(const WeightPlan& p, const void* q, int64_t q_str
 }
 
 hipError_t launch_evict(const EvictCall& c, hipStream_t stream) {
-  EvictArgs a{c.weights, c.table, c.lens, c.table_out, c.freed, c.count, static_cast<int32_t>(c.num_pages),
-              static_cast<int32_t>(c.max_pages), 0, c.keep, c.first, c.last};
+  EvictArgs a{c.weights, c.table, c.lens, c.table_out, c.freed, c.count, static_cast<int32_t>(c.B),
+              static_cast<int32_t>(c.num_pages), static_cast<int32_t>(c.max_pages), 0, c.keep, c.first, c.last};
   while ((int64_t{1} << a.page_log2) < c.page_size) ++a.page_log2;
   // A table of 512 pages takes 6.7 us with four waves and 8.2 with sixteen, one of 1024
   // 9.0 and 10.6, one of 2048 13.5 and 12.3 (64 sequences; one takes about as long).
