@@ -698,7 +698,7 @@ hipError_t launch_evict(const EvictCall& c, hipStream_t stream) {
   if (c.max_pages <= kEvSmall)
     hipLaunchKernelGGL(evict<4>, grid_of(c.B), dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL(evict<16>, grid_of(c.B), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL(evict<16>, grid_of(c.B, 1024), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
 
