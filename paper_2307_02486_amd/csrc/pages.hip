@@ -514,8 +514,9 @@ __global__ __launch_bounds__(kWaves * 64) void evict(EvictArgs a) {
   constexpr int kAtOnce = kWaves / 2;                    // chunks whose loads are under way together
   // Digits are counted in kWaves copies, a lane in one of them: most weights share
   // their first digits, and adds to one address come one after another.
+  constexpr int kCopy = 260;  // words of a copy: 256, and the copies begin in different banks
   __shared__ __attribute__((aligned(16))) uint32_t keys[kKept];
-  __shared__ __attribute__((aligned(16))) uint32_t hist[kWaves][260];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kWaves * kCopy];
   __shared__ int red[2][kWaves];
   __shared__ int found[2];
   const int tid = __builtin_amdgcn_workitem_id_x(), lane = tid & 63;
@@ -579,18 +580,18 @@ __global__ __launch_bounds__(kWaves * 64) void evict(EvictArgs a) {
   uint32_t least = 0;
   int rest = go;  // of those that have the digits so far
   for (int shift = 24; shift >= 0 && go > 0; shift -= 8) {
-    for (int i = tid; i < kWaves * 260; i += kWaves * 64) hist[0][i] = 0;
+    for (int i = tid; i < kWaves * kCopy; i += kWaves * 64) hist[i] = 0;
     __syncthreads();
     for (int pg = w0 + lane; pg < min(w1, n); pg += 64) {
       const uint32_t k = key_at(pg);
       if (k != 0 && (shift == 24 || k >> (shift + 8) == least >> (shift + 8)))
-        atomicAdd(&hist[lane & (kWaves - 1)][k >> shift & 255], 1u);
+        atomicAdd(&hist[(lane & (kWaves - 1)) * kCopy + (k >> shift & 255)], 1u);
     }
     __syncthreads();
     if (wv == 0) {  // four digits a lane
       u32x4 h = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) h += *reinterpret_cast<const u32x4*>(&hist[w][4 * lane]);
+      for (int w = 0; w < kWaves; ++w) h += *reinterpret_cast<const u32x4*>(&hist[w * kCopy + 4 * lane]);
       const int s = static_cast<int>(h[0] + h[1] + h[2] + h[3]);
       int before = running_sum(s) - s;
       if (before < rest && before + s >= rest) {
