@@ -85,7 +85,7 @@ int dilated_attn_paged_fwd_f8(const void* q, const da_paged_cache_f8_t* cache, v
  *             dilated_attn_page_weights_workspace reports for the same sizes, one
  *             call's at a time.
  *
- * Other arguments as for dilated_attn_paged_fwd_f8.  Scores are sums of exact
+ * Other arguments as for dilated_attn_paged_fwd_f8, with (T + 32) * H < 2^31.  Scores are sums of exact
  * products in float32 (float32 queries as three bf16 terms), sums are float32 in an
  * order that the sizes fix: the same call gives the same bits every time.
  */
@@ -114,7 +114,7 @@ int dilated_attn_page_weights(const void* q, const float* lse, const da_paged_ca
  * freed       device pointer, int32 [B, max_pages], written: the pages that go, in
  *             the order of the row, then -1.
  * count       device pointer, int32 [B], written: how many go.
- * keep, first, last: at least 0.
+ * page_size, max_pages: as in da_paged_cache_t.  keep, first, last: at least 0.
  */
 int dilated_attn_evict_pages(const float* weights, const int32_t* block_table, const int32_t* seq_lens,
                              int32_t* table_out, int32_t* freed, int32_t* count, int64_t B, int64_t num_pages,

@@ -74,7 +74,7 @@ int dilated_attn_qk_norm_xpos_bwd(const void* dqo, const void* dko, const void* 
 /*
  * A paged cache of keys and values, and the sequences of one call.
  *
- * A call has T new tokens of B sequences, side by side: those of sequence b
+ * A call has T new tokens of B sequences (1 <= B <= 2^31 - 2^16), side by side: those of sequence b
  * are rows q_start[b] .. q_start[b + 1] - 1 of its token arrays, and they are
  * the last of the seq_lens[b] tokens that the sequence has with them.  Token p
  * (0-based) of sequence b lies in page block_table[b][p / page_size] at
@@ -96,7 +96,7 @@ typedef struct {
   const int32_t* q_start;     /* device, [B + 1], ascending, from 0 to T       */
   int64_t num_pages;          /* num_pages * Hkv * page_size <= 2^32           */
   int64_t page_size;          /* a power of two, at most 2^16                  */
-  int64_t max_pages;          /* entries of a table row; max_pages * page_size < 2^31 */
+  int64_t max_pages;          /* entries of a table row; max_pages * page_size <= 2^31 - 2^16 */
 } da_paged_cache_t;
 
 /*

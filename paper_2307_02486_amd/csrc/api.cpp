@@ -386,8 +386,9 @@ namespace {
 bool cache_ok(int64_t B, int64_t Hkv, const da_paged_cache_t* c, bool values = true) {
   if (!c || !c->k || (values && !c->v) || !c->block_table || !c->seq_lens || !c->q_start) return false;
   constexpr int64_t kMost = int64_t{1} << 31;
-  return B >= 1 && B < kMost && c->page_size >= 1 && c->page_size <= (int64_t{1} << 16) &&
-         (c->page_size & (c->page_size - 1)) == 0 && c->max_pages >= 1 && c->max_pages < kMost / c->page_size &&
+  return B >= 1 && B <= da::kPagedMost && c->page_size >= 1 && c->page_size <= (int64_t{1} << 16) &&
+         (c->page_size & (c->page_size - 1)) == 0 && c->max_pages >= 1 &&
+         c->max_pages <= da::kPagedMost / c->page_size &&
          c->num_pages >= 1 && c->num_pages < kMost && c->num_pages <= (int64_t{1} << 32) / c->page_size / Hkv;
 }
 
@@ -590,7 +591,7 @@ int dilated_attn_evict_pages(const float* weights, const int32_t* block_table, c
   if (!weights || !block_table || !seq_lens || !table_out || !freed || !count) return DA_EINVAL;
   if (B < 1 || B >= kMost || num_pages < 1 || num_pages >= kMost || page_size < 1 ||
       page_size > (int64_t{1} << 16) || (page_size & (page_size - 1)) || max_pages < 1 ||
-      max_pages >= kMost / page_size || keep < 0 || first < 0 || last < 0 || last >= kMost)
+      max_pages > da::kPagedMost / page_size || keep < 0 || first < 0 || last < 0 || last >= kMost)
     return DA_EINVAL;
   for (const void* x : {static_cast<const void*>(weights), static_cast<const void*>(block_table),
                         static_cast<const void*>(seq_lens), static_cast<const void*>(table_out),

@@ -139,10 +139,13 @@ __device__ inline bool weight_item(const WeightArgs& a, int idx, int pi, int lan
   // this split's pages, of those from the first token's segment on
   it.seg0 = static_cast<int>(P.fw.div(it.c.c0)) * P.w;
   const int pg0 = it.seg0 >> a.page_log2, pages = ((it.c.c1 - 1) >> a.page_log2) + 1 - pg0;
-  const int per = min(static_cast<int>(P.one_split.div(pages + P.one_split.d - 1)), static_cast<int>(kWeightPages));
-  it.p0 = pg0 + split * per;
-  it.p1 = min(it.p0 + per, pg0 + pages);
-  return it.p0 < it.p1;
+  const int per = min(static_cast<int>(P.one_split.div(pages - 1)) + 1, static_cast<int>(kWeightPages));
+  // (where a table has close to 2^31 pages, the splits past the row's end begin beyond that)
+  const uint32_t skip = static_cast<uint32_t>(split) * per;
+  if (skip >= static_cast<uint32_t>(pages)) return false;
+  it.p0 = pg0 + static_cast<int>(skip);
+  it.p1 = pg0 + min(static_cast<int>(skip) + per, pages);
+  return true;
 }
 // The first t at or after segment-local position x, of those rho + t r.
 __device__ inline int first_at(const PagedPattern& P, int rho, int x) {

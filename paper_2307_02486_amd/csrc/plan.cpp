@@ -186,9 +186,9 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
                     int64_t dtype, float softmax_scale, PagedPlan* out) {
   constexpr int64_t kMost = int64_t{1} << 31;
   if (!patterns || !out) return DA_EINVAL;
-  if (T < 0 || T >= kMost || B < 1 || B >= kMost || H < 1 || H >= (int64_t{1} << 16) || Hkv < 1 || H % Hkv)
+  if (T < 0 || T >= kMost || B < 1 || B > kPagedMost || H < 1 || H >= (int64_t{1} << 16) || Hkv < 1 || H % Hkv)
     return DA_EINVAL;
-  if (page < 1 || page > (int64_t{1} << 16) || (page & (page - 1)) || max_pages < 1 || max_pages >= kMost / page ||
+  if (page < 1 || page > (int64_t{1} << 16) || (page & (page - 1)) || max_pages < 1 || max_pages > kPagedMost / page ||
       num_pages < 1 || num_pages > (int64_t{1} << 32) / page / Hkv || num_pages >= kMost || max_new < 0)
     return DA_EINVAL;
   if (num_patterns < 1 || num_patterns > DA_MAX_PATTERNS) return DA_EINVAL;
@@ -334,6 +334,7 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
                                      softmax_scale, &base);
       rc != DA_OK)
     return rc;
+  if ((T + 32) * H >= kMost) return DA_EINVAL;  // a unit's columns are counted in blocks of 16 tokens
   WeightPlan p;
   std::memset(&p, 0, sizeof(p));
   p.T = T; p.B = B; p.H = H; p.Hkv = Hkv; p.D = D;

@@ -118,6 +118,9 @@ int make_plan(int64_t B, int64_t N, int64_t H, int64_t D, const da_pattern_t* pa
 // 16 in tiles 37.)  Both write one partial row per (token, head) and slot, a
 // slot being one split of one pattern's keys, and the join reads them.
 constexpr int64_t kPagedFew = 4;
+// Positions of a table, and sequences of a call, at most: the kernels step over either by
+// up to some thousands (tiles of keys, waves of sequences), whose sum with them has to fit 31 bits.
+constexpr int64_t kPagedMost = (int64_t{1} << 31) - (int64_t{1} << 16);
 constexpr int64_t kPagedRows = 128;      // query rows of a tile
 constexpr int64_t kPagedKeyTile = 64;    // its keys at a time
 constexpr int64_t kPagedGroupRows = 16;  // query heads of one key head that a token's workgroup holds
