@@ -153,7 +153,9 @@ int dilated_attn_cache_append(const void* q, const void* k, const void* v, const
  * pattern's rows are kept as in dilated_attn_fwd; out rounded once.  DA_F32
  * computes in float32 throughout.  Results are finite under the conditions of
  * dilated_attn_fwd for the sequence's own tokens; a row that sees a key whose
- * score is NaN or plus infinity is NaN in out and lse.  What lies in the pool
+ * score is NaN or plus infinity is NaN in out and lse, and an element of v that is
+ * not finite makes that element of the rows that see its key not finite, and of no
+ * others.  What lies in the pool
  * beyond a sequence's length is never used, whatever it holds.  The same call gives
  * the same bits every time; keys are split by the sizes of the call, so a
  * sequence alone and in a batch can differ by the rounding of its sums.

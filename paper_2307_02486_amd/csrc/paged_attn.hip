@@ -39,6 +39,7 @@
 
 #include <algorithm>
 
+#include "heads_device.h"
 #include "paged_device.h"
 
 namespace da {
@@ -1348,6 +1349,7 @@ __device__ inline uint32_t bits_of(float x) {
   asm("" : "+v"(u));
   return u;
 }
+__device__ inline bool not_finite(float x) { return (bits_of(x) & 0x7f800000u) == 0x7f800000u; }
 // Whether a record marks a row that is not there.
 __device__ inline bool no_row(float x) { return bits_of(x) == 0xff800000u; }
 
@@ -1453,6 +1455,59 @@ __device__ inline void join_singles(const PagedArgs& a, int group) {
   if (sub == 0) put_row<T, D>(a, tk.tok, head, ch, x);
 }
 
+// Elements 8 ch .. of one row's out from its log-sum-exp (log2 units), key by key in
+// float32, by the D/8 lanes of the row.  For rows that tiles leave with something that is
+// not finite: a tile multiplies V by probabilities of zero where a row does not see a
+// key, and zero times a V that is not finite is NaN.  (Rows that see the key come out with
+// it once more.  4096 tokens at 28672, one of them with NaN in each head: 7 ms, where
+// without it the call takes 0.078, with the look at a row's sums or without.  Two keys at
+// a time: with four the join holds more registers, and that call takes 0.079.)
+template <int D>
+__device__ inline f32x8 row_by_keys(const PagedArgs& a, int b, int tok, int head, int ch, int pos, float lse2) {
+  constexpr int kUnroll = 2;
+  const int32_t* table = a.table + static_cast<int64_t>(b) * a.max_pages;
+  const int hk = head / a.G;
+  float q[8];
+  unpack(load16(static_cast<const u16*>(a.q) + tok * a.qs + head * D + ch * 8), q);
+  f32x8 acc = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+  for (int i = 0; i < a.npat; ++i) {
+    const PagedPattern& P = a.pat[i];
+    const Lattice x = lattice_of(P, pos);
+    if (head_offset(P, head) != x.rho) continue;
+    for (int t0 = 0; t0 < x.n; t0 += kUnroll) {
+      float k[kUnroll][8], v[kUnroll][8];
+      bool there[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int at = x.first + min(t0 + u, x.n - 1) * P.r, entry = table_entry(a, table, at);
+        there[u] = t0 + u < x.n && (!a.ks || static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.num_pages));
+        const int64_t row = cache_row(a, entry, hk, at);
+        if (a.ks) {
+          const float ks = scale_of(a.ks[row >> a.block_log2]), vs = scale_of(a.vs[row >> a.block_log2]);
+          const u32x2 kw = *reinterpret_cast<const u32x2*>(a.kc + row * D + ch * 8);
+          const u32x2 vw = *reinterpret_cast<const u32x2*>(a.vc + row * D + ch * 8);
+          unpack(widen8(kw[0], kw[1], ks), k[u]);
+          unpack(widen8(vw[0], vw[1], vs), v[u]);
+        } else {
+          unpack(*reinterpret_cast<const u32x4*>(a.kc + (row * D + ch * 8) * 2), k[u]);
+          unpack(*reinterpret_cast<const u32x4*>(a.vc + (row * D + ch * 8) * 2), v[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        float d = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d += q[e] * k[u][e];
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(row_sum<D / 8>(d), a.scale_log2, -lse2));
+        if (there[u])
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] += p * v[u][e];
+      }
+    }
+  }
+  return acc;
+}
+
 // Tokens of tiles, and those of no sequence: D/8 lanes a row, head by head and
 // token by token, the loads of all patterns before their use.  kPats bounds the
 // patterns at compile time: 5, the length of the paper's list, or all 16, whose
@@ -1520,7 +1575,19 @@ __device__ inline void join_tiles(const PagedArgs& a, int group) {
   }
 #pragma unroll
   for (int m = kLanes; m < kLanes * kSubs; m <<= 1) x.meet(m);
-  if (sub == 0 && group * kRows + tid / (kLanes * kSubs) < total) put_row<u16, D>(a, tok, head, ch, x);
+  if (sub != 0 || group * kRows + tid / (kLanes * kSubs) >= total) return;
+  float sum = x.acc[0];  // not finite if one of them is not
+#pragma unroll
+  for (int i = 1; i < 8; ++i) sum += x.acc[i];
+  if (const uint64_t bad = __ballot(not_finite(sum)); __builtin_expect(bad != 0, false)) {
+    const float lse2 = x.m + __builtin_amdgcn_logf(x.l);
+    if ((bad >> (lane - ch) & ((uint64_t{1} << kLanes) - 1)) && !not_finite(lse2)) {
+      x.acc = row_by_keys<D>(a, s.b, tok, head, ch, pos, lse2);
+      x.m = lse2;
+      x.l = 1.0f;
+    }
+  }
+  put_row<u16, D>(a, tok, head, ch, x);
 }
 
 // kTogether: the waves of a workgroup share a single token's row.
