@@ -38,7 +38,9 @@ typedef struct {
  * 448-fold is not below the block's largest finite magnitude; a block that has
  * tokens already keeps its scale or takes a larger one, its older values then
  * multiplied by the quotient (exact, but for those that fall below 2^-6 times the
- * new scale).  Scales never shrink while a block has tokens.  Infinities and NaN
+ * new scale: these are rounded once more).  Scales never shrink while a block has
+ * tokens; whoever wants to take an append back keeps a copy of the blocks in which
+ * its tokens follow earlier ones.  Infinities and NaN
  * become NaN and do not count for the scale.  Finite magnitudes have to be below
  * 2^127.
  *

@@ -535,9 +535,9 @@ CACHE_SCALE = torch.float8_e8m0fnu  # powers of two, one for each block of token
 CACHE_BLOCK = 16  # tokens of a block (a page of fewer is one block)
 
 
-def cache_scale_shape(k_cache: torch.Tensor) -> tuple:
-    """[num_pages, Hkv, blocks of a page]: the shape of the scales of a cache in 8 bits."""
-    pages, Hkv, page, _ = k_cache.shape
+def cache_scale_shape(k_cache) -> tuple:
+    """[num_pages, Hkv, blocks of a page]: the shape of the scales of a cache in 8 bits (a tensor or its shape)."""
+    pages, Hkv, page, _ = getattr(k_cache, "shape", k_cache)
     return pages, Hkv, page // min(page, CACHE_BLOCK)
 
 

@@ -9,7 +9,7 @@ from typing import NamedTuple, Sequence
 
 import torch
 
-from .ops import CACHE_F8, CACHE_SCALE, cache_scale_shape, evict_pages
+from .ops import CACHE_BLOCK, CACHE_F8, CACHE_SCALE, cache_scale_shape, evict_pages
 
 
 def xpos_span(gamma: float, scale_base: float) -> int:
@@ -82,13 +82,14 @@ class PagedCache:
         if xpos is not None:
             check_xpos(max_pages * page_size, self.center, *xpos)
         shape = (num_pages, num_heads, page_size, head_dim)
-        self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
-        self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
         self.k_scale = self.v_scale = self.weights = None
+        self._blocks = []  # 8 bits: bytes of k, k_scale, v, v_scale [layers, num_pages, num_heads, blocks of a page, ...]
         if dtype == CACHE_F8:
-            scales = dict(size=cache_scale_shape(self.k[0]), device=device, dtype=CACHE_SCALE)
-            self.k_scale = [torch.empty(**scales) for _ in range(layers)]
-            self.v_scale = [torch.empty(**scales) for _ in range(layers)]
+            self.k, self.k_scale, self.v, self.v_scale = (self._pool(layers, *x, device) for x in (
+                (shape, dtype), (cache_scale_shape(shape), CACHE_SCALE)) * 2)
+        else:
+            self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
+            self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
         if weigh:
             if dtype != CACHE_F8:
                 raise ValueError(f"weigh goes with a cache of {CACHE_F8}")
@@ -99,7 +100,15 @@ class PagedCache:
         self._pages: dict = {}
         self._length: dict = {}
         self._last: dict = {}  # the step in which a sequence was last extended
+        self._before: dict = {}  # 8 bits: by step, the blocks that its tokens share with earlier ones, as they were
         self._number = 0
+
+    def _pool(self, layers: int, shape: tuple, dtype, device) -> list:
+        """A tensor of this shape for each layer, of one allocation."""
+        pool = torch.empty((layers, *shape), device=device, dtype=dtype)
+        self._blocks.append(pool.view(torch.uint8).view(layers, *shape[:2], shape[2] // min(shape[2], CACHE_BLOCK), -1)
+                            if len(shape) == 4 else pool.view(torch.uint8))
+        return list(pool.unbind(0))
 
     def length(self, sequence) -> int:
         """Tokens that the cache holds of a sequence (any hashable name)."""
@@ -109,15 +118,55 @@ class PagedCache:
         """Forget a sequence; its pages go back to the pool."""
         self._free += [p for p in self._pages.pop(sequence, []) if p >= 0]
         self._length.pop(sequence, None)
-        self._last.pop(sequence, None)
+        self._settle(sequence)
+
+    def _settle(self, sequence):
+        """The sequence's last batch cannot be taken back any more."""
+        self._before.pop(self._last.pop(sequence, None), None)
+
+    def _keep_blocks(self, sequences: Sequence, new: Sequence[int]):
+        """The blocks in which these new tokens follow earlier ones, as they are: their
+        page and number in it, the earlier tokens, and their bytes.  An append may take a
+        larger scale for such a block and round its earlier values once more."""
+        size, at = min(self.page_size, CACHE_BLOCK), []
+        for s, n in zip(sequences, new):
+            had = self.length(s)
+            page = self._pages[s][had // self.page_size] if n > 0 and had % size else -1
+            if page >= 0:
+                at.append((page, had % self.page_size // size, had % size))
+        if not at:
+            return None
+        page, block, rows = torch.tensor(at).t().contiguous().to(self.device)
+        return page, block, rows, [b[:, page, :, block] for b in self._blocks]
+
+    def _put_back(self, page, block, rows, kept: list):
+        """The blocks of _keep_blocks, where an append has rescaled them.  A block whose
+        earlier values are not what rescaling makes of those kept (the batch before had not
+        run when they were kept) stays as it is."""
+        size = min(self.page_size, CACHE_BLOCK)
+        for i in (0, 2):  # k and v, each with its scale
+            was, scale = kept[i], kept[i + 1]
+            now, now_scale = (b[:, page, :, block] for b in self._blocks[i: i + 2])
+            more = now_scale.int() - scale.int()
+            want = (was.view(CACHE_F8).double() * torch.exp2(-more.double())[..., None]).float().to(CACHE_F8).float()
+            have = now.view(CACHE_F8).float()
+            same = ((want == have) | (want.isnan() & have.isnan())).view(*was.shape[:-1], size, -1).all(-1)
+            earlier = torch.arange(size, device=rows.device) < rows[:, None]
+            back = (same | ~earlier[:, None, None]).all(-1) & (more > 0)
+            self._blocks[i][:, page, :, block] = torch.where(back[..., None], was, now)
+            self._blocks[i + 1][:, page, :, block] = torch.where(back, scale, now_scale)
 
     def retract(self, batch: Batch):
         """Take back the extend that gave this batch: its sequences have their
         earlier lengths again, and pages taken for it go back to the pool.  Only
         while no other extend of one of them, nor a release or an evict, came since.
-        What its layers added to the weights of other pages stays."""
+        In a cache in 8 bits, blocks that its layers rescaled have their earlier values
+        and scales again, if the batches before had run when it was made.  What its
+        layers added to the weights of other pages stays."""
         if not batch.sequences or any(self._last.get(s) != batch.number for s in batch.sequences):
             raise ValueError("not the last batch of all its sequences")
+        if kept := self._before.pop(batch.number, None):
+            self._put_back(*kept)
         for s, n in zip(batch.sequences, batch.new):
             self._length[s] -= n
             pages, keep = self._pages[s], -(-self._length[s] // self.page_size)
@@ -150,7 +199,7 @@ class PagedCache:
                 gone = set(row[:n].tolist())
                 self._pages[s] = [-1 if p in gone else p for p in self._pages[s]]
                 self._free += reversed(sorted(gone))
-                self._last.pop(s, None)  # a batch made before cannot be taken back
+                self._settle(s)  # a batch made before names pages that went
         return sum(count)
 
     def _table(self, names: Sequence) -> torch.Tensor:
@@ -165,7 +214,8 @@ class PagedCache:
         it is empty), and the batch of a step in which they come.  Every layer
         then takes this batch once; if a layer does not (it raises, say), the
         batch has to be taken back, or the next one attends to tokens that are
-        not there."""
+        not there.  For that a cache in 8 bits keeps the blocks of 16 tokens that the
+        new ones share with earlier ones, until a sequence's next extend."""
         if len(set(sequences)) != len(sequences) or len(new) != len(sequences) or not len(new):
             raise ValueError("sequences must be different ones, with a number of new tokens each")
         if min(new) < 0:
@@ -177,7 +227,12 @@ class PagedCache:
             raise ValueError(f"a sequence of {max(lengths)} tokens is beyond {self.max_pages} pages of {self.page_size}")
         if sum(short) > len(self._free):
             raise RuntimeError(f"{sum(short)} pages are needed and {len(self._free)} are free")
+        kept = self._keep_blocks(sequences, new) if self._blocks else None
+        for s in sequences:
+            self._settle(s)
         self._number += 1
+        if kept is not None:
+            self._before[self._number] = kept
         taken = []
         for s, n, more in zip(sequences, lengths, short):
             taken += (fresh := [self._free.pop() for _ in range(more)])
