@@ -510,6 +510,12 @@ __device__ inline uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// grid_of for workgroups of 1024 threads, of which 2^22 are 2^32 work-items.
+inline dim3 grid_of_1024(int64_t workgroups) {
+  if (workgroups < (int64_t{1} << 22)) return dim3(static_cast<unsigned>(workgroups));
+  return dim3(static_cast<unsigned>(kGridRow), static_cast<unsigned>((workgroups + kGridRow - 1) / kGridRow));
+}
+
 // A wave has a run of the table's chunks of 64 pages, a lane a page.
 template <int kWaves>
 __global__ __launch_bounds__(kWaves * 64) void evict(EvictArgs a) {
@@ -702,7 +708,7 @@ hipError_t launch_evict(const EvictCall& c, hipStream_t stream) {
   if (c.max_pages <= kEvSmall)
     hipLaunchKernelGGL(evict<4>, grid_of(c.B), dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL(evict<16>, grid_of(c.B, 1024), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL(evict<16>, grid_of_1024(c.B), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
 
