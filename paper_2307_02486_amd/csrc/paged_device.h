@@ -61,20 +61,17 @@ struct Sequence {
 // wave: start [B + 1] ascends and the last entry that is not above a token is
 // its sequence's (empty ones before it share that value).  Whatever start
 // holds, the result is below B.  Up to 63 sequences all entries arrive in one
-// round of loads.
+// round of loads, which the caller has begun: lane l's entries of start and lens.
 template <typename Args, int kTokens>
-__device__ inline void find_sequences(const Args& a, const int (&tok)[kTokens], int lane, Sequence (&sq)[kTokens]) {
+__device__ inline void find_sequences(const Args& a, const int (&tok)[kTokens], int lane, int start, int len,
+                                      Sequence (&sq)[kTokens]) {
   int n[kTokens];
 #pragma unroll
-  for (int i = 0; i < kTokens; ++i) n[i] = 0;
-  int start = 0, len = 0;
-  for (int b0 = 0; b0 <= a.B; b0 += 64) {
-    const int b = b0 + lane;
-    start = a.start[min(b, a.B)];
-    len = a.lens[min(b, a.B - 1)];
-    here(len);
+  for (int i = 0; i < kTokens; ++i) n[i] = __popcll(__ballot(lane <= a.B && start <= tok[i]));
+  for (int b0 = 64; b0 <= a.B; b0 += 64) {
+    const int next = a.start[min(b0 + lane, a.B)];
 #pragma unroll
-    for (int i = 0; i < kTokens; ++i) n[i] += __popcll(__ballot(b <= a.B && start <= tok[i]));
+    for (int i = 0; i < kTokens; ++i) n[i] += __popcll(__ballot(b0 + lane <= a.B && next <= tok[i]));
   }
 #pragma unroll
   for (int i = 0; i < kTokens; ++i) {
@@ -91,6 +88,13 @@ __device__ inline void find_sequences(const Args& a, const int (&tok)[kTokens], 
       sq[i].len = a.lens[b];
     }
   }
+}
+template <typename Args, int kTokens>
+__device__ inline void find_sequences(const Args& a, const int (&tok)[kTokens], int lane, Sequence (&sq)[kTokens]) {
+  const int start = a.start[min(lane, a.B)];
+  int len = a.lens[min(lane, a.B - 1)];
+  here(len);
+  find_sequences(a, tok, lane, start, len, sq);
 }
 
 // Position of row tok of its sequence; -1 where it has none in the table.
