@@ -42,7 +42,7 @@ struct WeightArgs {
   const char* kc;
   const uint8_t* ks;
   const int32_t *table, *lens, *start;
-  float* part;     // [units][rows][max_pages]
+  float* part;     // of each pattern [units][rows][pages], from the row's first page on
   float* weights;  // [num_pages]
   int64_t qs;
   int32_t T, B, H, Hkv, G, npat, num_pages, max_pages, page_log2, block_log2, rows, items;
@@ -146,6 +146,13 @@ __device__ inline bool weight_item(const WeightArgs& a, int idx, int pi, int lan
   it.p0 = pg0 + static_cast<int>(skip);
   it.p1 = pg0 + min(static_cast<int>(skip) + per, pages);
   return true;
+}
+// The page that a row's sums begin with, if pg is its first.
+__device__ inline int first_sum(int pg) { return pg & -static_cast<int>(kWeightAlign); }
+// The item's partial sums: of page 0, were it among the row's.
+__device__ inline float* sums_of(const WeightArgs& a, const PagedPattern& P, const WeightItem& it) {
+  return a.part + P.one_slot * kWeightAlign + (static_cast<int64_t>(it.u) * a.rows + it.row) * P.tiles -
+         first_sum(it.seg0 >> a.page_log2);
 }
 // The first t at or after segment-local position x, of those rho + t r.
 __device__ inline int first_at(const PagedPattern& P, int rho, int x) {
@@ -312,7 +319,7 @@ __global__ __launch_bounds__(kPgThreads) void weight_tokens(WeightArgs a) {
       add_pages(a, P, base, first, min(first + kWtKeys, t1) - 1, lane, sm.sums[wv][lane], sm.psum - it.p0);
     }
   }
-  float* part = a.part + (static_cast<int64_t>(P.one_slot + it.u) * a.rows + it.row) * a.max_pages;
+  float* part = sums_of(a, P, it);
   for (int i = p0 + lane; i < p1; i += 64) part[i] = sm.psum[i - it.p0];
 }
 
@@ -426,7 +433,7 @@ __global__ __launch_bounds__(kPgThreads) void weight_sequences(WeightArgs a) {
     }
   }
   __syncthreads();
-  float* part = a.part + (static_cast<int64_t>(P.one_slot + it.u) * a.rows + it.row) * a.max_pages;
+  float* part = sums_of(a, P, it);
   for (int i = tid; i < it.p1 - it.p0; i += kPgThreads) part[it.p0 + i] = sm.psum[i];
 }
 
@@ -446,7 +453,6 @@ __global__ __launch_bounds__(kPgThreads) void weight_join(WeightArgs a) {
   const int at = min(pg, a.max_pages - 1), entry = a.table[static_cast<int64_t>(b) * a.max_pages + at];
   float s = 0.0f;
   const int rows = kLone ? c.c1 - c.c0 : 1;
-  const int64_t step = static_cast<int64_t>(a.rows) * a.max_pages;
   for (int i = 0; i < rows; ++i) {
     const int c0 = c.c0 + i, last = kLone ? c0 : c.c1 - 1;
     const int64_t row = kLone ? c.tok0 + c0 : b;
@@ -455,7 +461,8 @@ __global__ __launch_bounds__(kPgThreads) void weight_join(WeightArgs a) {
       const int from = (static_cast<int>(P.fw.div(c0)) * P.w) >> a.page_log2, to = last >> a.page_log2;
       if (pg - lane > to || pg - lane + 63 < from) continue;
       const bool in = pg >= from && pg <= to;
-      const float* part = a.part + P.one_slot * step + row * a.max_pages + min(max(pg, from), to);
+      const int64_t step = static_cast<int64_t>(a.rows) * P.tiles;
+      const float* part = a.part + P.one_slot * kWeightAlign + row * P.tiles + (min(max(pg, from), to) - first_sum(from));
       int units = P.one_heads.d;  // those that the row has
       if constexpr (kLone) {
         const int rho = lattice_of(P, c0).rho;

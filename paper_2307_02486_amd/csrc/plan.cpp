@@ -361,6 +361,7 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
   auto shares = [&](int64_t r) {
     return p.lone ? 1 : std::max<int64_t>(1, std::min<int64_t>(8, columns(r) / 512));
   };
+  int64_t sums = 0;  // in lines of kWeightAlign
   double busy = 0.0;
   for (int i = 0; i < p.npat; ++i)
     busy += static_cast<double>(p.rows) * units(base.pat[i].r) * shares(base.pat[i].r);
@@ -384,15 +385,18 @@ int make_weight_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, in
     if (splits >= kMost || p.rows * n >= kMost - 8) return DA_EINVAL;
     t.one_split = make_fastdiv(static_cast<uint32_t>(splits));
     t.one_heads = make_fastdiv(static_cast<uint32_t>(n));
-    t.one_slot = static_cast<int32_t>(p.units);
     t.one_begin = static_cast<int32_t>(p.items);
-    p.units += n;
+    // in lines: of a row that begins within one, no more than those of the table
+    const int64_t lines = std::min((pages - 1) / kWeightAlign + 2, (max_pages - 1) / kWeightAlign + 1);
+    if (sums >= kMost || lines > (int64_t{1} << 56) / std::max<int64_t>(1, p.rows * n)) return DA_EINVAL;
+    t.one_slot = static_cast<int32_t>(sums);
+    t.tiles = static_cast<int32_t>(lines * kWeightAlign);
+    sums += p.rows * n * lines;
     const int64_t padded = (p.rows * n + 7) / 8 * 8;  // units XCD by XCD
     if (padded > 0 && splits > (kMost - 1 - p.items) / padded) return DA_EINVAL;
     p.items += padded * splits;
   }
-  if (p.units >= kMost || (p.rows > 0 && p.units * max_pages > (int64_t{1} << 60) / p.rows)) return DA_EINVAL;
-  p.workspace_bytes = align_up(static_cast<uint64_t>(p.units) * p.rows * max_pages * 4);
+  p.workspace_bytes = static_cast<uint64_t>(sums) * kWeightAlign * 4;
   *out = p;
   return DA_OK;
 }

@@ -165,8 +165,12 @@ int make_paged_plan(int64_t T, int64_t B, int64_t H, int64_t Hkv, int64_t D, int
 // its keys lie in; it writes a partial sum for each of its pages, and a second launch
 // adds a page's.  A sequence's tokens and heads of a unit are dealt out to several
 // units where they are many.  In a PagedPattern: one_split are the splits, one_heads
-// the units, tile_split how many of them share a key head and offset, one_slot the
-// first unit's number among all, one_begin the first item.
+// the units, tile_split how many of them share a key head and offset, one_begin the
+// first item.  A row's partial sums of a unit are those of the pages from its first
+// token's segment on (from the kWeightAlign-fold before that, so that the lines that
+// the join reads are whole), `tiles` of them, which the pattern's segments bound and not
+// the table alone; a pattern's begin at one_slot times kWeightAlign floats.
+constexpr int64_t kWeightAlign = 32;
 constexpr int64_t kWeightPages = 1024;  // pages of an item at most
 constexpr int64_t kWeightApart = 256;   // (token, head) pairs of a unit up to which each wave has keys of its own
 struct WeightPlan {
@@ -174,8 +178,8 @@ struct WeightPlan {
   int dtype, page_log2, npat;
   float scale;
   bool lone;                 // rows are tokens
-  int64_t rows, units, items;
-  uint64_t workspace_bytes;  // float32 [units][rows][max_pages]
+  int64_t rows, items;
+  uint64_t workspace_bytes;  // float32, of each pattern [units][rows][pages]
   PagedPattern pat[DA_MAX_PATTERNS];
 };
 

@@ -54,3 +54,22 @@ def test_weights_count_columns_in_blocks_of_tokens():
     assert (T + 1) * sizes["H"] < 1 << 31 < (T + 32) * sizes["H"]
     assert plan_refuses(weights_need, **sizes) == "DA_EINVAL"
     assert weights_need(**dict(sizes, T=T - 64)) > 0
+
+
+PAPER = ((2048, 1), (4096, 2), (8192, 4), (16384, 6), (32768, 12))
+
+
+def test_the_weights_workspace_goes_by_the_segments_not_by_the_table():
+    """A row's sums are those of pages that its patterns reach: a wider table needs no
+    more, once it holds them."""
+    for T, B in ((1, 1), (64, 64), (1087, 64), (8255, 64)):
+        sizes = dict(T=T, B=B, H=32, Hkv=8, D=128, num_pages=1 << 16, patterns=PAPER)
+        got = [weights_need(max_pages=n, **sizes) for n in (4096, 8192, 65536, 1 << 20)]
+        assert got[0] == got[1] == got[2] == got[3]
+    # one token: a page more than a segment's at either end, of each pattern and head, in lines of 128 bytes
+    each = 4 * sum(w // 16 + 2 for w, _ in PAPER)
+    assert each <= weights_need(T=1, B=1, H=1, Hkv=1, max_pages=65536, patterns=PAPER) <= each + 5 * 256
+    assert 4 * 5 * 8 <= weights_need(T=1, B=1, H=1, Hkv=1, max_pages=8, patterns=PAPER) <= 5 * 128
+    # 64 sequences, 4096 new tokens of one: no more than the attention of the call
+    sizes = dict(T=4159, B=64, H=12, Hkv=12, D=64, num_pages=1 << 16, patterns=PAPER, max_pages=65536)
+    assert weights_need(**sizes) <= 2 * need(**sizes)
