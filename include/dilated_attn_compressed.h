@@ -33,16 +33,15 @@ typedef struct {
 
 /*
  * dilated_attn_cache_append_f8 - dilated_attn_cache_append into an 8-bit cache:
- * keys (normed and rotated in float32) and values are rounded to e4m3 once,
- * nearest even.  A block's scale is the least power of two, 2^-126 at least, whose
- * 448-fold is not below the block's largest finite magnitude; a block that has
- * tokens already keeps its scale or takes a larger one, its older values then
- * multiplied by the quotient (exact, but for those that fall below 2^-6 times the
- * new scale: these are rounded once more).  Scales never shrink while a block has
- * tokens; whoever wants to take an append back keeps a copy of the blocks in which
- * its tokens follow earlier ones.  Infinities and NaN
- * become NaN and do not count for the scale.  Finite magnitudes have to be below
- * 2^127.
+ * keys (normed and rotated in float32) and values are rounded to e4m3, nearest even.
+ * A block's scale is the least power of two, 2^-126 at least, whose 448-fold is not
+ * below the block's largest finite magnitude; a block that has tokens already keeps
+ * its scale or takes a larger one, its older values then multiplied by the quotient
+ * (exact, but for those that fall below 2^-6 times the new scale: these are rounded
+ * once more).  Scales never shrink while a block has tokens; whoever wants to take
+ * an append back keeps a copy of the blocks in which its tokens follow earlier ones.
+ * Infinities and NaN become NaN and do not count for the scale.  Finite magnitudes
+ * have to be below 2^127.
  *
  * Arguments as for dilated_attn_cache_append, dtype the type of q, k, v, qw, kw and
  * qo; T < 2^30.  A page belongs to one sequence of the call: two sequences that name
@@ -57,10 +56,11 @@ int dilated_attn_cache_append_f8(const void* q, const void* k, const void* v, co
 /*
  * dilated_attn_paged_fwd_f8 - dilated_attn_paged_fwd over an 8-bit cache; the
  * workspace is that of dilated_attn_paged_workspace.  dtype is the type of q and
- * out.  An element of the cache is exact in bf16 and float32, so that a result is
- * what dilated_attn_paged_fwd gives (up to the rounding of its sums) on a cache that
- * holds the same values; keys of pages that are not there are left out, and a row
- * all of whose keys are has out = 0 and lse = -inf.
+ * out.  An element of the cache of 2^-126 or more is exact in bf16 and float32 (a
+ * smaller one may count as zero), so that a result is what dilated_attn_paged_fwd
+ * gives (up to the rounding of its sums) on a cache that holds the same values; keys
+ * of pages that are not there are left out, and a row all of whose keys are has out = 0
+ * and lse = -inf.
  */
 int dilated_attn_paged_fwd_f8(const void* q, const da_paged_cache_f8_t* cache, void* out, float* lse, int64_t T,
                               int64_t B, int64_t H, int64_t Hkv, int64_t D, int64_t q_stride, int64_t max_new,

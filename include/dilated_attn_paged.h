@@ -74,8 +74,8 @@ int dilated_attn_qk_norm_xpos_bwd(const void* dqo, const void* dko, const void* 
 /*
  * A paged cache of keys and values, and the sequences of one call.
  *
- * A call has T new tokens of B sequences (1 <= B <= 2^31 - 2^16), side by side: those of sequence b
- * are rows q_start[b] .. q_start[b + 1] - 1 of its token arrays, and they are
+ * A call has T new tokens of B sequences (1 <= B <= 2^31 - 2^16), side by side:
+ * those of sequence b are rows q_start[b] .. q_start[b + 1] - 1 of its token arrays, and they are
  * the last of the seq_lens[b] tokens that the sequence has with them.  Token p
  * (0-based) of sequence b lies in page block_table[b][p / page_size] at
  * p % page_size.  The three arrays are device memory and read by the kernels:
@@ -155,9 +155,8 @@ int dilated_attn_cache_append(const void* q, const void* k, const void* v, const
  * dilated_attn_fwd for the sequence's own tokens; a row that sees a key whose
  * score is NaN or plus infinity is NaN in out and lse, and an element of v that is
  * not finite makes that element of the rows that see its key not finite, and of no
- * others.  What lies in the pool
- * beyond a sequence's length is never used, whatever it holds.  The same call gives
- * the same bits every time; keys are split by the sizes of the call, so a
+ * others.  What lies in the pool beyond a sequence's length is never used, whatever it
+ * holds.  The same call gives the same bits every time; keys are split by the sizes of the call, so a
  * sequence alone and in a batch can differ by the rounding of its sums.
  * Outputs and workspace must not overlap each other, q or the cache.
  */

@@ -4,15 +4,17 @@
 // are e4m3 times one power of two 2^e, the least with
 //   max |x| <= 448 * 2^e   (448: the largest e4m3 value),  e >= -126,
 // so that no value is cut off and a value keeps four significant bits down to
-// 2^-15 of the block's largest.  A block that has tokens already keeps its e or
+// 2^-13 of the block's largest (e4m3 is normal from 2^-6 on, the largest is above 224),
+// and is off by 2^-10 2^e at most below.  A block that has tokens already keeps its e or
 // takes a larger one, its older values then multiplied by a power of two: exact,
-// but for those that fall below e4m3's least normal value.
+// but for those that fall below e4m3's least normal value, which are rounded again.
 //
 // A workgroup is the new tokens of one block (16 at most), of a share of the
 // heads: D/8 lanes hold a row, eight elements each, the block's rows of several
 // heads at once; a head's largest value meets in LDS (a maximum of bits: in any
 // order the same).  Further workgroups have the queries, a token a wave.
-// Only rounding to fewer bits: keys and values to e4m3 once, from float32.
+// Only rounding to fewer bits: keys and values to e4m3, once from float32 and again
+// where a block's scale grows past them.
 //
 // Bound by HBM where there are many tokens: three prompts, 15 thousand tokens of 16
 // heads of 128 and four key heads, 133 MB in 30 us (4.4 TB/s; the wide cache's append

@@ -24,7 +24,8 @@
 // segment) of a pattern against 64-key tiles in LDS.  Bound by the matrix cores
 // and the softmax's vector work where a launch is long (8192 tokens of 12 heads of
 // 64, dense: 103 GFLOP in 150 us), by the start-up of an item (8 us) and the tail
-// where it is short (4096 tokens at 28672, five patterns: 31.9 GFLOP in 59 us).
+// where it is short (4096 tokens at 28672, five patterns: 31.9 GFLOP in 56 us, launch
+// after launch; 65 to 69 in the first ones after a pause).
 // Both write normalised partial rows with their log-sum-exps; paged_join mixes
 // a row's partials.
 //
@@ -955,10 +956,10 @@ __device__ inline void query_tiles(const PagedArgs& a, const TileItem& it, SmemT
   }
   // 8-bit caches: a thread has a quarter of a row of K and of V, whose loads are
   // under way while a tile is computed; they go to LDS as bf16, once for the four
-  // waves that read the tile.  (4096 tokens at 28672, five patterns: 70 us, and 58 with
+  // waves that read the tile.  (4096 tokens at 28672, five patterns: 60 us, and 56 with
   // a wide cache, whose rows go to LDS by themselves: 16 conversions and four stores a
   // thread and tile beside 32 exponentials.  Without rows and missing pages read a
-  // tile ahead: 73.)
+  // tile ahead the call takes 77.0 us where it takes 75.5.)
   constexpr int kPieces = D > 32 ? D / 64 : 1;  // 16-byte loads (D = 32: of 8 bytes) of a thread's quarter
   const int brow = tid >> 2, bpart = tid & 3;
   uint32_t kbytes[kPieces * 4], vbytes[kPieces * 4], kscale = 0, vscale = 0;

@@ -12,12 +12,12 @@
 // products with an e4m3 key are exact.  All sums are float32.
 //
 // Single tokens (64 at 1K to 32K cached, five patterns, 56 MB of keys): 33 us and the
-// join's 6.7.  Waves that look their own rows up, with the next tile's keys under way
+// join's 7.0.  Waves that look their own rows up, with the next tile's keys under way
 // and a segmented sum of a tile's pages, where a sum over the wave for each page took
 // 45 us and 256 keys a round of the workgroup 67.  What is left is the chain of an
 // item's start (lengths, table, queries, keys) and the tail, as in the attention.
 // Chunks (512 tokens at 31500, 16 heads of 128 over four key heads, five patterns, 6.1
-// GFLOP): 33 us and 6.4; with a tile of keys a workgroup in every pattern 45, and with
+// GFLOP): 33 us and 6.8; with a tile of keys a workgroup in every pattern 45, and with
 // every key operand read from LDS again for each 16 columns 159.  Bound by latency: an
 // item's start and its few steps of 16 columns, at two to three waves a SIMD.
 //
