@@ -81,19 +81,20 @@ class PagedCache:
         self.center = max_pages * page_size // 2 if center is None else center
         if xpos is not None:
             check_xpos(max_pages * page_size, self.center, *xpos)
+        if weigh and dtype != CACHE_F8:
+            raise ValueError(f"weigh goes with a cache of {CACHE_F8}")
         shape = (num_pages, num_heads, page_size, head_dim)
         self.k_scale = self.v_scale = self.weights = None
         self._blocks = []  # 8 bits: bytes of k, k_scale, v, v_scale [layers, num_pages, num_heads, blocks of a page, ...]
-        if dtype == CACHE_F8:
-            self.k, self.k_scale, self.v, self.v_scale = (self._pool(layers, *x, device) for x in (
-                (shape, dtype), (cache_scale_shape(shape), CACHE_SCALE)) * 2)
-        else:
-            self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
-            self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
-        if weigh:
-            if dtype != CACHE_F8:
-                raise ValueError(f"weigh goes with a cache of {CACHE_F8}")
-            self.weights = torch.zeros(num_pages, device=device)
+        with torch.inference_mode(False):  # extend and retract write them in any mode
+            if dtype == CACHE_F8:
+                self.k, self.k_scale, self.v, self.v_scale = (self._pool(layers, *x, device) for x in (
+                    (shape, dtype), (cache_scale_shape(shape), CACHE_SCALE)) * 2)
+            else:
+                self.k = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
+                self.v = [torch.empty(shape, device=device, dtype=dtype) for _ in range(layers)]
+            if weigh:
+                self.weights = torch.zeros(num_pages, device=device)
         self.page_size, self.max_pages = page_size, max_pages
         self.device = self.k[0].device
         self._free = list(range(num_pages - 1, -1, -1))

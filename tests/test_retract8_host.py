@@ -121,3 +121,16 @@ def test_wide_caches_keep_nothing():
     assert not cache._before
     cache.retract(batch)
     assert cache.length("a") == 5
+
+
+def test_a_cache_made_in_inference_mode_serves_outside():
+    for inside in (True, False):
+        with torch.inference_mode(not inside):
+            cache = make(weigh=True)
+        with torch.inference_mode(inside):
+            append(cache, cache.extend(["a"], [5]), rows(6, 5))
+            before = held(cache, "a")
+            batch = cache.extend(["a"], [1])
+            append(cache, batch, rows(7, 1, 100.0))
+            cache.retract(batch)
+            assert equal(held(cache, "a"), before)
